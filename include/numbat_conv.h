@@ -73,8 +73,15 @@ typedef enum {
   NUMBAT_OP_BN_SILU_FWD = 3,
   NUMBAT_OP_BN_SILU_BWD = 4,
   NUMBAT_OP_CLIP_SGD_NESTEROV = 5, /* problem ignored (may be NULL) */
-  NUMBAT_OP_CONV_BWD_DATA_BN_SILU = 6 /* numbat_conv_bwd_data_bn_silu_prologue: 0 bytes, or
+  NUMBAT_OP_CONV_BWD_DATA_BN_SILU = 6, /* numbat_conv_bwd_data_bn_silu_prologue: 0 bytes, or
                                          NUMBAT_ERR_UNSUPPORTED for a problem it does not take */
+  /* the functions of numbat_mlp.h (problem: a numbat_linear_problem* for the linear ops, a
+   * numbat_layer_norm_problem* for the layer norm; ignored for AdamW) */
+  NUMBAT_OP_LINEAR_FWD = 7,
+  NUMBAT_OP_LINEAR_BWD_DATA = 8,
+  NUMBAT_OP_LINEAR_BWD_WEIGHT = 9,
+  NUMBAT_OP_LAYER_NORM_BWD = 10,
+  NUMBAT_OP_ADAMW = 11
 } numbat_op;
 
 /* One 2-D convolution (dilation 1, one group).  Output size

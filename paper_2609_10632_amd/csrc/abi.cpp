@@ -13,6 +13,7 @@
 #include <vector>
 
 #include "../../include/numbat_conv.h"
+#include "abi_util.h"
 #include "kernels.h"
 
 using namespace numbat;
@@ -50,6 +51,14 @@ const char* const kClassNames[KC_COUNT] = {
     "conv_fwd_igemm", "stats_merge", "dgrad_weight_relayout", "conv_dgrad_igemm", "wgrad_igemm",
     "wgrad_splitk_reduce", "bn_stats", "bn_silu_fwd_apply", "bn_silu_bwd_reduce", "bn_silu_bwd_finalize",
     "bn_silu_bwd_apply", "narrow_input_pack", "opt_sumsq", "opt_update", "pool_upsample"};
+const char* const kMlpClassNames[KC_MLP_END - KC_MLP_FIRST] = {
+    "linear", "linear_pack", "linear_finish", "linear_bias_grad", "layer_norm_fwd", "layer_norm_bwd",
+    "layer_norm_bwd_finish", "adamw_norm", "adamw"};
+
+const char* class_name(int c) {
+  if (c >= 0 && c < KC_COUNT) return kClassNames[c];
+  return c >= KC_MLP_FIRST && c < KC_MLP_END ? kMlpClassNames[c - KC_MLP_FIRST] : nullptr;
+}
 
 }  // namespace
 
@@ -73,8 +82,10 @@ bool timing_events(hipEvent_t* start, hipEvent_t* stop) {
 }  // namespace numbat
 
 namespace {
-
 thread_local std::string g_err;
+}
+
+namespace numbat {
 
 numbat_status fail(numbat_status st, const char* fmt, ...) {
   char buf[512];
@@ -95,18 +106,17 @@ numbat_status hip_fail(hipError_t e, const char* what) {
   return fail(NUMBAT_ERR_DEVICE, "%s: %s", what, hipGetErrorString(e));
 }
 
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+numbat_status check_ws(void* ws, size_t have, size_t need) {
+  if (need == 0) return NUMBAT_OK;
+  if (ws == nullptr) return fail(NUMBAT_ERR_WORKSPACE, "workspace of %zu bytes required, got NULL", need);
+  if (have < need) return fail(NUMBAT_ERR_WORKSPACE, "workspace of %zu bytes required, got %zu", need, have);
+  if (!aligned16(ws)) return fail(NUMBAT_ERR_ALIGN, "workspace must be 16-byte aligned");
+  return NUMBAT_OK;
+}
 
-size_t round_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
+}  // namespace numbat
 
-// Every non-empty workspace begins with a 256-byte header of counters for the kernels'
-// grid-wide synchronisation (zero before a workspace's first use; every call leaves it
-// zero); the op's own data follows.
-constexpr size_t kWsHeader = 256;
-size_t with_header(size_t body) { return body ? body + kWsHeader : 0; }
-void* ws_body(void* ws) { return ws ? static_cast<char*>(ws) + kWsHeader : nullptr; }
-
-constexpr int64_t kMaxIndex = (1ll << 31) - 1;
+namespace {
 
 // ---------------------------------------------------------------------------
 struct ConvDesc {
@@ -531,14 +541,6 @@ size_t bn_bwd_ws(const BnDesc& d) {
   return round_up((size_t)nb * d.a.c * sizeof(float2), 256) + round_up(4 * d.a.c * sizeof(float), 256);
 }
 
-numbat_status check_ws(void* ws, size_t have, size_t need) {
-  if (need == 0) return NUMBAT_OK;
-  if (ws == nullptr) return fail(NUMBAT_ERR_WORKSPACE, "workspace of %zu bytes required, got NULL", need);
-  if (have < need) return fail(NUMBAT_ERR_WORKSPACE, "workspace of %zu bytes required, got %zu", need, have);
-  if (!aligned16(ws)) return fail(NUMBAT_ERR_ALIGN, "workspace must be 16-byte aligned");
-  return NUMBAT_OK;
-}
-
 // the checks of numbat_conv_fwd that do not involve the workspace
 numbat_status check_conv_fwd(const numbat_conv_problem* p, const void* x, const void* w, const void* y,
                              const float* batch_stats, ConvDesc* dp) {
@@ -652,7 +654,8 @@ uint32_t numbat_abi_version(void) { return NUMBAT_ABI_VERSION; }
 int numbat_kernel_class_count(void) { return KC_COUNT; }
 
 const char* numbat_kernel_class_name(int kernel_class) {
-  return (kernel_class >= 0 && kernel_class < KC_COUNT) ? kClassNames[kernel_class] : "";
+  const char* name = class_name(kernel_class);
+  return name ? name : "";
 }
 
 numbat_status numbat_timing_enable(int enable) {
@@ -665,7 +668,7 @@ numbat_status numbat_timing_enable(int enable) {
 
 numbat_status numbat_timing_read(int kernel_class, double* total_ms, int64_t* launches) {
   if (total_ms == nullptr || launches == nullptr) return fail(NUMBAT_ERR_NULL, "total_ms / launches is NULL");
-  if (kernel_class < 0 || kernel_class >= KC_COUNT) return fail(NUMBAT_ERR_BAD_DESC, "unknown kernel class %d", kernel_class);
+  if (class_name(kernel_class) == nullptr) return fail(NUMBAT_ERR_BAD_DESC, "unknown kernel class %d", kernel_class);
   std::lock_guard<std::mutex> lk(g_tmu);
   double t = 0;
   int64_t n = 0;
@@ -743,6 +746,10 @@ numbat_status numbat_workspace_size(numbat_op op, const void* problem, size_t* b
       if (st != NUMBAT_OK) return st;
       *bytes = with_header(op == NUMBAT_OP_BN_SILU_FWD ? bn_fwd_ws(d) : bn_bwd_ws(d));
       return ok();
+    }
+    default: {
+      numbat_status st;
+      if (mlp_workspace_size(op, problem, bytes, &st)) return st;
     }
   }
   return fail(NUMBAT_ERR_BAD_DESC, "unknown op %d", (int)op);

@@ -1,0 +1,555 @@
+// The matrix products of a linear layer on gfx950: y = act(x w^T + b) + r, the data gradient
+// (dy w) * act'(z) and the weight gradient dy^T x, as one tiled product
+//   C[m][n] = sum_k A(m, k) B(n, k)
+// whose operands either run along the reduction in memory ([m][k], [n][k]) or across it
+// ([k][m], [k][n]), with the layer's element-wise work in its epilogue.
+//
+// A block owns a BM x BN tile of C and walks the reduction in steps of BK.  A step's two
+// operand tiles are loaded by direct-to-LDS loads into one of S stages, in the operands' own
+// layout; the MFMA fragments (8 consecutive k of one row per lane) come out by 16-byte reads
+// where the operand runs along the reduction and by transposing reads (ds_read_b64_tr_b16)
+// where it runs across it, so neither form costs a register transpose or a copy in memory.
+// w's side is the MFMA's row operand: a lane's accumulators then hold 4 consecutive n of one
+// m, which the epilogue stages through LDS with 16-byte writes and stores as rows.
+//
+// Per step a block reads (BM + BN) * BK * 2 bytes of operands and issues BM * BN * BK
+// multiply-adds: a 256 x 256 tile needs 1/64 byte per flop, which the L2s deliver at the
+// matrix cores' rate; what bounds long reductions is the matrix cores, short ones (maps of
+// few channels) the bytes of x, z and y.
+#include <algorithm>
+
+#include "act.h"
+#include "mlp_kernels.h"
+
+namespace numbat {
+
+namespace {
+
+constexpr uint32_t kOob = 0x80000000u;  // a buffer offset past every range
+constexpr int kRecords = 0x7ffffff0;
+
+typedef __attribute__((address_space(3))) void lds_void_t;
+typedef short v4s_t __attribute__((ext_vector_type(4)));
+typedef unsigned v2u_t __attribute__((ext_vector_type(2)));
+typedef __attribute__((address_space(3))) v4s_t lds_v4s_t;
+
+template <int V>
+using Ic = std::integral_constant<int, V>;
+template <int I, int N, typename F>
+__device__ __forceinline__ void static_for(F&& f) {
+  if constexpr (I < N) {
+    f(Ic<I>{});
+    static_for<I + 1, N>(f);
+  }
+}
+
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rsrc(const void* base) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), (short)0, kRecords, 0x00020000);
+}
+
+// ---------------------------------------------------------------------------
+// The epilogue on NV consecutive columns of one row (NV = 8: 16-byte accesses, or 1).
+template <int NV>
+__device__ __forceinline__ void load_cols(const bf16_t* p, float (&f)[NV]) {
+  if constexpr (NV == 8) unpack8(*reinterpret_cast<const uint4*>(p), f);
+  else f[0] = bf2f(*p);
+}
+template <int NV>
+__device__ __forceinline__ void load_cols(const float* p, float (&f)[NV]) {
+  if constexpr (NV == 8) {
+    const float4 lo = reinterpret_cast<const float4*>(p)[0], hi = reinterpret_cast<const float4*>(p)[1];
+    f[0] = lo.x; f[1] = lo.y; f[2] = lo.z; f[3] = lo.w;
+    f[4] = hi.x; f[5] = hi.y; f[6] = hi.z; f[7] = hi.w;
+  } else {
+    f[0] = *p;
+  }
+}
+template <int NV>
+__device__ __forceinline__ void store_cols(bf16_t* p, const float (&f)[NV]) {
+  if constexpr (NV == 8) {
+    const uint4 v = pack8(f);
+    __builtin_nontemporal_store(u32x4{v.x, v.y, v.z, v.w}, reinterpret_cast<u32x4*>(p));
+  } else {
+    *p = (bf16_t)f2bf(f[0]);
+  }
+}
+template <int NV>
+__device__ __forceinline__ void store_cols(float* p, const float (&f)[NV]) {
+  if constexpr (NV == 8) {
+    __builtin_nontemporal_store(f32x4{f[0], f[1], f[2], f[3]}, reinterpret_cast<f32x4*>(p));
+    __builtin_nontemporal_store(f32x4{f[4], f[5], f[6], f[7]}, reinterpret_cast<f32x4*>(p) + 1);
+  } else {
+    *p = f[0];
+  }
+}
+
+// f: the sums; bias: those of the columns
+template <int KIND, int NV>
+__device__ __forceinline__ void finish_cols(const GemmEpilogue& e, int64_t row, int col, float (&f)[NV],
+                                            const float (&bias)[NV]) {
+  float o[NV];
+  if constexpr (KIND == kGemmFwd) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) f[i] += bias[i];
+    if (e.z != nullptr) store_cols<NV>(e.z + row * e.ldz + col, f);
+    if (e.act != kActNone) {
+#pragma unroll
+      for (int i = 0; i < NV; ++i) f[i] = act_apply(f[i], e.act);
+    }
+    if (e.res != nullptr) {
+      if (e.out_f32) load_cols<NV>(static_cast<const float*>(e.res) + row * e.ldr + col, o);
+      else load_cols<NV>(static_cast<const bf16_t*>(e.res) + row * e.ldr + col, o);
+#pragma unroll
+      for (int i = 0; i < NV; ++i) f[i] += o[i];
+    }
+    if (e.out_f32) store_cols<NV>(static_cast<float*>(e.out) + row * e.ldo + col, f);
+    else store_cols<NV>(static_cast<bf16_t*>(e.out) + row * e.ldo + col, f);
+  } else if constexpr (KIND == kGemmDgrad) {
+    if (e.act != kActNone) {
+      load_cols<NV>(e.z + row * e.ldz + col, o);
+#pragma unroll
+      for (int i = 0; i < NV; ++i) f[i] *= act_slope(o[i], e.act);
+    }
+    bf16_t* p = static_cast<bf16_t*>(e.out) + row * e.ldo + col;
+    if (e.accumulate) {
+      load_cols<NV>(p, o);
+#pragma unroll
+      for (int i = 0; i < NV; ++i) f[i] += o[i];
+    }
+    store_cols<NV>(p, f);
+  } else {
+    float* p = static_cast<float*>(e.out) + row * e.ldo + col;
+    if (e.accumulate) {
+      load_cols<NV>(p, o);
+#pragma unroll
+      for (int i = 0; i < NV; ++i) f[i] += o[i];
+    }
+    store_cols<NV>(p, f);
+  }
+}
+
+template <int KIND, int NV>
+__device__ __forceinline__ void load_bias(const GemmEpilogue& e, int col, int n, float (&b)[NV]) {
+#pragma unroll
+  for (int i = 0; i < NV; ++i) b[i] = 0.f;
+  if constexpr (KIND == kGemmFwd) {
+    if (e.bias != nullptr && col < n) load_cols<NV>(e.bias + col, b);
+  }
+}
+
+// ---------------------------------------------------------------------------
+template <int BM_, int BN_, int BK_, int S_, int WM_, int WN_>
+struct Tile {
+  static constexpr int BM = BM_, BN = BN_, BK = BK_, S = S_, WM = WM_, WN = WN_, NW = WM * WN;
+  static constexpr int TM = BM / WM / 32, TN = BN / WN / 32;   // 32 x 32 blocks per wave
+  static constexpr int A_BYTES = BM * BK * 2, B_BYTES = BN * BK * 2, STAGE = A_BYTES + B_BYTES;
+  static constexpr int AI = A_BYTES / 1024 / NW, BI = B_BYTES / 1024 / NW;  // load instructions per wave
+  static constexpr int KS = BK / 16;
+  static constexpr int OW = TN == 1 ? 32 : 64;                 // columns a wave stages at a time
+  static constexpr int OLD = OW + 4;                           // fp32 per staged row
+  static constexpr int OUT_BYTES = 32 * OLD * 4;               // per wave
+  static constexpr int WPS = (NW + S - 1) / S;                 // waves that stage in one stage's space
+  static_assert(A_BYTES % (1024 * NW) == 0 && B_BYTES % (1024 * NW) == 0, "whole load instructions");
+  static_assert(WPS * OUT_BYTES <= STAGE, "the epilogue fits the stages");
+  static_assert(KS % 2 == 0 && S >= 2 && S <= 4, "two fragment buffers, 2 to 4 stages");
+  static_assert(TN == 1 || TN % 2 == 0, "whole staging strips");
+};
+
+// An operand tile of SIDE rows of C (or columns) by BK of the reduction, as LDS holds it.
+//  T false: [SIDE][BK], rows of 2 BK bytes; 16-byte chunk c of row r in slot c ^ (r / WIN % CPR),
+//           WIN rows filling the 64 banks once, so that 16 rows' reads of one chunk spread over them
+//  T true:  [BK][SIDE]; chunk c of row r in slot c ^ swz(r): a transposing read of 32 lanes covers
+//           4 rows x 64 bytes, which the swizzle puts in different quarters of the banks
+template <bool T, int SIDE, int BK, int NW, int NI>
+struct Operand {
+  static constexpr int CPR = BK / 8, WIN = 128 / BK;
+  static __device__ __forceinline__ int swz(int r) { return SIDE == 64 ? 4 * ((r >> 1) & 1) : 4 * (r & 3); }
+
+  const unsigned char* base;  // first element of the tile's rows, at the block's first k
+  int64_t step;               // bytes to the next step
+  uint32_t off[NI];           // this lane's part of each load instruction, kOob past the matrix
+  int kpos[T ? NI : 1];       // its k within a step
+
+  __device__ __forceinline__ void init(const bf16_t* p, int64_t ld, int64_t r0, int64_t rows, int64_t k0, int wave,
+                                       int lane) {
+    if constexpr (!T) {
+      base = reinterpret_cast<const unsigned char*>(p + r0 * ld + k0);
+      step = 2 * BK;
+#pragma unroll
+      for (int q = 0; q < NI; ++q) {
+        const int row = (q * NW + wave) * (512 / BK) + lane / CPR;
+        const int chunk = (lane % CPR) ^ (row / WIN % CPR);  // the same for every q: NW is even
+        kpos[0] = chunk * 8;
+        off[q] = r0 + row < rows ? (uint32_t)(row * ld * 2) + chunk * 16 : kOob;
+      }
+    } else {
+      base = reinterpret_cast<const unsigned char*>(p + k0 * ld + r0);
+      step = 2 * BK * ld;
+#pragma unroll
+      for (int q = 0; q < NI; ++q) {
+        const int byte = (q * NW + wave) * 1024 + lane * 16;
+        const int row = byte / (2 * SIDE), chunk = (byte % (2 * SIDE)) / 16 ^ swz(row);
+        kpos[q] = row;
+        off[q] = r0 + chunk * 8 < rows ? (uint32_t)(row * ld * 2) + chunk * 16 : kOob;
+      }
+    }
+  }
+
+  // the loads of the next step, of which `left` k remain (none or fewer: zeros)
+  __device__ __forceinline__ void issue(unsigned char* stage, int64_t left, int wave) {
+    const __amdgpu_buffer_rsrc_t rs = rsrc(base);
+#pragma unroll
+    for (int q = 0; q < NI; ++q) {
+      const uint32_t vo = kpos[T ? q : 0] < left ? off[q] : kOob;
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_void_t*)(stage + (q * NW + wave) * 1024), 16, vo, 0, 0, 0);
+    }
+    base += step;
+  }
+};
+
+// fragment addresses of NB blocks of 32 rows from row `first` of an operand tile
+template <bool T, int SIDE, int BK, int NB>
+struct Frags {
+  using Op = Operand<T, SIDE, BK, 2, 1>;
+  uint32_t at[T ? NB : BK / 16];
+  __device__ __forceinline__ void init(int first, int lane) {
+    if constexpr (!T) {
+      const int l32 = lane & 31, half = lane >> 5;
+#pragma unroll
+      for (int ks = 0; ks < BK / 16; ++ks)
+        at[ks] = (uint32_t)((first + l32) * (BK * 2) + ((2 * ks + half) ^ (l32 / Op::WIN % Op::CPR)) * 16);
+    } else {
+      // lane 16 g + 4 e + q reads 4 columns (8 bytes) of rows 8 (g / 2) + e and that + 4 of a
+      // 16-row slice; the read hands each lane 4 consecutive rows of one column
+      const int g = lane >> 4, e = (lane & 15) >> 2, q = lane & 3, r0 = 8 * (g >> 1) + e;
+#pragma unroll
+      for (int i = 0; i < NB; ++i) {
+        const int c = first / 8 + 4 * i + 2 * (g & 1) + (q >> 1);
+        at[i] = (uint32_t)(r0 * 2 * SIDE + (c ^ Op::swz(r0)) * 16 + (q & 1) * 8);
+      }
+    }
+  }
+  __device__ __forceinline__ u32x4 read(const unsigned char* tile, int i, int ks) const {
+    if constexpr (!T) {
+      return *reinterpret_cast<const u32x4*>(tile + at[ks] + i * 32 * BK * 2);
+    } else {
+      const unsigned char* p = tile + at[i] + ks * 16 * 2 * SIDE;
+      const v2u_t lo = __builtin_bit_cast(v2u_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s_t*)p));
+      const v2u_t hi =
+          __builtin_bit_cast(v2u_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s_t*)(p + 4 * 2 * SIDE)));
+      return u32x4{lo.x, lo.y, hi.x, hi.y};
+    }
+  }
+};
+
+template <int KIND, typename C>
+__global__ __launch_bounds__(C::NW * 64) void gemm_kernel(GemmArgs a) {
+  constexpr bool TA = KIND == kGemmWgrad, TB = KIND != kGemmFwd;
+  constexpr int BM = C::BM, BN = C::BN, BK = C::BK, S = C::S, NW = C::NW, TM = C::TM, TN = C::TN, KS = C::KS;
+  // one object per stage: the compiler then knows that a stage's reads do not wait for the
+  // loads in flight into the others
+  __shared__ __attribute__((aligned(1024))) unsigned char st0[C::STAGE];
+  __shared__ __attribute__((aligned(1024))) unsigned char st1[C::STAGE];
+  __shared__ __attribute__((aligned(1024))) unsigned char st2[S > 2 ? C::STAGE : 16];
+  __shared__ __attribute__((aligned(1024))) unsigned char st3[S > 3 ? C::STAGE : 16];
+  auto stage = [&](auto uc) __attribute__((always_inline)) -> unsigned char* {
+    constexpr int u = decltype(uc)::value;
+    if constexpr (u == 0) return st0;
+    else if constexpr (u == 1) return st1;
+    else if constexpr (u == 2) return st2;
+    else return st3;
+  };
+
+  // tile of this block: each XCD takes a contiguous run of tiles, in columns of 8 tiles of m, so
+  // that the blocks running on it at a time share operand rows in its L2
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const uint32_t tiles = (uint32_t)a.tiles_m * (uint32_t)a.tiles_n;
+  uint32_t t = xcd_remap(blockIdx.x, gridDim.x);
+  const uint32_t split = t / tiles;
+  t -= split * tiles;
+  const uint32_t per_group = 8u * (uint32_t)a.tiles_n;
+  const uint32_t grp = t / per_group, in_grp = t - grp * per_group;
+  const uint32_t gsize = (uint32_t)a.tiles_m - grp * 8u < 8u ? (uint32_t)a.tiles_m - grp * 8u : 8u;
+  const uint32_t tn = in_grp / gsize, tm = grp * 8u + (in_grp - tn * gsize);
+  const int64_t m0 = (int64_t)tm * BM;
+  const int n0 = (int)tn * BN;
+  const int64_t k0 = (int64_t)split * a.k_per_split;
+  int64_t left = (a.k - k0 < a.k_per_split ? a.k - k0 : a.k_per_split);  // k not yet loaded
+  const int nk = (int)((left + BK - 1) / BK);
+
+  Operand<TA, BM, BK, NW, C::AI> oa;
+  Operand<TB, BN, BK, NW, C::BI> ob;
+  oa.init(a.a, a.lda, m0, a.m, k0, wave, lane);
+  ob.init(a.b, a.ldb, n0, a.n, k0, wave, lane);
+  auto issue = [&](auto uc) __attribute__((always_inline)) {
+    unsigned char* st = stage(uc);
+    oa.issue(st, left, wave);
+    ob.issue(st + C::A_BYTES, left, wave);
+    left -= BK;
+  };
+
+  const int wm = wave / C::WN, wn = wave % C::WN;
+  Frags<TA, BM, BK, TM> fa;
+  Frags<TB, BN, BK, TN> fb;
+  fa.init(wm * TM * 32, lane);
+  fb.init(wn * TN * 32, lane);
+
+  f32x16 acc[TM][TN];
+#pragma unroll
+  for (int i = 0; i < TM; ++i)
+#pragma unroll
+    for (int j = 0; j < TN; ++j)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
+
+  u32x4 af[2][TM], bf[2][TN];
+  auto rd = [&](auto uc, int ks, int b) __attribute__((always_inline)) {
+    const unsigned char* st = stage(uc);
+#pragma unroll
+    for (int i = 0; i < TM; ++i) af[b][i] = fa.read(st, i, ks);
+#pragma unroll
+    for (int j = 0; j < TN; ++j) bf[b][j] = fb.read(st + C::A_BYTES, j, ks);
+  };
+  auto mma = [&](int b) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+      for (int j = 0; j < TN; ++j) acc[i][j] = mfma32x32x16(bf[b][j], af[b][i], acc[i][j]);
+  };
+  // step kt multiplies out of stage u = kt mod S.  Before its last slice's products the wave's
+  // reads of the stage are done and the next stage's loads have landed (those of later ones stay
+  // in flight); past the barrier that holds for every wave, so the stage is refilled and the next
+  // one's first fragments are read behind those products.
+  auto step = [&](auto uc) __attribute__((always_inline)) {
+    constexpr int u = decltype(uc)::value;
+#pragma unroll
+    for (int ks = 0; ks + 1 < KS; ++ks) {
+      rd(uc, ks + 1, (ks + 1) & 1);
+      mma(ks & 1);
+    }
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((S - 2) * (C::AI + C::BI)) : "memory");
+    issue(uc);
+    rd(Ic<(u + 1) % S>{}, 0, 0);
+    mma((KS - 1) & 1);
+  };
+  static_for<0, S>([&](auto uc) { issue(uc); });
+  asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((S - 1) * (C::AI + C::BI)) : "memory");
+  rd(Ic<0>{}, 0, 0);
+  int kt = 0;
+  for (; kt + S <= nk; kt += S) static_for<0, S>([&](auto uc) { step(uc); });
+  static_for<0, S - 1>([&](auto uc) {
+    if (kt + decltype(uc)::value < nk) step(uc);
+  });
+  // the loads issued past the last step land before the stages become staging space
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+
+  // ---- epilogue: a wave stages 32 rows x OW columns of its sums as fp32 in LDS of its own and
+  // takes them out again as rows
+  const int ws = wave / C::WPS;
+  unsigned char* mine = ws == 0 ? st0 : ws == 1 ? st1 : ws == 2 ? st2 : st3;
+  float* out = reinterpret_cast<float*>(mine + (wave % C::WPS) * C::OUT_BYTES);
+  const int l32 = lane & 31, half = lane >> 5;
+  constexpr int JS = C::OW / 32;
+  constexpr int VPR = C::OW / 8, RPP = 64 / VPR;  // vectors per row, rows per pass
+  static_for<0, TN / JS>([&](auto jc) __attribute__((always_inline)) {
+    constexpr int js = decltype(jc)::value * JS;
+    const int c0 = n0 + (wn * TN + js) * 32;
+    const int vc = c0 + (lane % VPR) * 8, sc = c0 + lane % C::OW;
+    float vbias[8], sbias[1];
+    if (a.e.vec) load_bias<KIND, 8>(a.e, vc, a.n, vbias);
+    else load_bias<KIND, 1>(a.e, sc, a.n, sbias);
+    static_for<0, TM>([&](auto ic) __attribute__((always_inline)) {
+      constexpr int i = decltype(ic)::value;
+      const int64_t r0 = m0 + (wm * TM + i) * 32;
+#pragma unroll
+      for (int j = 0; j < JS; ++j)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const f32x16& x = acc[i][js + j];
+          *reinterpret_cast<f32x4*>(out + l32 * C::OLD + j * 32 + 8 * g + 4 * half) =
+              f32x4{x[4 * g], x[4 * g + 1], x[4 * g + 2], x[4 * g + 3]};
+        }
+      __builtin_amdgcn_wave_barrier();
+      if (a.splits > 1 || a.e.vec) {
+#pragma unroll 1
+        for (int p = 0; p < 32 / RPP; ++p) {
+          const int r = p * RPP + lane / VPR;
+          float f[8];
+          load_cols<8>(out + r * C::OLD + (lane % VPR) * 8, f);
+          if (r0 + r < a.m && vc < a.n) {
+            if (a.splits > 1)  // (the partials' rows are padded to whole vectors)
+              store_cols<8>(a.part + ((int64_t)split * a.m + r0 + r) * a.ldp + vc, f);
+            else
+              finish_cols<KIND, 8>(a.e, r0 + r, vc, f, vbias);
+          }
+        }
+      } else {
+#pragma unroll 1
+        for (int p = 0; p < 32 * C::OW / 64; ++p) {
+          const int r = p * (64 / C::OW) + lane / C::OW;
+          float f[1] = {out[r * C::OLD + lane % C::OW]};
+          if (r0 + r < a.m && sc < a.n) finish_cols<KIND, 1>(a.e, r0 + r, sc, f, sbias);
+        }
+      }
+      __builtin_amdgcn_wave_barrier();
+    });
+  });
+}
+
+// the sums of the reduction ranges, added in order, then the epilogue
+template <int KIND, int NV>
+__global__ __launch_bounds__(256) void gemm_finish_kernel(GemmArgs a) {
+  const int per_row = (a.n + NV - 1) / NV;
+  const int64_t total = a.m * per_row;
+  for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < total; i += gridDim.x * 256ll) {
+    const int64_t row = i / per_row;
+    const int col = (int)(i - row * per_row) * NV;
+    float f[NV], b[NV];
+#pragma unroll
+    for (int e = 0; e < NV; ++e) f[e] = 0.f;
+    const float* p = a.part + row * a.ldp + col;
+    for (int s = 0; s < a.splits; ++s, p += a.m * a.ldp) {
+      load_cols<NV>(p, b);
+#pragma unroll
+      for (int e = 0; e < NV; ++e) f[e] += b[e];
+    }
+    load_bias<KIND, NV>(a.e, col, a.n, b);
+    finish_cols<KIND, NV>(a.e, row, col, f, b);
+  }
+}
+
+__global__ __launch_bounds__(256) void gemm_pack_kernel(const bf16_t* src, int64_t lds, int64_t rows, int cols,
+                                                        bf16_t* dst, int64_t ldd) {
+  const int per_row = (int)(ldd / 8);
+  const int64_t total = rows * per_row;
+  for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < total; i += gridDim.x * 256ll) {
+    const int64_t row = i / per_row;
+    const int c = (int)(i - row * per_row) * 8;
+    const bf16_t* s = src + row * lds + c;
+    uint32_t h[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) h[e] = c + e < cols ? s[e] : 0;
+    *reinterpret_cast<uint4*>(dst + row * ldd + c) =
+        make_uint4(h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16);
+  }
+}
+
+// bias gradient: blocks of 256 columns x a range of rows; thread t sums column t
+constexpr int kColsumRanges = 256;
+__global__ __launch_bounds__(256) void colsum_part_kernel(const bf16_t* src, int64_t lds, int64_t rows, int cols,
+                                                          int64_t rows_per, float* part) {
+  const int c = blockIdx.x * 256 + threadIdx.x;
+  if (c >= cols) return;
+  const int64_t r0 = blockIdx.y * rows_per, r1 = r0 + rows_per < rows ? r0 + rows_per : rows;
+  float s = 0.f;
+  for (int64_t r = r0; r < r1; ++r) s += bf2f(src[r * lds + c]);
+  part[(int64_t)blockIdx.y * cols + c] = s;
+}
+__global__ __launch_bounds__(256) void colsum_finish_kernel(const float* part, int ranges, int cols, float* out,
+                                                            int accumulate) {
+  const int c = blockIdx.x * 256 + threadIdx.x;
+  if (c >= cols) return;
+  float s = 0.f;
+  for (int r = 0; r < ranges; ++r) s += part[(int64_t)r * cols + c];
+  out[c] = accumulate ? out[c] + s : s;
+}
+int64_t colsum_rows_per(int64_t rows) { return std::max<int64_t>(16, (rows + kColsumRanges - 1) / kColsumRanges); }
+
+__global__ __launch_bounds__(256) void fill_zero_kernel(float* p, int64_t n) {
+  for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < n; i += gridDim.x * 256ll) p[i] = 0.f;
+}
+
+unsigned grid_for(int64_t threads) { return (unsigned)std::min<int64_t>(4096, std::max<int64_t>(1, (threads + 255) / 256)); }
+
+using T256 = Tile<256, 256, 64, 2, 2, 2>;
+using T128 = Tile<128, 128, 64, 2, 2, 2>;
+using T64 = Tile<64, 64, 64, 3, 2, 2>;
+
+template <int KIND, typename C>
+hipError_t launch_tile(const GemmArgs& a, hipStream_t s) {
+  NUMBAT_LAUNCH((gemm_kernel<KIND, C>), dim3((unsigned)(a.tiles_m * a.tiles_n * a.splits)), dim3(C::NW * 64), 0, s, a);
+  return hipGetLastError();
+}
+
+template <int KIND>
+hipError_t launch_kind(const GemmArgs& a, int tile, hipStream_t s) {
+  trace_begin(KC_LINEAR);
+  hipError_t e = tile == 0   ? launch_tile<KIND, T256>(a, s)
+                 : tile == 1 ? launch_tile<KIND, T128>(a, s)
+                             : launch_tile<KIND, T64>(a, s);
+  trace_end(KC_LINEAR);
+  if (e != hipSuccess || a.splits == 1) return e;
+  trace_begin(KC_LINEAR_FINISH);
+  if (a.e.vec) NUMBAT_LAUNCH((gemm_finish_kernel<KIND, 8>), dim3(grid_for(a.m * ((a.n + 7) / 8))), dim3(256), 0, s, a);
+  else NUMBAT_LAUNCH((gemm_finish_kernel<KIND, 1>), dim3(grid_for(a.m * a.n)), dim3(256), 0, s, a);
+  trace_end(KC_LINEAR_FINISH);
+  return hipGetLastError();
+}
+
+int tile_side(int tile) { return tile == 0 ? 256 : tile == 1 ? 128 : 64; }
+int64_t tile_count(int tile, int64_t m, int n) {
+  const int b = tile_side(tile);
+  return ((m + b - 1) / b) * ((n + b - 1) / b);
+}
+
+}  // namespace
+
+GemmPlan gemm_pick(GemmKind, int64_t m, int n, int64_t k) {
+  GemmPlan p{2, 1, 0};
+  if (tile_count(0, m, n) >= 256) p.tile = 0;
+  else if (tile_count(1, m, n) >= 256) p.tile = 1;
+  const int64_t tiles = tile_count(p.tile, m, n), steps = (k + 63) / 64;
+  if (tiles < 256) p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({512 / tiles, steps / 8, 64}));
+  p.k_per_split = (steps + p.splits - 1) / p.splits * 64;
+  p.splits = (int)((k + p.k_per_split - 1) / p.k_per_split);
+  return p;
+}
+
+size_t gemm_part_bytes(const GemmPlan& p, int64_t m, int n) {
+  return p.splits > 1 ? (size_t)p.splits * (size_t)m * ((n + 7) / 8 * 8) * sizeof(float) : 0;
+}
+
+hipError_t gemm_launch(GemmKind kind, GemmArgs a, const GemmPlan& p, hipStream_t s) {
+  const int b = tile_side(p.tile);
+  a.tiles_m = (int32_t)((a.m + b - 1) / b);
+  a.tiles_n = (a.n + b - 1) / b;
+  a.splits = p.splits;
+  a.k_per_split = p.k_per_split;
+  a.ldp = (a.n + 7) / 8 * 8;
+  return kind == kGemmFwd     ? launch_kind<kGemmFwd>(a, p.tile, s)
+         : kind == kGemmDgrad ? launch_kind<kGemmDgrad>(a, p.tile, s)
+                              : launch_kind<kGemmWgrad>(a, p.tile, s);
+}
+
+hipError_t gemm_pack_launch(const bf16_t* src, int64_t lds, int64_t rows, int32_t cols, bf16_t* dst, int64_t ldd,
+                            hipStream_t s) {
+  trace_begin(KC_LINEAR_PACK);
+  NUMBAT_LAUNCH(gemm_pack_kernel, dim3(grid_for(rows * (ldd / 8))), dim3(256), 0, s, src, lds, rows, cols, dst, ldd);
+  trace_end(KC_LINEAR_PACK);
+  return hipGetLastError();
+}
+
+size_t colsum_part_bytes(int64_t rows, int32_t cols) {
+  const int64_t per = colsum_rows_per(rows);
+  return (size_t)((rows + per - 1) / per) * cols * sizeof(float);
+}
+
+hipError_t colsum_launch(const bf16_t* src, int64_t lds, int64_t rows, int32_t cols, float* part, float* out,
+                         int accumulate, hipStream_t s) {
+  const int64_t per = colsum_rows_per(rows);
+  const unsigned ranges = (unsigned)((rows + per - 1) / per), cb = (unsigned)((cols + 255) / 256);
+  trace_begin(KC_LINEAR_BIAS_GRAD);
+  NUMBAT_LAUNCH(colsum_part_kernel, dim3(cb, ranges), dim3(256), 0, s, src, lds, rows, cols, per, part);
+  NUMBAT_LAUNCH(colsum_finish_kernel, dim3(cb), dim3(256), 0, s, (const float*)part, (int)ranges, cols, out, accumulate);
+  trace_end(KC_LINEAR_BIAS_GRAD);
+  return hipGetLastError();
+}
+
+hipError_t fill_zero_launch(float* p, int64_t n, hipStream_t s) {
+  trace_begin(KC_LINEAR_FINISH);
+  NUMBAT_LAUNCH(fill_zero_kernel, dim3(grid_for(n)), dim3(256), 0, s, p, n);
+  trace_end(KC_LINEAR_FINISH);
+  return hipGetLastError();
+}
+
+}  // namespace numbat

@@ -1,4 +1,5 @@
-"""Thin Python binding of the C ABI in ``include/numbat_conv.h`` (argument marshalling only).
+"""Thin Python binding of the C ABI in ``include/numbat_conv.h`` and ``include/numbat_mlp.h``
+(argument marshalling only).
 
 Every function here has the name of the C entry point it calls and does nothing but
 turn Python arguments into C arguments: tensors become device pointers (their
@@ -20,7 +21,11 @@ NUMBAT_ABI_VERSION = 1
 
 OK, ERR_NULL, ERR_BAD_DESC, ERR_UNSUPPORTED, ERR_ALIGN, ERR_WORKSPACE, ERR_DEVICE, ERR_VERSION = range(8)
 (OP_CONV_FWD, OP_CONV_BWD_DATA, OP_CONV_BWD_WEIGHT, OP_BN_SILU_FWD, OP_BN_SILU_BWD, OP_CLIP_SGD_NESTEROV,
- OP_CONV_BWD_DATA_BN_SILU) = range(7)
+ OP_CONV_BWD_DATA_BN_SILU, OP_LINEAR_FWD, OP_LINEAR_BWD_DATA, OP_LINEAR_BWD_WEIGHT, OP_LAYER_NORM_BWD,
+ OP_ADAMW) = range(12)
+BF16, F32 = range(2)
+MLP_KERNEL_CLASSES = range(64, 64 + 9)
+ACT_NONE, ACT_RELU, ACT_GELU, ACT_GELU_TANH, ACT_SILU = range(5)
 
 EXPORTED = (
     "numbat_abi_version", "numbat_last_error", "numbat_status_string", "numbat_conv_output_shape",
@@ -30,6 +35,10 @@ EXPORTED = (
     "numbat_conv_fwd_bias", "numbat_conv_bn_silu_infer", "numbat_bn_silu_infer",
     "numbat_maxpool5_fwd", "numbat_maxpool5_bwd", "numbat_upsample2x_fwd", "numbat_upsample2x_bwd",
     "numbat_conv_fwd_bn_silu_prologue", "numbat_conv_bwd_data_bn_silu_prologue",
+)
+EXPORTED_MLP = (
+    "numbat_linear_fwd", "numbat_linear_bwd_data", "numbat_linear_bwd_weight", "numbat_layer_norm_fwd",
+    "numbat_layer_norm_bwd", "numbat_adamw_step", "numbat_adamw_state_values",
 )
 
 
@@ -63,6 +72,26 @@ class numbat_sgd_group(ctypes.Structure):
     _fields_ = [("lr", ctypes.c_float), ("weight_decay", ctypes.c_float)]
 
 
+class numbat_linear_problem(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_uint32), ("n", ctypes.c_int32), ("k", ctypes.c_int32), ("act", ctypes.c_int32),
+                ("m", ctypes.c_int64), ("y_type", ctypes.c_int32), ("reserved", ctypes.c_int32),
+                ("x_row_stride", ctypes.c_int64), ("y_row_stride", ctypes.c_int64), ("r_row_stride", ctypes.c_int64),
+                ("z_row_stride", ctypes.c_int64)]
+
+
+class numbat_layer_norm_problem(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_uint32), ("c", ctypes.c_int32), ("m", ctypes.c_int64), ("eps", ctypes.c_float),
+                ("x_type", ctypes.c_int32), ("y_type", ctypes.c_int32), ("reserved", ctypes.c_int32),
+                ("x_row_stride", ctypes.c_int64), ("y_row_stride", ctypes.c_int64), ("r_row_stride", ctypes.c_int64),
+                ("dx_row_stride", ctypes.c_int64)]
+
+
+class numbat_adamw_tensor(ctypes.Structure):
+    _fields_ = [("w", ctypes.c_void_p), ("grad", ctypes.c_void_p), ("m", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("m_unit", ctypes.c_void_p), ("v_unit", ctypes.c_void_p), ("w_copy", ctypes.c_void_p),
+                ("n", ctypes.c_int64), ("group", ctypes.c_int32), ("grad_type", ctypes.c_int32)]
+
+
 class NumbatError(RuntimeError):
     def __init__(self, status: int, name: str, detail: str, call: str):
         super().__init__(f"{call}: {name}: {detail}")
@@ -84,6 +113,8 @@ def load() -> ctypes.CDLL:
         P, S = ctypes.c_void_p, ctypes.c_size_t
         CP, BP = ctypes.POINTER(numbat_conv_problem), ctypes.POINTER(numbat_bn_problem)
         PP = ctypes.POINTER(numbat_pool_problem)
+        LP, NP = ctypes.POINTER(numbat_linear_problem), ctypes.POINTER(numbat_layer_norm_problem)
+        D = ctypes.c_double
         sig = {
             "numbat_abi_version": (ctypes.c_uint32, []),
             "numbat_last_error": (ctypes.c_char_p, []),
@@ -109,6 +140,14 @@ def load() -> ctypes.CDLL:
             "numbat_conv_bwd_weight": (ctypes.c_int, [CP, P, P, P, ctypes.c_int, P, S, P]),
             "numbat_bn_silu_fwd": (ctypes.c_int, [BP, P, P, P, P, P, P, P, P, P, P, P, S, P]),
             "numbat_bn_silu_bwd": (ctypes.c_int, [BP, P, P, P, P, P, P, P, P, P, P, P, S, P]),
+            "numbat_linear_fwd": (ctypes.c_int, [LP, P, P, P, P, P, P, P, S, P]),
+            "numbat_linear_bwd_data": (ctypes.c_int, [LP, P, P, P, P, ctypes.c_int, P, S, P]),
+            "numbat_linear_bwd_weight": (ctypes.c_int, [LP, P, P, P, P, ctypes.c_int, P, S, P]),
+            "numbat_layer_norm_fwd": (ctypes.c_int, [NP, P, P, P, P, P, P, P]),
+            "numbat_layer_norm_bwd": (ctypes.c_int, [NP, P, P, P, P, P, P, P, P, P, ctypes.c_int, P, S, P]),
+            "numbat_adamw_step": (ctypes.c_int, [P, ctypes.c_int32, ctypes.POINTER(numbat_sgd_group), ctypes.c_int32,
+                                                  ctypes.c_int32, D, D, D, ctypes.c_int64, D, P, P, S, P]),
+            "numbat_adamw_state_values": (ctypes.c_int, [ctypes.c_int64, P, P, P, P, P, P, P]),
             "numbat_kernel_class_count": (ctypes.c_int, []),
             "numbat_kernel_class_name": (ctypes.c_char_p, [ctypes.c_int]),
             "numbat_timing_enable": (ctypes.c_int, [ctypes.c_int]),
@@ -221,7 +260,8 @@ def numbat_conv_output_shape(p: numbat_conv_problem):
 
 def numbat_workspace_size(op: int, p) -> int:
     n = ctypes.c_size_t()
-    _check(load().numbat_workspace_size(op, ctypes.cast(ctypes.pointer(p), ctypes.c_void_p), ctypes.byref(n)),
+    desc = None if p is None else ctypes.cast(ctypes.pointer(p), ctypes.c_void_p)
+    _check(load().numbat_workspace_size(op, desc, ctypes.byref(n)),
            "numbat_workspace_size")
     return n.value
 
@@ -320,6 +360,83 @@ def numbat_clip_sgd_nesterov(tensors, count, groups, momentum_factor, max_norm, 
                                            _ptr(total_norm), _ptr(ws), _nbytes(ws) if ws_bytes is None else ws_bytes,
                                            _stream(stream)),
            "numbat_clip_sgd_nesterov")
+
+
+def linear_problem(m, n, k, act=ACT_NONE, y_type=BF16, x_row_stride=0, y_row_stride=0, r_row_stride=0,
+                   z_row_stride=0):
+    return numbat_linear_problem(ctypes.sizeof(numbat_linear_problem), n, k, act, m, y_type, 0, x_row_stride,
+                                 y_row_stride, r_row_stride, z_row_stride)
+
+
+def layer_norm_problem(m, c, eps=1e-5, x_type=BF16, y_type=BF16, x_row_stride=0, y_row_stride=0, r_row_stride=0,
+                       dx_row_stride=0):
+    return numbat_layer_norm_problem(ctypes.sizeof(numbat_layer_norm_problem), c, m, eps, x_type, y_type, 0,
+                                     x_row_stride, y_row_stride, r_row_stride, dx_row_stride)
+
+
+def numbat_linear_fwd(p, x, w, bias, residual, z, y, ws=None, stream=None, ws_bytes=None):
+    _check(load().numbat_linear_fwd(ctypes.byref(p), _ptr(x), _ptr(w), _ptr(bias), _ptr(residual), _ptr(z), _ptr(y),
+                                    _ptr(ws), _nbytes(ws) if ws_bytes is None else ws_bytes, _stream(stream)),
+           "numbat_linear_fwd")
+
+
+def numbat_linear_bwd_data(p, dy, w, z, dx, accumulate=False, ws=None, stream=None, ws_bytes=None):
+    _check(load().numbat_linear_bwd_data(ctypes.byref(p), _ptr(dy), _ptr(w), _ptr(z), _ptr(dx), int(bool(accumulate)),
+                                         _ptr(ws), _nbytes(ws) if ws_bytes is None else ws_bytes, _stream(stream)),
+           "numbat_linear_bwd_data")
+
+
+def numbat_linear_bwd_weight(p, x, dy, dw, db=None, accumulate=False, ws=None, stream=None, ws_bytes=None):
+    _check(load().numbat_linear_bwd_weight(ctypes.byref(p), _ptr(x), _ptr(dy), _ptr(dw), _ptr(db),
+                                           int(bool(accumulate)), _ptr(ws),
+                                           _nbytes(ws) if ws_bytes is None else ws_bytes, _stream(stream)),
+           "numbat_linear_bwd_weight")
+
+
+def numbat_layer_norm_fwd(p, x, gamma, beta, y, mean=None, rstd=None, stream=None):
+    _check(load().numbat_layer_norm_fwd(ctypes.byref(p), _ptr(x), _ptr(gamma), _ptr(beta), _ptr(y), _ptr(mean),
+                                        _ptr(rstd), _stream(stream)),
+           "numbat_layer_norm_fwd")
+
+
+def numbat_layer_norm_bwd(p, dy, x, mean, rstd, gamma, residual_grad, dx, dgamma, dbeta, accumulate=False, ws=None,
+                          stream=None, ws_bytes=None):
+    _check(load().numbat_layer_norm_bwd(ctypes.byref(p), _ptr(dy), _ptr(x), _ptr(mean), _ptr(rstd), _ptr(gamma),
+                                        _ptr(residual_grad), _ptr(dx), _ptr(dgamma), _ptr(dbeta),
+                                        int(bool(accumulate)), _ptr(ws),
+                                        _nbytes(ws) if ws_bytes is None else ws_bytes, _stream(stream)),
+           "numbat_layer_norm_bwd")
+
+
+def adamw_table(entries):
+    """numbat_adamw_tensor entries as bytes laid out like the C array (upload them to the device
+    to pass as `tensors`).  Each entry is a dict of the tensors ``w``, ``grad``, ``m``, ``v`` and the
+    ``group``; with 8-bit state ``m_unit`` and ``v_unit``; ``w_copy`` where a bf16 copy is wanted.
+    The gradient's type is its tensor's."""
+    arr = (numbat_adamw_tensor * len(entries))()
+    for e, d in zip(arr, entries):
+        for f in ("w", "grad", "m", "v", "m_unit", "v_unit", "w_copy"):
+            setattr(e, f, _ptr(d.get(f)))
+        e.n, e.group = d["w"].numel(), d["group"]
+        e.grad_type = BF16 if d["grad"].element_size() == 2 else F32
+    return bytes(arr)
+
+
+def numbat_adamw_step(tensors, count, groups, state_bits, beta1, beta2, eps, step, max_norm=0.0, total_norm=None,
+                      ws=None, stream=None, ws_bytes=None):
+    """tensors: device buffer holding `count` numbat_adamw_tensor entries; groups: list of
+    (lr, weight_decay) pairs."""
+    g = (numbat_sgd_group * len(groups))(*[numbat_sgd_group(lr, wd) for lr, wd in groups])
+    _check(load().numbat_adamw_step(_ptr(tensors), count, g, len(groups), state_bits, beta1, beta2, eps, step, max_norm,
+                                    _ptr(total_norm), _ptr(ws), _nbytes(ws) if ws_bytes is None else ws_bytes,
+                                    _stream(stream)),
+           "numbat_adamw_step")
+
+
+def numbat_adamw_state_values(n, m, m_unit, v, v_unit, m_value, v_value, stream=None):
+    _check(load().numbat_adamw_state_values(n, _ptr(m), _ptr(m_unit), _ptr(v), _ptr(v_unit), _ptr(m_value),
+                                            _ptr(v_value), _stream(stream)),
+           "numbat_adamw_state_values")
 
 
 def numbat_kernel_class_count() -> int:
