@@ -195,15 +195,10 @@ struct Operand {
     }
   }
 
-  // the loads of the next step, of which `left` k remain (none or fewer: zeros)
-  __device__ __forceinline__ void issue(unsigned char* stage, int64_t left, int wave) {
-    const __amdgpu_buffer_rsrc_t rs = rsrc(base);
-#pragma unroll
-    for (int q = 0; q < NI; ++q) {
-      const uint32_t vo = kpos[T ? q : 0] < left ? off[q] : kOob;
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_void_t*)(stage + (q * NW + wave) * 1024), 16, vo, 0, 0, 0);
-    }
-    base += step;
+  // load instruction q of the next step, of which `left` k remain (none or fewer: zeros)
+  __device__ __forceinline__ void load(unsigned char* stage, int q, int64_t left, int wave) const {
+    const uint32_t vo = kpos[T ? q : 0] < left ? off[q] : kOob;
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc(base), (lds_void_t*)(stage + (q * NW + wave) * 1024), 16, vo, 0, 0, 0);
   }
 };
 
@@ -281,10 +276,16 @@ __global__ __launch_bounds__(C::NW * 64) void gemm_kernel(GemmArgs a) {
   Operand<TB, BN, BK, NW, C::BI> ob;
   oa.init(a.a, a.lda, m0, a.m, k0, wave, lane);
   ob.init(a.b, a.ldb, n0, a.n, k0, wave, lane);
-  auto issue = [&](auto uc) __attribute__((always_inline)) {
+  // load instruction q of the step that `left` counts, A's first
+  constexpr int L = C::AI + C::BI;
+  auto load = [&](auto uc, int q) __attribute__((always_inline)) {
     unsigned char* st = stage(uc);
-    oa.issue(st, left, wave);
-    ob.issue(st + C::A_BYTES, left, wave);
+    if (q < C::AI) oa.load(st, q, left, wave);
+    else ob.load(st + C::A_BYTES, q - C::AI, left, wave);
+  };
+  auto advance = [&]() __attribute__((always_inline)) {
+    oa.base += oa.step;
+    ob.base += ob.step;
     left -= BK;
   };
 
@@ -303,38 +304,53 @@ __global__ __launch_bounds__(C::NW * 64) void gemm_kernel(GemmArgs a) {
       for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
 
   u32x4 af[2][TM], bf[2][TN];
-  auto rd = [&](auto uc, int ks, int b) __attribute__((always_inline)) {
+  // fragment r of slice ks of a stage, A's first, into buffer b
+  auto rd = [&](auto uc, int r, int ks, int b) __attribute__((always_inline)) {
     const unsigned char* st = stage(uc);
-#pragma unroll
-    for (int i = 0; i < TM; ++i) af[b][i] = fa.read(st, i, ks);
-#pragma unroll
-    for (int j = 0; j < TN; ++j) bf[b][j] = fb.read(st + C::A_BYTES, j, ks);
+    if (r < TM) af[b][r] = fa.read(st, r, ks);
+    else bf[b][r - TM] = fb.read(st + C::A_BYTES, r - TM, ks);
   };
-  auto mma = [&](int b) __attribute__((always_inline)) {
+  // The products of slice ks of stage u, with the reads of the next slice's fragments behind the
+  // first half of them and a share of the step's loads spread over them.  Pinned: left to itself the
+  // compiler sinks each read to its use, and a SIMD with one wave then waits out the LDS's latency
+  // in every slice.
+  constexpr int LOADING = S == 2 ? KS - 1 : KS;  // slices that carry loads
+  auto slice = [&](auto uc, auto kc) __attribute__((always_inline)) {
+    constexpr int u = decltype(uc)::value, ks = decltype(kc)::value, b = ks & 1;
+    constexpr bool last = ks == KS - 1;
+    constexpr int L0 = ks < LOADING ? ks * L / LOADING : L, L1 = ks < LOADING ? (ks + 1) * L / LOADING : L;
+    constexpr int NM = TM * TN, NR = TM + TN, RW = NM >= 2 * NR ? NM / 2 : NM;
+    static_for<0, NM>([&](auto tc) __attribute__((always_inline)) {
+      constexpr int t = decltype(tc)::value;
+      constexpr int r0 = t < RW ? t * NR / RW : NR, r1 = t < RW ? (t + 1) * NR / RW : NR;
+      constexpr int l0 = L0 + t * (L1 - L0) / NM, l1 = L0 + (t + 1) * (L1 - L0) / NM;
 #pragma unroll
-    for (int i = 0; i < TM; ++i)
+      for (int r = r0; r < r1; ++r) rd(Ic<last ? (u + 1) % S : u>{}, r, last ? 0 : ks + 1, b ^ 1);
 #pragma unroll
-      for (int j = 0; j < TN; ++j) acc[i][j] = mfma32x32x16(bf[b][j], af[b][i], acc[i][j]);
+      for (int q = l0; q < l1; ++q) load(Ic<(u + S - 1) % S>{}, q);
+      acc[t / TN][t % TN] = mfma32x32x16(bf[b][t % TN], af[b][t / TN], acc[t / TN][t % TN]);
+      __builtin_amdgcn_sched_barrier(0);
+    });
   };
-  // step kt multiplies out of stage u = kt mod S.  Before its last slice's products the wave's
-  // reads of the stage are done and the next stage's loads have landed (those of later ones stay
-  // in flight); past the barrier that holds for every wave, so the stage is refilled and the next
-  // one's first fragments are read behind those products.
+  // Step kt multiplies out of stage u = kt mod S and loads step kt + S - 1 into the stage read last
+  // step.  Before its last slice the wave's reads of the stage are done and the next step's loads
+  // have landed (those of later steps stay in flight); past the barrier that holds for every wave,
+  // so the last slice can read the next stage.
+  constexpr int PENDING = S == 2 ? 0 : (S - 3) * L + (KS - 1) * L / KS;
   auto step = [&](auto uc) __attribute__((always_inline)) {
-    constexpr int u = decltype(uc)::value;
-#pragma unroll
-    for (int ks = 0; ks + 1 < KS; ++ks) {
-      rd(uc, ks + 1, (ks + 1) & 1);
-      mma(ks & 1);
-    }
-    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((S - 2) * (C::AI + C::BI)) : "memory");
-    issue(uc);
-    rd(Ic<(u + 1) % S>{}, 0, 0);
-    mma((KS - 1) & 1);
+    static_for<0, KS - 1>([&](auto kc) __attribute__((always_inline)) { slice(uc, kc); });
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(PENDING) : "memory");
+    slice(uc, Ic<KS - 1>{});
+    advance();
   };
-  static_for<0, S>([&](auto uc) { issue(uc); });
-  asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((S - 1) * (C::AI + C::BI)) : "memory");
-  rd(Ic<0>{}, 0, 0);
+  static_for<0, S - 1>([&](auto uc) {
+#pragma unroll
+    for (int q = 0; q < L; ++q) load(uc, q);
+    advance();
+  });
+  asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((S - 2) * L) : "memory");
+#pragma unroll
+  for (int r = 0; r < TM + TN; ++r) rd(Ic<0>{}, r, 0, 0);
   int kt = 0;
   for (; kt + S <= nk; kt += S) static_for<0, S>([&](auto uc) { step(uc); });
   static_for<0, S - 1>([&](auto uc) {
@@ -461,7 +477,7 @@ __global__ __launch_bounds__(256) void fill_zero_kernel(float* p, int64_t n) {
 
 unsigned grid_for(int64_t threads) { return (unsigned)std::min<int64_t>(4096, std::max<int64_t>(1, (threads + 255) / 256)); }
 
-using T256 = Tile<256, 256, 64, 2, 2, 2>;
+using T256 = Tile<256, 256, 32, 4, 2, 2>;
 using T128 = Tile<128, 128, 64, 2, 2, 2>;
 using T64 = Tile<64, 64, 64, 3, 2, 2>;
 
