@@ -83,48 +83,99 @@ __device__ __forceinline__ void store_cols(float* p, const float (&f)[NV]) {
   }
 }
 
-// f: the sums; bias: those of the columns
+// The matrix that the epilogue reads beside the sums: the residual (forward), z (data gradient
+// through an activation) or the old values (weight gradient that accumulates).  Raw, so that its
+// loads can be issued early and cost few registers.
+template <int NV>
+struct Aux {
+  uint4 lo, hi;  // 8 bf16, or 8 fp32; element 0 alone for NV = 1
+};
+template <int KIND>
+__device__ __forceinline__ const void* aux_base(const GemmEpilogue& e, int64_t* ld, bool* f32) {
+  *f32 = KIND == kGemmWgrad || (KIND == kGemmFwd && e.out_f32);
+  *ld = KIND == kGemmFwd ? e.ldr : KIND == kGemmDgrad ? e.ldz : e.ldo;
+  return KIND == kGemmFwd     ? e.res
+         : KIND == kGemmDgrad ? (e.act != kActNone ? e.z : nullptr)
+                              : (e.accumulate ? e.out : nullptr);
+}
+template <int KIND, int NV>
+__device__ __forceinline__ void load_aux(const GemmEpilogue& e, int64_t row, int col, Aux<NV>& x) {
+  int64_t ld;
+  bool f32;
+  const void* base = aux_base<KIND>(e, &ld, &f32);
+  if (base == nullptr) return;
+  const char* p = static_cast<const char*>(base) + (row * ld + col) * (f32 ? 4 : 2);
+  if constexpr (NV == 8) {
+    x.lo = *reinterpret_cast<const uint4*>(p);
+    if (f32) x.hi = *reinterpret_cast<const uint4*>(p + 16);
+  } else {
+    x.lo.x = f32 ? *reinterpret_cast<const uint32_t*>(p) : *reinterpret_cast<const uint16_t*>(p);
+  }
+}
+template <int NV>
+__device__ __forceinline__ void aux_values(const Aux<NV>& x, bool f32, float (&f)[NV]) {
+  if constexpr (NV == 8) {
+    if (f32) {
+      const uint32_t u[8] = {x.lo.x, x.lo.y, x.lo.z, x.lo.w, x.hi.x, x.hi.y, x.hi.z, x.hi.w};
+#pragma unroll
+      for (int i = 0; i < 8; ++i) f[i] = __uint_as_float(u[i]);
+    } else {
+      unpack8(x.lo, f);
+    }
+  } else {
+    f[0] = f32 ? __uint_as_float(x.lo.x) : bf2f(x.lo.x);
+  }
+}
+
+template <int NV, typename F>
+__device__ __forceinline__ void each(float (&f)[NV], F&& fn) {
+#pragma unroll
+  for (int i = 0; i < NV; ++i) f[i] = fn(i);
+}
+
+// f: the sums; bias: those of the columns; x: loaded by load_aux
 template <int KIND, int NV>
 __device__ __forceinline__ void finish_cols(const GemmEpilogue& e, int64_t row, int col, float (&f)[NV],
-                                            const float (&bias)[NV]) {
+                                            const float (&bias)[NV], const Aux<NV>& x) {
   float o[NV];
   if constexpr (KIND == kGemmFwd) {
-#pragma unroll
-    for (int i = 0; i < NV; ++i) f[i] += bias[i];
+    each(f, [&](int i) { return f[i] + bias[i]; });
     if (e.z != nullptr) store_cols<NV>(e.z + row * e.ldz + col, f);
-    if (e.act != kActNone) {
-#pragma unroll
-      for (int i = 0; i < NV; ++i) f[i] = act_apply(f[i], e.act);
+    // (one branch for the vector, not one per element)
+    switch (e.act) {
+      case kActRelu: each(f, [&](int i) { return act_apply(f[i], kActRelu); }); break;
+      case kActGelu: each(f, [&](int i) { return act_apply(f[i], kActGelu); }); break;
+      case kActGeluTanh: each(f, [&](int i) { return act_apply(f[i], kActGeluTanh); }); break;
+      case kActSilu: each(f, [&](int i) { return act_apply(f[i], kActSilu); }); break;
+      default: break;
     }
     if (e.res != nullptr) {
-      if (e.out_f32) load_cols<NV>(static_cast<const float*>(e.res) + row * e.ldr + col, o);
-      else load_cols<NV>(static_cast<const bf16_t*>(e.res) + row * e.ldr + col, o);
-#pragma unroll
-      for (int i = 0; i < NV; ++i) f[i] += o[i];
+      aux_values<NV>(x, e.out_f32, o);
+      each(f, [&](int i) { return f[i] + o[i]; });
     }
     if (e.out_f32) store_cols<NV>(static_cast<float*>(e.out) + row * e.ldo + col, f);
     else store_cols<NV>(static_cast<bf16_t*>(e.out) + row * e.ldo + col, f);
   } else if constexpr (KIND == kGemmDgrad) {
-    if (e.act != kActNone) {
-      load_cols<NV>(e.z + row * e.ldz + col, o);
-#pragma unroll
-      for (int i = 0; i < NV; ++i) f[i] *= act_slope(o[i], e.act);
+    if (e.act != kActNone) aux_values<NV>(x, false, o);
+    switch (e.act) {
+      case kActRelu: each(f, [&](int i) { return f[i] * act_slope(o[i], kActRelu); }); break;
+      case kActGelu: each(f, [&](int i) { return f[i] * act_slope(o[i], kActGelu); }); break;
+      case kActGeluTanh: each(f, [&](int i) { return f[i] * act_slope(o[i], kActGeluTanh); }); break;
+      case kActSilu: each(f, [&](int i) { return f[i] * act_slope(o[i], kActSilu); }); break;
+      default: break;
     }
     bf16_t* p = static_cast<bf16_t*>(e.out) + row * e.ldo + col;
     if (e.accumulate) {
       load_cols<NV>(p, o);
-#pragma unroll
-      for (int i = 0; i < NV; ++i) f[i] += o[i];
+      each(f, [&](int i) { return f[i] + o[i]; });
     }
     store_cols<NV>(p, f);
   } else {
-    float* p = static_cast<float*>(e.out) + row * e.ldo + col;
     if (e.accumulate) {
-      load_cols<NV>(p, o);
-#pragma unroll
-      for (int i = 0; i < NV; ++i) f[i] += o[i];
+      aux_values<NV>(x, true, o);
+      each(f, [&](int i) { return f[i] + o[i]; });
     }
-    store_cols<NV>(p, f);
+    store_cols<NV>(static_cast<float*>(e.out) + row * e.ldo + col, f);
   }
 }
 
@@ -365,51 +416,90 @@ __global__ __launch_bounds__(C::NW * 64) void gemm_kernel(GemmArgs a) {
   unsigned char* mine = ws == 0 ? st0 : ws == 1 ? st1 : ws == 2 ? st2 : st3;
   float* out = reinterpret_cast<float*>(mine + (wave % C::WPS) * C::OUT_BYTES);
   const int l32 = lane & 31, half = lane >> 5;
-  constexpr int JS = C::OW / 32;
-  constexpr int VPR = C::OW / 8, RPP = 64 / VPR;  // vectors per row, rows per pass
-  static_for<0, TN / JS>([&](auto jc) __attribute__((always_inline)) {
-    constexpr int js = decltype(jc)::value * JS;
-    const int c0 = n0 + (wn * TN + js) * 32;
-    const int vc = c0 + (lane % VPR) * 8, sc = c0 + lane % C::OW;
-    float vbias[8], sbias[1];
-    if (a.e.vec) load_bias<KIND, 8>(a.e, vc, a.n, vbias);
-    else load_bias<KIND, 1>(a.e, sc, a.n, sbias);
-    static_for<0, TM>([&](auto ic) __attribute__((always_inline)) {
-      constexpr int i = decltype(ic)::value;
-      const int64_t r0 = m0 + (wm * TM + i) * 32;
+  constexpr int JS = C::OW / 32, STRIPS = TN / JS * TM;
+  constexpr int VPR = C::OW / 8, RPP = 64 / VPR, NP = 32 / RPP;  // vectors per row, rows per pass, passes
+  // accumulators of strip s (rows first, then columns) into the wave's LDS
+  auto put = [&](auto sc) __attribute__((always_inline)) {
+    constexpr int i = decltype(sc)::value % TM, js = decltype(sc)::value / TM * JS;
 #pragma unroll
-      for (int j = 0; j < JS; ++j)
+    for (int j = 0; j < JS; ++j)
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          const f32x16& x = acc[i][js + j];
-          *reinterpret_cast<f32x4*>(out + l32 * C::OLD + j * 32 + 8 * g + 4 * half) =
-              f32x4{x[4 * g], x[4 * g + 1], x[4 * g + 2], x[4 * g + 3]};
-        }
+      for (int g = 0; g < 4; ++g) {
+        const f32x16& x = acc[i][js + j];
+        *reinterpret_cast<f32x4*>(out + l32 * C::OLD + j * 32 + 8 * g + 4 * half) =
+            f32x4{x[4 * g], x[4 * g + 1], x[4 * g + 2], x[4 * g + 3]};
+      }
+    __builtin_amdgcn_wave_barrier();
+  };
+  // the strip's first row and column
+  auto row_of = [&](int s) __attribute__((always_inline)) { return m0 + (wm * TM + s % TM) * 32; };
+  auto col_of = [&](int s) __attribute__((always_inline)) { return n0 + (wn * TN + s / TM * JS) * 32; };
+  if (a.splits > 1) {
+    static_for<0, STRIPS>([&](auto sc) __attribute__((always_inline)) {
+      constexpr int s = decltype(sc)::value;
+      put(sc);
+      const int vc = col_of(s) + (lane % VPR) * 8;
+#pragma unroll
+      for (int p = 0; p < NP; ++p) {
+        const int r = p * RPP + lane / VPR;
+        const int64_t row = row_of(s) + r;
+        float f[8];
+        load_cols<8>(out + r * C::OLD + (lane % VPR) * 8, f);
+        // (the partials' rows are padded to whole vectors)
+        if (row < a.m && vc < a.n) store_cols<8>(a.part + ((int64_t)split * a.m + row) * a.ldp + vc, f);
+      }
       __builtin_amdgcn_wave_barrier();
-      if (a.splits > 1 || a.e.vec) {
-#pragma unroll 1
-        for (int p = 0; p < 32 / RPP; ++p) {
-          const int r = p * RPP + lane / VPR;
-          float f[8];
-          load_cols<8>(out + r * C::OLD + (lane % VPR) * 8, f);
-          if (r0 + r < a.m && vc < a.n) {
-            if (a.splits > 1)  // (the partials' rows are padded to whole vectors)
-              store_cols<8>(a.part + ((int64_t)split * a.m + r0 + r) * a.ldp + vc, f);
-            else
-              finish_cols<KIND, 8>(a.e, r0 + r, vc, f, vbias);
-          }
-        }
-      } else {
-#pragma unroll 1
-        for (int p = 0; p < 32 * C::OW / 64; ++p) {
-          const int r = p * (64 / C::OW) + lane / C::OW;
-          float f[1] = {out[r * C::OLD + lane % C::OW]};
-          if (r0 + r < a.m && sc < a.n) finish_cols<KIND, 1>(a.e, r0 + r, sc, f, sbias);
+    });
+  } else if (a.e.vec) {
+    // the next strip's auxiliary loads are in flight while a strip is finished
+    Aux<8> x[2][NP];
+    float bias[8];
+    auto fetch = [&](int s, int b) __attribute__((always_inline)) {
+      const int vc = col_of(s) + (lane % VPR) * 8;
+#pragma unroll
+      for (int p = 0; p < NP; ++p) {
+        const int64_t row = row_of(s) + p * RPP + lane / VPR;
+        if (row < a.m && vc < a.n) load_aux<KIND, 8>(a.e, row, vc, x[b][p]);
+      }
+    };
+    fetch(0, 0);
+    static_for<0, STRIPS>([&](auto sc) __attribute__((always_inline)) {
+      constexpr int s = decltype(sc)::value;
+      const int vc = col_of(s) + (lane % VPR) * 8;
+      if constexpr (s % TM == 0) load_bias<KIND, 8>(a.e, vc, a.n, bias);
+      if constexpr (s + 1 < STRIPS) fetch(s + 1, (s + 1) & 1);
+      put(sc);
+#pragma unroll
+      for (int p = 0; p < NP; ++p) {
+        const int r = p * RPP + lane / VPR;
+        const int64_t row = row_of(s) + r;
+        float f[8];
+        load_cols<8>(out + r * C::OLD + (lane % VPR) * 8, f);
+        if (row < a.m && vc < a.n) finish_cols<KIND, 8>(a.e, row, vc, f, bias, x[s & 1][p]);
+      }
+      __builtin_amdgcn_wave_barrier();
+    });
+  } else {
+    static_for<0, STRIPS>([&](auto sc) __attribute__((always_inline)) {
+      constexpr int s = decltype(sc)::value;
+      put(sc);
+      const int col = col_of(s) + lane % C::OW;
+      float bias[1];
+      load_bias<KIND, 1>(a.e, col, a.n, bias);
+#pragma unroll 4
+      for (int p = 0; p < 32 * C::OW / 64; ++p) {
+        const int r = p * (64 / C::OW) + lane / C::OW;
+        const int64_t row = row_of(s) + r;
+        float f[1] = {out[r * C::OLD + lane % C::OW]};
+        Aux<1> x;
+        if (row < a.m && col < a.n) {
+          load_aux<KIND, 1>(a.e, row, col, x);
+          finish_cols<KIND, 1>(a.e, row, col, f, bias, x);
         }
       }
       __builtin_amdgcn_wave_barrier();
     });
-  });
+  }
 }
 
 // the sums of the reduction ranges, added in order, then the epilogue
@@ -429,8 +519,10 @@ __global__ __launch_bounds__(256) void gemm_finish_kernel(GemmArgs a) {
 #pragma unroll
       for (int e = 0; e < NV; ++e) f[e] += b[e];
     }
+    Aux<NV> x;
+    load_aux<KIND, NV>(a.e, row, col, x);
     load_bias<KIND, NV>(a.e, col, a.n, b);
-    finish_cols<KIND, NV>(a.e, row, col, f, b);
+    finish_cols<KIND, NV>(a.e, row, col, f, b, x);
   }
 }
 
@@ -450,26 +542,87 @@ __global__ __launch_bounds__(256) void gemm_pack_kernel(const bf16_t* src, int64
   }
 }
 
-// bias gradient: blocks of 256 columns x a range of rows; thread t sums column t
-constexpr int kColsumRanges = 256;
+// Bias gradient: a block sums a range of rows of 512 columns, a wave every fourth row of it with 8
+// columns per lane and four rows' loads in flight; colsum_finish adds the blocks' sums.
+template <bool VEC>
 __global__ __launch_bounds__(256) void colsum_part_kernel(const bf16_t* src, int64_t lds, int64_t rows, int cols,
                                                           int64_t rows_per, float* part) {
-  const int c = blockIdx.x * 256 + threadIdx.x;
-  if (c >= cols) return;
+  __shared__ float s_sum[4][512];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = blockIdx.x * 512 + lane * 8;
   const int64_t r0 = blockIdx.y * rows_per, r1 = r0 + rows_per < rows ? r0 + rows_per : rows;
-  float s = 0.f;
-  for (int64_t r = r0; r < r1; ++r) s += bf2f(src[r * lds + c]);
-  part[(int64_t)blockIdx.y * cols + c] = s;
+  float s[8] = {};
+  auto add = [&](const uint4& v) __attribute__((always_inline)) {
+    float f[8];
+    unpack8(v, f);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) s[e] += f[e];
+  };
+  auto get = [&](int64_t r) __attribute__((always_inline)) -> uint4 {
+    const bf16_t* p = src + r * lds + c;
+    if constexpr (VEC) return *reinterpret_cast<const uint4*>(p);
+    uint32_t h[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) h[e] = c + e < cols ? p[e] : 0;
+    return make_uint4(h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16);
+  };
+  if (c < cols) {
+    int64_t r = r0 + wave;
+    for (; r + 12 < r1; r += 16) {
+      const uint4 v0 = get(r), v1 = get(r + 4), v2 = get(r + 8), v3 = get(r + 12);
+      add(v0);
+      add(v1);
+      add(v2);
+      add(v3);
+    }
+    for (; r < r1; r += 4) add(get(r));
+  }
+#pragma unroll
+  for (int e = 0; e < 8; ++e) s_sum[wave][lane * 8 + e] = s[e];
+  __syncthreads();
+  for (int i = threadIdx.x; i < 512; i += 256) {
+    const int col = blockIdx.x * 512 + i;
+    if (col < cols) part[(int64_t)blockIdx.y * cols + col] = (s_sum[0][i] + s_sum[1][i]) + (s_sum[2][i] + s_sum[3][i]);
+  }
 }
-__global__ __launch_bounds__(256) void colsum_finish_kernel(const float* part, int ranges, int cols, float* out,
-                                                            int accumulate) {
-  const int c = blockIdx.x * 256 + threadIdx.x;
-  if (c >= cols) return;
+
+// The sums of the columns of a [rows][ld] matrix of partials, in a fixed order: the first cols0 go to
+// out0, the others to out1 (each may be nullptr).  A block takes 64 columns, each of its 16 waves every
+// sixteenth row, eight loads in flight.
+__global__ __launch_bounds__(1024) void column_sum_kernel(const float* part, int rows, int64_t ld, int cols, int cols0,
+                                                          float* out0, float* out1, int accumulate) {
+  __shared__ float s_sum[16][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = blockIdx.x * 64 + lane;
   float s = 0.f;
-  for (int r = 0; r < ranges; ++r) s += part[(int64_t)r * cols + c];
-  out[c] = accumulate ? out[c] + s : s;
+  if (c < cols) {
+    int r = wave;
+    for (; r + 112 < rows; r += 128) {
+      float v[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = part[(int64_t)(r + 16 * e) * ld + c];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s += v[e];
+    }
+    for (; r < rows; r += 16) s += part[(int64_t)r * ld + c];
+  }
+  s_sum[wave][lane] = s;
+  __syncthreads();
+  if (wave == 0 && c < cols) {
+    s = s_sum[0][lane];
+#pragma unroll
+    for (int w = 1; w < 16; ++w) s += s_sum[w][lane];
+    float* out = c < cols0 ? out0 : out1;
+    if (out != nullptr) {
+      out += c < cols0 ? c : c - cols0;
+      *out = accumulate ? *out + s : s;
+    }
+  }
 }
-int64_t colsum_rows_per(int64_t rows) { return std::max<int64_t>(16, (rows + kColsumRanges - 1) / kColsumRanges); }
+
+// ranges of rows: enough blocks for the chip, at least 32 rows each
+int64_t colsum_rows_per(int64_t rows, int cols) {
+  const int64_t ranges = std::max<int64_t>(1, std::min<int64_t>(2048 / ((cols + 511) / 512), (rows + 31) / 32));
+  return (rows + ranges - 1) / ranges;
+}
 
 __global__ __launch_bounds__(256) void fill_zero_kernel(float* p, int64_t n) {
   for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < n; i += gridDim.x * 256ll) p[i] = 0.f;
@@ -477,9 +630,12 @@ __global__ __launch_bounds__(256) void fill_zero_kernel(float* p, int64_t n) {
 
 unsigned grid_for(int64_t threads) { return (unsigned)std::min<int64_t>(4096, std::max<int64_t>(1, (threads + 255) / 256)); }
 
-using T256 = Tile<256, 256, 32, 4, 2, 2>;
+using T256 = Tile<256, 256, 32, 4, 2, 4>;
+using T256N = Tile<256, 128, 32, 3, 2, 2>;
 using T128 = Tile<128, 128, 64, 2, 2, 2>;
 using T64 = Tile<64, 64, 64, 3, 2, 2>;
+
+enum { kTile256, kTile256N, kTile128, kTile64 };
 
 template <int KIND, typename C>
 hipError_t launch_tile(const GemmArgs& a, hipStream_t s) {
@@ -490,9 +646,10 @@ hipError_t launch_tile(const GemmArgs& a, hipStream_t s) {
 template <int KIND>
 hipError_t launch_kind(const GemmArgs& a, int tile, hipStream_t s) {
   trace_begin(KC_LINEAR);
-  hipError_t e = tile == 0   ? launch_tile<KIND, T256>(a, s)
-                 : tile == 1 ? launch_tile<KIND, T128>(a, s)
-                             : launch_tile<KIND, T64>(a, s);
+  hipError_t e = tile == kTile256    ? launch_tile<KIND, T256>(a, s)
+                 : tile == kTile256N ? launch_tile<KIND, T256N>(a, s)
+                 : tile == kTile128  ? launch_tile<KIND, T128>(a, s)
+                                     : launch_tile<KIND, T64>(a, s);
   trace_end(KC_LINEAR);
   if (e != hipSuccess || a.splits == 1) return e;
   trace_begin(KC_LINEAR_FINISH);
@@ -502,18 +659,22 @@ hipError_t launch_kind(const GemmArgs& a, int tile, hipStream_t s) {
   return hipGetLastError();
 }
 
-int tile_side(int tile) { return tile == 0 ? 256 : tile == 1 ? 128 : 64; }
+struct TileSize {
+  int m, n;
+};
+constexpr TileSize kTiles[] = {{T256::BM, T256::BN}, {T256N::BM, T256N::BN}, {T128::BM, T128::BN}, {T64::BM, T64::BN}};
 int64_t tile_count(int tile, int64_t m, int n) {
-  const int b = tile_side(tile);
-  return ((m + b - 1) / b) * ((n + b - 1) / b);
+  const TileSize t = kTiles[tile];
+  return ((m + t.m - 1) / t.m) * ((n + t.n - 1) / t.n);
 }
 
 }  // namespace
 
 GemmPlan gemm_pick(GemmKind, int64_t m, int n, int64_t k) {
-  GemmPlan p{2, 1, 0};
-  if (tile_count(0, m, n) >= 256) p.tile = 0;
-  else if (tile_count(1, m, n) >= 256) p.tile = 1;
+  GemmPlan p{kTile64, 1, 0};
+  if (tile_count(kTile256, m, n) >= 256) p.tile = kTile256;
+  else if (tile_count(kTile256N, m, n) >= 256) p.tile = kTile256N;
+  else if (tile_count(kTile128, m, n) >= 256) p.tile = kTile128;
   const int64_t tiles = tile_count(p.tile, m, n), steps = (k + 63) / 64;
   if (tiles < 256) p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({512 / tiles, steps / 8, 64}));
   p.k_per_split = (steps + p.splits - 1) / p.splits * 64;
@@ -526,9 +687,9 @@ size_t gemm_part_bytes(const GemmPlan& p, int64_t m, int n) {
 }
 
 hipError_t gemm_launch(GemmKind kind, GemmArgs a, const GemmPlan& p, hipStream_t s) {
-  const int b = tile_side(p.tile);
-  a.tiles_m = (int32_t)((a.m + b - 1) / b);
-  a.tiles_n = (a.n + b - 1) / b;
+  const TileSize t = kTiles[p.tile];
+  a.tiles_m = (int32_t)((a.m + t.m - 1) / t.m);
+  a.tiles_n = (a.n + t.n - 1) / t.n;
   a.splits = p.splits;
   a.k_per_split = p.k_per_split;
   a.ldp = (a.n + 7) / 8 * 8;
@@ -546,19 +707,29 @@ hipError_t gemm_pack_launch(const bf16_t* src, int64_t lds, int64_t rows, int32_
 }
 
 size_t colsum_part_bytes(int64_t rows, int32_t cols) {
-  const int64_t per = colsum_rows_per(rows);
+  const int64_t per = colsum_rows_per(rows, cols);
   return (size_t)((rows + per - 1) / per) * cols * sizeof(float);
 }
 
 hipError_t colsum_launch(const bf16_t* src, int64_t lds, int64_t rows, int32_t cols, float* part, float* out,
                          int accumulate, hipStream_t s) {
-  const int64_t per = colsum_rows_per(rows);
-  const unsigned ranges = (unsigned)((rows + per - 1) / per), cb = (unsigned)((cols + 255) / 256);
+  const int64_t per = colsum_rows_per(rows, cols);
+  const unsigned ranges = (unsigned)((rows + per - 1) / per);
+  const dim3 grid((unsigned)((cols + 511) / 512), ranges);
   trace_begin(KC_LINEAR_BIAS_GRAD);
-  NUMBAT_LAUNCH(colsum_part_kernel, dim3(cb, ranges), dim3(256), 0, s, src, lds, rows, cols, per, part);
-  NUMBAT_LAUNCH(colsum_finish_kernel, dim3(cb), dim3(256), 0, s, (const float*)part, (int)ranges, cols, out, accumulate);
+  if (cols % 8 == 0 && lds % 8 == 0)
+    NUMBAT_LAUNCH(colsum_part_kernel<true>, grid, dim3(256), 0, s, src, lds, rows, cols, per, part);
+  else NUMBAT_LAUNCH(colsum_part_kernel<false>, grid, dim3(256), 0, s, src, lds, rows, cols, per, part);
+  const hipError_t e = hipGetLastError();
+  if (e == hipSuccess) column_sum_launch(part, (int)ranges, cols, cols, cols, out, nullptr, accumulate, s);
   trace_end(KC_LINEAR_BIAS_GRAD);
-  return hipGetLastError();
+  return e != hipSuccess ? e : hipGetLastError();
+}
+
+void column_sum_launch(const float* part, int rows, int64_t ld, int cols, int cols0, float* out0, float* out1,
+                       int accumulate, hipStream_t s) {
+  NUMBAT_LAUNCH(column_sum_kernel, dim3((unsigned)((cols + 63) / 64)), dim3(1024), 0, s, part, rows, ld, cols, cols0,
+                out0, out1, accumulate);
 }
 
 hipError_t fill_zero_launch(float* p, int64_t n, hipStream_t s) {

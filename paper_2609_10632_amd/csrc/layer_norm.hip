@@ -301,18 +301,6 @@ __global__ __launch_bounds__(256) void ln_bwd_cols_kernel(LnArgs a, const TY* dy
   p[a.c + c] = db;
 }
 
-__global__ __launch_bounds__(256) void ln_bwd_finish_kernel(const float* part, int blocks, int c, float* dgamma,
-                                                            float* dbeta, int accumulate) {
-  const int i = blockIdx.x * 256 + threadIdx.x;  // [2][c]
-  if (i >= 2 * c) return;
-  float s = 0.f;
-  for (int b = 0; b < blocks; ++b) s += part[(int64_t)b * 2 * c + i];
-  float* out = i < c ? dgamma : dbeta;
-  if (out == nullptr) return;
-  out += i < c ? i : i - c;
-  *out = accumulate ? *out + s : s;
-}
-
 constexpr int kLongest = 16384;  // the longest row that is held in registers
 constexpr int kBwdBlocks = 512, kLongRanges = 64;
 
@@ -421,8 +409,7 @@ hipError_t ln_bwd_launch(const LnArgs& a, const void* dy, const void* x, const f
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || pt == nullptr) return e;
   trace_begin(KC_LN_BWD_FINISH);
-  NUMBAT_LAUNCH(ln_bwd_finish_kernel, dim3((unsigned)((2 * a.c + 255) / 256)), dim3(256), 0, s, (const float*)pt,
-                bwd_blocks(a), a.c, dgamma, dbeta, accumulate);
+  column_sum_launch(pt, bwd_blocks(a), 2 * (int64_t)a.c, 2 * a.c, a.c, dgamma, dbeta, accumulate, s);
   trace_end(KC_LN_BWD_FINISH);
   return hipGetLastError();
 }

@@ -63,6 +63,12 @@ size_t colsum_part_bytes(int64_t rows, int32_t cols);
 hipError_t colsum_launch(const bf16_t* src, int64_t lds, int64_t rows, int32_t cols, float* part, float* out,
                          int accumulate, hipStream_t s);
 
+// the column sums of rows x cols partials (row stride ld), in a fixed order: the first cols0 (+)= to
+// out0, the others to out1 (each may be nullptr); the caller opens the timing class and reads the
+// launch status
+void column_sum_launch(const float* part, int rows, int64_t ld, int cols, int cols0, float* out0, float* out1,
+                       int accumulate, hipStream_t s);
+
 hipError_t fill_zero_launch(float* p, int64_t n, hipStream_t s);
 
 // ---------------------------------------------------------------------------
