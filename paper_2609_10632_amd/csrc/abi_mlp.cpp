@@ -170,7 +170,7 @@ numbat_status check_ln(const numbat_layer_norm_problem* p, LnArgs* a) {
 }
 
 size_t ln_bwd_ws(const LnArgs& a) { return a.m > 0 ? ln_bwd_part_bytes(a) : 0; }
-constexpr size_t kAdamWs = kAdamBlocks * sizeof(double);
+constexpr size_t kAdamWs = kAdamNormBlocks * sizeof(double);
 
 }  // namespace
 

@@ -70,6 +70,43 @@ __device__ __forceinline__ void store_row(T* row, int c, int gl, const float (&f
     }
   }
 }
+// The same part of a row as it lies in memory, for loads that are issued long before their use.
+template <int G, int V, bool VEC, typename T>
+struct Row {
+  static constexpr int Q = sizeof(T) / 2;  // 16-byte vectors per 8 elements
+  uint4 q[VEC ? V * Q : 1];
+  float f[VEC ? 1 : V][8];
+  __device__ __forceinline__ void load(const T* row, int c, int gl) {
+    if constexpr (VEC) {
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        const int col = (v * G + gl) * 8;
+#pragma unroll
+        for (int i = 0; i < Q; ++i)
+          q[v * Q + i] = col < c ? reinterpret_cast<const uint4*>(row + col)[i] : make_uint4(0, 0, 0, 0);
+      }
+    } else {
+      load_row<G, V, false>(row, c, gl, 0.f, f);
+    }
+  }
+  __device__ __forceinline__ void values(float (&o)[V][8]) const {
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      if constexpr (!VEC) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) o[v][e] = f[v][e];
+      } else if constexpr (Q == 1) {
+        unpack8(q[v], o[v]);
+      } else {
+        const uint4 a = q[v * Q], b = q[v * Q + Q - 1];
+        const uint32_t u[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+        for (int e = 0; e < 8; ++e) o[v][e] = __uint_as_float(u[e]);
+      }
+    }
+  }
+};
+
 // whether the lane's element (v, e) is inside the row
 template <int G, bool VEC>
 __device__ __forceinline__ bool inside(int v, int e, int c, int gl) {
@@ -164,16 +201,30 @@ __global__ __launch_bounds__(ln_threads<G>()) void ln_bwd_kernel(LnArgs a, const
       if (gamma == nullptr) g[v][e] = 1.f;
       dg[v][e] = db[v][e] = 0.f;
     }
-  // every group of the block takes the same number of rounds (the sums of wide groups hold barriers)
+  // every group of the block takes the same number of rounds (the sums of wide groups hold barriers);
+  // a round's rows are loaded a round ahead where registers allow
+  constexpr bool AHEAD = G * V < 2048;
   const int64_t rounds = (a.m + RPB - 1) / RPB;
-  for (int64_t k = blockIdx.x; k < rounds; k += gridDim.x) {
+  struct Rows {
+    Row<G, V, VEC, TX> x, res;
+    Row<G, V, VEC, TY> dy;
+    float mu, rs;
+  };
+  auto fetch = [&](int64_t k, Rows& r) __attribute__((always_inline)) {
+    const int64_t row = k * RPB + grp, rr = row < a.m ? row : 0;
+    r.x.load(x + rr * a.ldx, a.c, gl);
+    r.dy.load(dy + rr * a.ldy, a.c, gl);
+    if (res != nullptr) r.res.load(res + rr * a.ldr, a.c, gl);
+    r.mu = mean[rr];
+    r.rs = rstd[rr];
+  };
+  auto work = [&](int64_t k, const Rows& r) __attribute__((always_inline)) {
     const int64_t row = k * RPB + grp;
     const bool live = row < a.m;
-    const int64_t rr = live ? row : 0;
     float f[V][8], h[V][8];
-    load_row<G, V, VEC>(x + rr * a.ldx, a.c, gl, 0.f, f);
-    load_row<G, V, VEC>(dy + rr * a.ldy, a.c, gl, 0.f, h);
-    const float mu = mean[rr], rs = rstd[rr];
+    r.x.values(f);
+    r.dy.values(h);
+    const float mu = r.mu, rs = r.rs;
     float s1 = 0.f, s2 = 0.f;
 #pragma unroll
     for (int v = 0; v < V; ++v)
@@ -192,7 +243,7 @@ __global__ __launch_bounds__(ln_threads<G>()) void ln_bwd_kernel(LnArgs a, const
     const float c1 = t.x * inv_c, c2 = t.y * inv_c;
     if (live && dx != nullptr) {
       float o[V][8];
-      if (res != nullptr) load_row<G, V, VEC>(res + row * a.ldr, a.c, gl, 0.f, o);
+      if (res != nullptr) r.res.values(o);
 #pragma unroll
       for (int v = 0; v < V; ++v)
 #pragma unroll
@@ -201,6 +252,21 @@ __global__ __launch_bounds__(ln_threads<G>()) void ln_bwd_kernel(LnArgs a, const
           f[v][e] = res != nullptr ? d + o[v][e] : d;
         }
       store_row<G, V, VEC>(dx + row * a.lddx, a.c, gl, f);
+    }
+  };
+  if constexpr (AHEAD) {
+    Rows now, next;
+    if (blockIdx.x < rounds) fetch(blockIdx.x, now);
+    for (int64_t k = blockIdx.x; k < rounds; k += gridDim.x) {
+      if (k + gridDim.x < rounds) fetch(k + gridDim.x, next);
+      work(k, now);
+      now = next;
+    }
+  } else {
+    for (int64_t k = blockIdx.x; k < rounds; k += gridDim.x) {
+      Rows now;
+      fetch(k, now);
+      work(k, now);
     }
   }
   if (part == nullptr) return;
@@ -302,7 +368,7 @@ __global__ __launch_bounds__(256) void ln_bwd_cols_kernel(LnArgs a, const TY* dy
 }
 
 constexpr int kLongest = 16384;  // the longest row that is held in registers
-constexpr int kBwdBlocks = 512, kLongRanges = 64;
+constexpr int kLongRanges = 64;
 
 int group_lanes(int c) {
   int g = 16;
@@ -312,7 +378,8 @@ int group_lanes(int c) {
 int bwd_blocks(const LnArgs& a) {
   if (a.c > kLongest) return (int)std::min<int64_t>(kLongRanges, a.m);
   const int g = group_lanes(a.c), rpb = (g > 256 ? g : 256) / g;
-  return (int)std::min<int64_t>(kBwdBlocks, (a.m + rpb - 1) / rpb);
+  // four blocks to a CU of short rows; a partial is as long as two rows, so long ones take fewer
+  return (int)std::min<int64_t>(g <= 128 ? 1024 : 512, (a.m + rpb - 1) / rpb);
 }
 
 // f.template operator()<G, V>() for the narrowest group that holds c elements

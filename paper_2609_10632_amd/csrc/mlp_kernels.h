@@ -103,8 +103,9 @@ struct AdamTensor {
   int32_t g_type;  // numbat_type
 };
 constexpr int kAdamBlock = 256;        // elements that share the units of 8-bit moments
-constexpr int kAdamMaxTensors = 1024;  // the table is staged in LDS
-constexpr int kAdamBlocks = 1024;      // most blocks of a launch, and partials of the norm
+constexpr int kAdamMaxTensors = 1024;  // a block's threads count four tensors each
+constexpr int kAdamBlocks = 1024;      // blocks of the update
+constexpr int kAdamNormBlocks = 2048;  // blocks of the norm's sum, and its partials
 struct AdamArgs {
   const AdamTensor* tab;
   int32_t count;
