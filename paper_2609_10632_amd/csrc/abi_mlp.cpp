@@ -79,8 +79,8 @@ size_t place(size_t* at, size_t bytes) {
   return here;
 }
 
-Product::Op operand(int64_t rows, int32_t cols, int64_t ld, size_t* at) {
-  Product::Op o{rows, cols, ld, cols % 8 != 0 || ld % 8 != 0, (int64_t)round_up((size_t)cols, 8), 0};
+Product::Op operand(int64_t rows, int32_t cols, int64_t ld, bool any, size_t* at) {
+  Product::Op o{rows, cols, ld, !any && (cols % 8 != 0 || ld % 8 != 0), (int64_t)round_up((size_t)cols, 8), 0};
   if (o.pack) o.at = place(at, (size_t)rows * o.ldp * sizeof(bf16_t));
   return o;
 }
@@ -90,24 +90,16 @@ Product product(const LinearDesc& d, GemmKind kind) {
   std::memset(&p, 0, sizeof p);
   p.kind = kind;
   size_t at = 0;
-  if (kind == kGemmFwd) {
-    p.m = d.m, p.n = d.n, p.k = d.k;
-    p.a = operand(d.m, d.k, d.ldx, &at);
-    p.b = operand(d.n, d.k, d.k, &at);
-  } else if (kind == kGemmDgrad) {
-    p.m = d.m, p.n = d.k, p.k = d.n;
-    p.a = operand(d.m, d.n, d.ldy, &at);
-    p.b = operand(d.n, d.k, d.k, &at);
-  } else {
-    p.m = d.n, p.n = d.k, p.k = d.m;
-    p.a = operand(d.m, d.n, d.ldy, &at);
-    p.b = operand(d.m, d.k, d.ldx, &at);
-  }
-  if (d.m > 0) {
-    p.plan = gemm_pick(kind, p.m, p.n, p.k);
-    p.part_at = place(&at, gemm_part_bytes(p.plan, p.m, p.n));
-    if (kind == kGemmWgrad) p.extra_at = place(&at, colsum_part_bytes(d.m, d.n));
-  }
+  if (d.m == 0) return p;
+  if (kind == kGemmFwd) p.m = d.m, p.n = d.n, p.k = d.k;
+  else if (kind == kGemmDgrad) p.m = d.m, p.n = d.k, p.k = d.n;
+  else p.m = d.n, p.n = d.k, p.k = d.m;
+  p.plan = gemm_pick(kind, p.m, p.n, p.k);
+  const bool any = gemm_any_rows(p.plan);
+  p.a = kind == kGemmFwd ? operand(d.m, d.k, d.ldx, any, &at) : operand(d.m, d.n, d.ldy, any, &at);
+  p.b = kind == kGemmWgrad ? operand(d.m, d.k, d.ldx, any, &at) : operand(d.n, d.k, d.k, any, &at);
+  p.part_at = place(&at, gemm_part_bytes(p.plan, p.m, p.n));
+  if (kind == kGemmWgrad) p.extra_at = place(&at, colsum_part_bytes(d.m, d.n));
   p.bytes = at;
   return p;
 }

@@ -31,7 +31,7 @@ struct GemmEpilogue {
 
 struct GemmArgs {
   const bf16_t *a, *b;
-  int64_t lda, ldb;     // elements between rows of the stored matrices, multiples of 8
+  int64_t lda, ldb;     // elements between rows of the stored matrices, multiples of 8 (or see gemm_any_rows)
   int64_t m, k;
   int32_t n;
   int32_t tiles_m, tiles_n;
@@ -49,9 +49,15 @@ struct GemmPlan {
   int64_t k_per_split;
 };
 GemmPlan gemm_pick(GemmKind kind, int64_t m, int n, int64_t k);
+// whether the plan's kernel takes operands whose rows start at any element
+bool gemm_any_rows(const GemmPlan& p);
 size_t gemm_part_bytes(const GemmPlan& p, int64_t m, int n);
 // a.part holds gemm_part_bytes; every dimension is at least 1
 hipError_t gemm_launch(GemmKind kind, GemmArgs a, const GemmPlan& p, hipStream_t s);
+
+// the forward of few rows (linear_rows.hip), m at most kLinearRows
+constexpr int kLinearRows = 64;
+hipError_t linear_rows_launch(const GemmArgs& a, hipStream_t s);
 
 // rows x cols of src (row stride lds) into dst with row stride ldd = cols rounded up to 8, the
 // padding zero
