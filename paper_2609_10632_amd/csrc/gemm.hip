@@ -489,11 +489,11 @@ __global__ __launch_bounds__(256) void fill_zero_kernel(float* p, int64_t n) {
 unsigned grid_for(int64_t threads) { return (unsigned)std::min<int64_t>(4096, std::max<int64_t>(1, (threads + 255) / 256)); }
 
 using T256 = Tile<256, 256, 32, 4, 2, 4>;
-using T256N = Tile<256, 128, 32, 3, 2, 2>;
-using T128 = Tile<128, 128, 64, 2, 2, 2>;
-using T64 = Tile<64, 64, 64, 3, 2, 2>;
+using T128D = Tile<128, 128, 64, 4, 2, 4>;
+using T128 = Tile<128, 128, 64, 2, 2, 4>;
+using T64 = Tile<64, 64, 64, 4, 2, 2>;
 
-enum { kTile256, kTile256N, kTile128, kTile64, kTileRows };
+enum { kTile256, kTile128D, kTile128, kTile64, kTileRows };
 
 template <int KIND, typename C>
 hipError_t launch_tile(const GemmArgs& a, hipStream_t s) {
@@ -505,7 +505,7 @@ template <int KIND>
 hipError_t launch_kind(const GemmArgs& a, int tile, hipStream_t s) {
   trace_begin(KC_LINEAR);
   hipError_t e = tile == kTile256    ? launch_tile<KIND, T256>(a, s)
-                 : tile == kTile256N ? launch_tile<KIND, T256N>(a, s)
+                 : tile == kTile128D ? launch_tile<KIND, T128D>(a, s)
                  : tile == kTile128  ? launch_tile<KIND, T128>(a, s)
                                      : launch_tile<KIND, T64>(a, s);
   trace_end(KC_LINEAR);
@@ -520,24 +520,47 @@ hipError_t launch_kind(const GemmArgs& a, int tile, hipStream_t s) {
 struct TileSize {
   int m, n;
 };
-constexpr TileSize kTiles[] = {{T256::BM, T256::BN}, {T256N::BM, T256N::BN}, {T128::BM, T128::BN}, {T64::BM, T64::BN}};
+constexpr TileSize kTiles[] = {{T256::BM, T256::BN}, {T128D::BM, T128D::BN}, {T128::BM, T128::BN}, {T64::BM, T64::BN}};
 int64_t tile_count(int tile, int64_t m, int n) {
   const TileSize t = kTiles[tile];
   return ((m + t.m - 1) / t.m) * ((n + t.n - 1) / t.n);
 }
+
+// What a product takes on a tile, in us, as measured: rounds of blocks over the 256 CUs, each a fixed
+// part (first loads, epilogue) and a part per k.
+double tile_time(int tile, int64_t blocks, int64_t k) {
+  switch (tile) {
+    case kTile256: return (double)((blocks + 255) / 256) * (7.0 + 0.0255 * k);
+    case kTile128D: return (double)((blocks + 255) / 256) * (2.5 + 0.0079 * k);
+    case kTile128: return blocks <= 256 ? 3.0 + 0.0115 * k : (double)((blocks + 511) / 512) * (4.0 + 0.015 * k);
+    default: return blocks <= 256 ? 2.5 + 0.0031 * k : (double)((blocks + 511) / 512) * (2.5 + 0.0058 * k);
+  }
+}
+
+// and the second launch that adds the sums of the splits
+double finish_time(int splits, int64_t m, int n) { return splits == 1 ? 0.0 : 4.0 + (double)splits * m * n * 8 / 4e6; }
 
 }  // namespace
 
 GemmPlan gemm_pick(GemmKind kind, int64_t m, int n, int64_t k) {
   GemmPlan p{kTile64, 1, 0};
   if (kind == kGemmFwd && m <= kLinearRows) return GemmPlan{kTileRows, 1, k};
-  if (tile_count(kTile256, m, n) >= 256) p.tile = kTile256;
-  else if (tile_count(kTile256N, m, n) >= 256) p.tile = kTile256N;
-  else if (tile_count(kTile128, m, n) >= 256) p.tile = kTile128;
-  const int64_t tiles = tile_count(p.tile, m, n), steps = (k + 63) / 64;
-  if (tiles < 256) p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({512 / tiles, steps / 8, 64}));
-  p.k_per_split = (steps + p.splits - 1) / p.splits * 64;
-  p.splits = (int)((k + p.k_per_split - 1) / p.k_per_split);
+  const int64_t steps = (k + 63) / 64;
+  double best = 1e30;
+  for (int tile = kTile256; tile <= kTile64; ++tile) {
+    const int64_t tiles = tile_count(tile, m, n);
+    for (int s : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
+      if (s > 1 && (steps / s < 4 || tiles * s > 1024)) break;
+      const int64_t kps = (steps + s - 1) / s;
+      const double t = tile_time(tile, tiles * s, kps * 64) + finish_time(s, m, n);
+      if (t < best) {
+        best = t;
+        p.tile = tile;
+        p.splits = (int)((steps + kps - 1) / kps);
+        p.k_per_split = kps * 64;
+      }
+    }
+  }
   return p;
 }
 

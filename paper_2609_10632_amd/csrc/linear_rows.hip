@@ -1,5 +1,5 @@
 // The forward of a linear layer for few rows (one token, a decode batch) on gfx950:
-//   y[m][n] = epilogue(sum_k x[m][k] w[n][k]),  m at most 64.
+//   y[m][n] = epilogue(sum_k x[m][k] w[n][k]),  m at most 16.
 // Bound by the bytes of w, which every launch reads once.  A block takes 16 rows of w and its waves
 // split the reduction, so that all 256 CUs stream w even for narrow layers and each wave has
 // 4 x 2 KiB of it in flight; the matrix core multiplies 16 rows of w by 16 rows of x per
@@ -35,45 +35,34 @@ __device__ __forceinline__ u32x4 load_k(const bf16_t* row, int k, int n) {
   return u32x4{h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16};
 }
 
-// MG groups of 16 rows of x, NW waves
-template <int MG, int NW, bool ALIGNED>
+template <int NW, bool ALIGNED>
 __global__ __launch_bounds__(NW * 64) void linear_rows_kernel(GemmArgs a) {
-  constexpr int U = MG == 4 ? 2 : 4;  // steps in flight
-  __shared__ float s_sum[NW][MG][16][17];
+  constexpr int U = 4;  // steps in flight
+  __shared__ float s_sum[NW][16][17];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l16 = lane & 15, kg = (lane >> 4) * 16;
   const int n0 = blockIdx.x * 16, K = (int)a.k, M = (int)a.m;
 
-  // this thread's outputs: column tid % 16 of rows tid / 16 + i NW * 4, and what the epilogue adds
-  constexpr int PER = MG * 256 / (NW * 64) > 0 ? MG * 256 / (NW * 64) : 1;
+  // this thread's output (the first 256 threads'), and what the epilogue adds to it
   const int oc = n0 + (tid & 15), orow = tid >> 4;
+  const bool mine = orow < M && oc < a.n;
   float bias[1];
-  Aux<1> aux[PER];
+  Aux<1> aux;
   load_bias<kGemmFwd, 1>(a.e, oc, a.n, bias);
-#pragma unroll
-  for (int i = 0; i < PER; ++i) {
-    const int r = orow + i * NW * 4;
-    if (r < M && oc < a.n) load_aux<kGemmFwd, 1>(a.e, r, oc, aux[i]);
-  }
+  if (mine) load_aux<kGemmFwd, 1>(a.e, orow, oc, aux);
 
   // (rows past the end read the last one: their sums are not stored)
   const bf16_t* wrow = a.b + (int64_t)(n0 + l16 < a.n ? n0 + l16 : a.n - 1) * a.ldb;
-  const bf16_t* xrow[MG];
-#pragma unroll
-  for (int g = 0; g < MG; ++g) xrow[g] = a.a + (int64_t)(g * 16 + l16 < M ? g * 16 + l16 : M - 1) * a.lda;
+  const bf16_t* xrow = a.a + (int64_t)(l16 < M ? l16 : M - 1) * a.lda;
   const int per = ((K + kStep - 1) / kStep + NW - 1) / NW * kStep;
   const int kbeg = wave * per, kend = kbeg + per < K ? kbeg + per : K;
-  f32x4 acc[MG];
-#pragma unroll
-  for (int g = 0; g < MG; ++g) acc[g] = f32x4{0.f, 0.f, 0.f, 0.f};
-  u32x4 wf[U][2], xf[U][MG][2];
+  f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
+  u32x4 wf[U][2], xf[U][2];
   auto mma = [&]() __attribute__((always_inline)) {
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int g = 0; g < MG; ++g) acc[g] = mfma16x16x32(wf[u][h], xf[u][g][h], acc[g]);
+      for (int h = 0; h < 2; ++h) acc = mfma16x16x32(wf[u][h], xf[u][h], acc);
   };
   auto fetch = [&](auto whole, int k) __attribute__((always_inline)) {
     constexpr bool W = decltype(whole)::value;
@@ -83,8 +72,7 @@ __global__ __launch_bounds__(NW * 64) void linear_rows_kernel(GemmArgs a) {
       for (int h = 0; h < 2; ++h) {
         const int at = k + u * kStep + kg + 8 * h;
         wf[u][h] = load_k<ALIGNED, W>(wrow, at, kend);
-#pragma unroll
-        for (int g = 0; g < MG; ++g) xf[u][g][h] = load_k<ALIGNED, W>(xrow[g], at, kend);
+        xf[u][h] = load_k<ALIGNED, W>(xrow, at, kend);
       }
   };
   int k = kbeg;
@@ -96,46 +84,32 @@ __global__ __launch_bounds__(NW * 64) void linear_rows_kernel(GemmArgs a) {
     fetch(std::false_type{}, k);
     mma();
   }
-  // lane holds columns 4 (lane / 16) .. + 3 of row lane % 16 of each group
+  // lane holds columns 4 (lane / 16) .. + 3 of row lane % 16
 #pragma unroll
-  for (int g = 0; g < MG; ++g)
-#pragma unroll
-    for (int r = 0; r < 4; ++r) s_sum[wave][g][l16][4 * (lane >> 4) + r] = acc[g][r];
+  for (int r = 0; r < 4; ++r) s_sum[wave][l16][4 * (lane >> 4) + r] = acc[r];
   __syncthreads();
+  if (!mine) return;
+  float f[1] = {s_sum[0][orow][tid & 15]};
 #pragma unroll
-  for (int i = 0; i < PER; ++i) {
-    const int r = orow + i * NW * 4;
-    if (r >= M || oc >= a.n || r >= MG * 16) continue;
-    float f[1] = {s_sum[0][r >> 4][r & 15][tid & 15]};
-#pragma unroll
-    for (int w = 1; w < NW; ++w) f[0] += s_sum[w][r >> 4][r & 15][tid & 15];
-    finish_cols<kGemmFwd, 1>(a.e, r, oc, f, bias, aux[i]);
-  }
+  for (int w = 1; w < NW; ++w) f[0] += s_sum[w][orow][tid & 15];
+  finish_cols<kGemmFwd, 1>(a.e, orow, oc, f, bias, aux);
 }
 
-template <int MG, int NW>
-void launch_rows(const GemmArgs& a, bool aligned, hipStream_t s) {
+template <int NW>
+void launch_rows(const GemmArgs& a, hipStream_t s) {
   const dim3 grid((unsigned)((a.n + 15) / 16)), block(NW * 64);
-  if (aligned) NUMBAT_LAUNCH((linear_rows_kernel<MG, NW, true>), grid, block, 0, s, a);
-  else NUMBAT_LAUNCH((linear_rows_kernel<MG, NW, false>), grid, block, 0, s, a);
-}
-
-template <int MG>
-void launch_groups(const GemmArgs& a, bool aligned, hipStream_t s) {
-  // a wave of at least 256 k: with less its sums cost more than its loads hide
-  if (a.k >= 4096) launch_rows<MG, 16>(a, aligned, s);
-  else if (a.k >= 1024) launch_rows<MG, 8>(a, aligned, s);
-  else launch_rows<MG, 4>(a, aligned, s);
+  if (a.lda % 8 == 0 && a.ldb % 8 == 0) NUMBAT_LAUNCH((linear_rows_kernel<NW, true>), grid, block, 0, s, a);
+  else NUMBAT_LAUNCH((linear_rows_kernel<NW, false>), grid, block, 0, s, a);
 }
 
 }  // namespace
 
 hipError_t linear_rows_launch(const GemmArgs& a, hipStream_t s) {
-  const bool aligned = a.lda % 8 == 0 && a.ldb % 8 == 0;
   trace_begin(KC_LINEAR);
-  if (a.m <= 16) launch_groups<1>(a, aligned, s);
-  else if (a.m <= 32) launch_groups<2>(a, aligned, s);
-  else launch_groups<4>(a, aligned, s);
+  // a wave of at least 256 k: with less its sums cost more than its loads hide
+  if (a.k >= 4096) launch_rows<16>(a, s);
+  else if (a.k >= 1024) launch_rows<8>(a, s);
+  else launch_rows<4>(a, s);
   trace_end(KC_LINEAR);
   return hipGetLastError();
 }

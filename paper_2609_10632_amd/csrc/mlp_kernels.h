@@ -56,7 +56,7 @@ size_t gemm_part_bytes(const GemmPlan& p, int64_t m, int n);
 hipError_t gemm_launch(GemmKind kind, GemmArgs a, const GemmPlan& p, hipStream_t s);
 
 // the forward of few rows (linear_rows.hip), m at most kLinearRows
-constexpr int kLinearRows = 64;
+constexpr int kLinearRows = 16;
 hipError_t linear_rows_launch(const GemmArgs& a, hipStream_t s);
 
 // rows x cols of src (row stride lds) into dst with row stride ldd = cols rounded up to 8, the
