@@ -94,7 +94,10 @@ Product product(const LinearDesc& d, GemmKind kind) {
   if (kind == kGemmFwd) p.m = d.m, p.n = d.n, p.k = d.k;
   else if (kind == kGemmDgrad) p.m = d.m, p.n = d.k, p.k = d.n;
   else p.m = d.n, p.n = d.k, p.k = d.m;
-  p.plan = gemm_pick(kind, p.m, p.n, p.k);
+  // (the workspace depends on the problem alone, so that z is kept and read where there is an
+  // activation is taken for granted here)
+  const int z = d.act != NUMBAT_ACT_NONE ? 2 : 0;
+  p.plan = gemm_pick(kind, p.m, p.n, p.k, kind == kGemmFwd ? (d.y_f32 ? 4 : 2) + z : kind == kGemmDgrad ? 2 + z : 4);
   const bool any = gemm_any_rows(p.plan);
   p.a = kind == kGemmFwd ? operand(d.m, d.k, d.ldx, any, &at) : operand(d.m, d.n, d.ldy, any, &at);
   p.b = kind == kGemmWgrad ? operand(d.m, d.k, d.ldx, any, &at) : operand(d.n, d.k, d.k, any, &at);
@@ -104,16 +107,13 @@ Product product(const LinearDesc& d, GemmKind kind) {
   return p;
 }
 
-hipError_t packed(const Product::Op& o, const void* src, char* ws, hipStream_t s, const bf16_t** out, int64_t* ld) {
-  if (!o.pack) {
-    *out = static_cast<const bf16_t*>(src);
-    *ld = o.ld;
-    return hipSuccess;
-  }
-  bf16_t* dst = reinterpret_cast<bf16_t*>(ws + o.at);
-  *out = dst;
-  *ld = o.ldp;
-  return gemm_pack_launch(static_cast<const bf16_t*>(src), o.ld, o.rows, o.cols, dst, o.ldp, s);
+// the operand as the product reads it: where it lies, or its padded copy to be made
+GemmPack packed(const Product::Op& o, const void* src, char* ws, const bf16_t** out, int64_t* ld) {
+  const bf16_t* s = static_cast<const bf16_t*>(src);
+  bf16_t* dst = o.pack ? reinterpret_cast<bf16_t*>(ws + o.at) : nullptr;
+  *out = o.pack ? dst : s;
+  *ld = o.pack ? o.ldp : o.ld;
+  return GemmPack{s, o.ld, o.pack ? o.rows : 0, o.cols, dst, o.ldp};
 }
 
 hipError_t run_product(const Product& p, const void* a, const void* b, const GemmEpilogue& e, void* ws,
@@ -121,9 +121,11 @@ hipError_t run_product(const Product& p, const void* a, const void* b, const Gem
   GemmArgs g;
   std::memset(&g, 0, sizeof g);
   char* body = static_cast<char*>(ws);
-  hipError_t err = packed(p.a, a, body, s, &g.a, &g.lda);
-  if (err == hipSuccess) err = packed(p.b, b, body, s, &g.b, &g.ldb);
-  if (err != hipSuccess) return err;
+  const GemmPack pa = packed(p.a, a, body, &g.a, &g.lda), pb = packed(p.b, b, body, &g.b, &g.ldb);
+  if (pa.rows > 0 || pb.rows > 0) {
+    const hipError_t err = gemm_pack_launch(pa, pb, s);
+    if (err != hipSuccess) return err;
+  }
   g.m = p.m;
   g.n = p.n;
   g.k = p.k;
@@ -223,8 +225,7 @@ numbat_status numbat_linear_fwd(const numbat_linear_problem* p, const void* x, c
   e.ldr = d.ldr;
   e.ldz = d.ldz;
   e.ldo = d.ldy;
-  e.vec = d.n % 8 == 0 && d.ldy % 8 == 0 && (residual == nullptr || d.ldr % 8 == 0) && (z == nullptr || d.ldz % 8 == 0) &&
-          aligned16(bias);
+  e.vec = d.n % 8 == 0 && d.ldy % 8 == 0 && (residual == nullptr || d.ldr % 8 == 0) && (z == nullptr || d.ldz % 8 == 0);
   const hipError_t err = run_product(pr, x, w, e, ws_body(ws), static_cast<hipStream_t>(stream));
   return err == hipSuccess ? ok() : hip_fail(err, "linear forward launch");
 }

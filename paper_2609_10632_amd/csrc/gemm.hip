@@ -17,6 +17,7 @@
 // matrix cores' rate; what bounds long reductions is the matrix cores, short ones (maps of
 // few channels) the bytes of x, z and y.
 #include <algorithm>
+#include <cmath>
 
 #include "gemm_epilogue.h"
 
@@ -181,6 +182,27 @@ __global__ __launch_bounds__(C::NW * 64) void gemm_kernel(GemmArgs a) {
   int64_t left = (a.k - k0 < a.k_per_split ? a.k - k0 : a.k_per_split);  // k not yet loaded
   const int nk = (int)((left + BK - 1) / BK);
 
+  const int wm = wave / C::WN, wn = wave % C::WN;
+  // The epilogue goes by strips of 32 rows x OW columns of the wave's sums.  What it reads beside them
+  // for the first strips is loaded before anything else, so that it is there when the sums are (and
+  // these loads, the oldest, disturb no count of those in flight).
+  constexpr int JS = C::OW / 32, STRIPS = TN / JS * TM;
+  constexpr int VPR = C::OW / 8, RPP = 64 / VPR, NP = 32 / RPP;  // vectors per row, rows per pass, passes
+  constexpr int XB = STRIPS <= 2 ? STRIPS : 2, AHEAD = XB == STRIPS ? STRIPS : 1;
+  auto row_of = [&](int s) __attribute__((always_inline)) { return m0 + (wm * TM + s % TM) * 32; };
+  auto col_of = [&](int s) __attribute__((always_inline)) { return n0 + (wn * TN + s / TM * JS) * 32; };
+  Aux<8> x[XB][NP];
+  auto fetch = [&](auto sc) __attribute__((always_inline)) {
+    constexpr int s = decltype(sc)::value;
+    const int vc = col_of(s) + (lane % VPR) * 8;
+#pragma unroll
+    for (int p = 0; p < NP; ++p) {
+      const int64_t row = row_of(s) + p * RPP + lane / VPR;
+      if (row < a.m && vc < a.n) load_aux<KIND, 8>(a.e, row, vc, x[s % XB][p]);
+    }
+  };
+  if (a.splits == 1 && a.e.vec) static_for<0, AHEAD>(fetch);
+
   Operand<TA, BM, BK, NW, C::AI> oa;
   Operand<TB, BN, BK, NW, C::BI> ob;
   oa.init(a.a, a.lda, m0, a.m, k0, wave, lane);
@@ -198,7 +220,6 @@ __global__ __launch_bounds__(C::NW * 64) void gemm_kernel(GemmArgs a) {
     left -= BK;
   };
 
-  const int wm = wave / C::WN, wn = wave % C::WN;
   Frags<TA, BM, BK, TM> fa;
   Frags<TB, BN, BK, TN> fb;
   fa.init(wm * TM * 32, lane);
@@ -274,8 +295,6 @@ __global__ __launch_bounds__(C::NW * 64) void gemm_kernel(GemmArgs a) {
   unsigned char* mine = ws == 0 ? st0 : ws == 1 ? st1 : ws == 2 ? st2 : st3;
   float* out = reinterpret_cast<float*>(mine + (wave % C::WPS) * C::OUT_BYTES);
   const int l32 = lane & 31, half = lane >> 5;
-  constexpr int JS = C::OW / 32, STRIPS = TN / JS * TM;
-  constexpr int VPR = C::OW / 8, RPP = 64 / VPR, NP = 32 / RPP;  // vectors per row, rows per pass, passes
   // accumulators of strip s (rows first, then columns) into the wave's LDS
   auto put = [&](auto sc) __attribute__((always_inline)) {
     constexpr int i = decltype(sc)::value % TM, js = decltype(sc)::value / TM * JS;
@@ -289,9 +308,6 @@ __global__ __launch_bounds__(C::NW * 64) void gemm_kernel(GemmArgs a) {
       }
     __builtin_amdgcn_wave_barrier();
   };
-  // the strip's first row and column
-  auto row_of = [&](int s) __attribute__((always_inline)) { return m0 + (wm * TM + s % TM) * 32; };
-  auto col_of = [&](int s) __attribute__((always_inline)) { return n0 + (wn * TN + s / TM * JS) * 32; };
   if (a.splits > 1) {
     static_for<0, STRIPS>([&](auto sc) __attribute__((always_inline)) {
       constexpr int s = decltype(sc)::value;
@@ -310,22 +326,12 @@ __global__ __launch_bounds__(C::NW * 64) void gemm_kernel(GemmArgs a) {
     });
   } else if (a.e.vec) {
     // the next strip's auxiliary loads are in flight while a strip is finished
-    Aux<8> x[2][NP];
     float bias[8];
-    auto fetch = [&](int s, int b) __attribute__((always_inline)) {
-      const int vc = col_of(s) + (lane % VPR) * 8;
-#pragma unroll
-      for (int p = 0; p < NP; ++p) {
-        const int64_t row = row_of(s) + p * RPP + lane / VPR;
-        if (row < a.m && vc < a.n) load_aux<KIND, 8>(a.e, row, vc, x[b][p]);
-      }
-    };
-    fetch(0, 0);
     static_for<0, STRIPS>([&](auto sc) __attribute__((always_inline)) {
       constexpr int s = decltype(sc)::value;
       const int vc = col_of(s) + (lane % VPR) * 8;
       if constexpr (s % TM == 0) load_bias<KIND, 8>(a.e, vc, a.n, bias);
-      if constexpr (s + 1 < STRIPS) fetch(s + 1, (s + 1) & 1);
+      if constexpr (s + AHEAD < STRIPS) fetch(Ic<s + AHEAD>{});
       put(sc);
 #pragma unroll
       for (int p = 0; p < NP; ++p) {
@@ -333,27 +339,24 @@ __global__ __launch_bounds__(C::NW * 64) void gemm_kernel(GemmArgs a) {
         const int64_t row = row_of(s) + r;
         float f[8];
         load_cols<8>(out + r * C::OLD + (lane % VPR) * 8, f);
-        if (row < a.m && vc < a.n) finish_cols<KIND, 8>(a.e, row, vc, f, bias, x[s & 1][p]);
+        if (row < a.m && vc < a.n) finish_cols<KIND, 8>(a.e, row, vc, f, bias, x[s % XB][p]);
       }
       __builtin_amdgcn_wave_barrier();
     });
   } else {
+    float bias[8];
     static_for<0, STRIPS>([&](auto sc) __attribute__((always_inline)) {
       constexpr int s = decltype(sc)::value;
+      const int vc = col_of(s) + (lane % VPR) * 8;
+      if constexpr (s % TM == 0) load_bias<KIND, 8>(a.e, vc, a.n, bias);
       put(sc);
-      const int col = col_of(s) + lane % C::OW;
-      float bias[1];
-      load_bias<KIND, 1>(a.e, col, a.n, bias);
-#pragma unroll 4
-      for (int p = 0; p < 32 * C::OW / 64; ++p) {
-        const int r = p * (64 / C::OW) + lane / C::OW;
+#pragma unroll 1
+      for (int p = 0; p < NP; ++p) {
+        const int r = p * RPP + lane / VPR;
         const int64_t row = row_of(s) + r;
-        float f[1] = {out[r * C::OLD + lane % C::OW]};
-        Aux<1> x;
-        if (row < a.m && col < a.n) {
-          load_aux<KIND, 1>(a.e, row, col, x);
-          finish_cols<KIND, 1>(a.e, row, col, f, bias, x);
-        }
+        float f[8];
+        load_cols<8>(out + r * C::OLD + (lane % VPR) * 8, f);
+        if (row < a.m) finish_any<KIND>(a.e, row, vc, a.n, f, bias);
       }
       __builtin_amdgcn_wave_barrier();
     });
@@ -384,19 +387,27 @@ __global__ __launch_bounds__(256) void gemm_finish_kernel(GemmArgs a) {
   }
 }
 
-__global__ __launch_bounds__(256) void gemm_pack_kernel(const bf16_t* src, int64_t lds, int64_t rows, int cols,
-                                                        bf16_t* dst, int64_t ldd) {
-  const int per_row = (int)(ldd / 8);
-  const int64_t total = rows * per_row;
+// Operands whose rows are not whole aligned vectors, copied with rows padded by zeros; both of a
+// product in one launch, a thread a vector.
+__global__ __launch_bounds__(256) void gemm_pack_kernel(GemmPack a, GemmPack b) {
+  const int64_t na = a.rows * (a.ldd / 8), total = na + b.rows * (b.ldd / 8);
   for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < total; i += gridDim.x * 256ll) {
-    const int64_t row = i / per_row;
-    const int c = (int)(i - row * per_row) * 8;
-    const bf16_t* s = src + row * lds + c;
-    uint32_t h[8];
+    const GemmPack& o = i < na ? a : b;
+    const int64_t j = i < na ? i : i - na;
+    const int per_row = (int)(o.ldd / 8);
+    const int64_t row = j / per_row;
+    const int c = (int)(j - row * per_row) * 8;
+    const bf16_t* s = o.src + row * o.lds + c;
+    uint4 v;
+    if (c + 8 <= o.cols) {
+      v = load16<false>(s);
+    } else {
+      uint32_t h[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) h[e] = c + e < cols ? s[e] : 0;
-    *reinterpret_cast<uint4*>(dst + row * ldd + c) =
-        make_uint4(h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16);
+      for (int e = 0; e < 8; ++e) h[e] = c + e < o.cols ? s[e] : 0;
+      v = make_uint4(h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16);
+    }
+    *reinterpret_cast<uint4*>(o.dst + row * o.ldd + c) = v;
   }
 }
 
@@ -527,13 +538,16 @@ int64_t tile_count(int tile, int64_t m, int n) {
 }
 
 // What a product takes on a tile, in us, as measured: rounds of blocks over the 256 CUs, each a fixed
-// part (first loads, epilogue) and a part per k.
-double tile_time(int tile, int64_t blocks, int64_t k) {
+// part (first loads, epilogue: out_bytes for each element of C) and a part per k.
+double tile_time(int tile, int64_t blocks, int64_t k, int out_bytes) {
+  const double b = (double)blocks;
   switch (tile) {
-    case kTile256: return (double)((blocks + 255) / 256) * (7.0 + 0.0255 * k);
-    case kTile128D: return (double)((blocks + 255) / 256) * (2.5 + 0.0079 * k);
-    case kTile128: return blocks <= 256 ? 3.0 + 0.0115 * k : (double)((blocks + 511) / 512) * (4.0 + 0.015 * k);
-    default: return blocks <= 256 ? 2.5 + 0.0031 * k : (double)((blocks + 511) / 512) * (2.5 + 0.0058 * k);
+    case kTile256: return std::ceil(b / 256) * (1.5 + 2.75 * out_bytes + 0.0255 * k);
+    case kTile128D: return std::ceil(b / 256) * (1.2 + 0.65 * out_bytes + 0.0079 * k);
+    case kTile128:
+      return blocks <= 256 ? 3.0 + 0.0115 * k : std::max(1.0, b / 512 + 0.25) * (2.5 + 0.75 * out_bytes + 0.015 * k);
+    default:
+      return blocks <= 256 ? 2.5 + 0.0031 * k : std::max(1.0, b / 512 + 0.25) * (1.7 + 0.4 * out_bytes + 0.0058 * k);
   }
 }
 
@@ -542,7 +556,7 @@ double finish_time(int splits, int64_t m, int n) { return splits == 1 ? 0.0 : 4.
 
 }  // namespace
 
-GemmPlan gemm_pick(GemmKind kind, int64_t m, int n, int64_t k) {
+GemmPlan gemm_pick(GemmKind kind, int64_t m, int n, int64_t k, int out_bytes) {
   GemmPlan p{kTile64, 1, 0};
   if (kind == kGemmFwd && m <= kLinearRows) return GemmPlan{kTileRows, 1, k};
   const int64_t steps = (k + 63) / 64;
@@ -552,7 +566,7 @@ GemmPlan gemm_pick(GemmKind kind, int64_t m, int n, int64_t k) {
     for (int s : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
       if (s > 1 && (steps / s < 4 || tiles * s > 1024)) break;
       const int64_t kps = (steps + s - 1) / s;
-      const double t = tile_time(tile, tiles * s, kps * 64) + finish_time(s, m, n);
+      const double t = tile_time(tile, tiles * s, kps * 64, s > 1 ? 4 : out_bytes) + finish_time(s, m, n);
       if (t < best) {
         best = t;
         p.tile = tile;
@@ -583,10 +597,9 @@ hipError_t gemm_launch(GemmKind kind, GemmArgs a, const GemmPlan& p, hipStream_t
                               : launch_kind<kGemmWgrad>(a, p.tile, s);
 }
 
-hipError_t gemm_pack_launch(const bf16_t* src, int64_t lds, int64_t rows, int32_t cols, bf16_t* dst, int64_t ldd,
-                            hipStream_t s) {
+hipError_t gemm_pack_launch(const GemmPack& a, const GemmPack& b, hipStream_t s) {
   trace_begin(KC_LINEAR_PACK);
-  NUMBAT_LAUNCH(gemm_pack_kernel, dim3(grid_for(rows * (ldd / 8))), dim3(256), 0, s, src, lds, rows, cols, dst, ldd);
+  NUMBAT_LAUNCH(gemm_pack_kernel, dim3(grid_for(a.rows * (a.ldd / 8) + b.rows * (b.ldd / 8))), dim3(256), 0, s, a, b);
   trace_end(KC_LINEAR_PACK);
   return hipGetLastError();
 }

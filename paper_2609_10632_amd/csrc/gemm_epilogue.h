@@ -9,35 +9,54 @@ namespace numbat {
 namespace {
 
 // The epilogue on NV consecutive columns of one row (NV = 8: 16-byte accesses, or 1).
-template <int NV>
+// A vector of columns whose row starts at any element: unaligned 16-byte accesses, which the hardware
+// splits where they cross a line.
+struct __attribute__((packed, aligned(2))) AnyVec {
+  uint32_t u[4];
+};
+template <bool ALIGNED>
+__device__ __forceinline__ uint4 load16(const void* p) {
+  if constexpr (ALIGNED) return *static_cast<const uint4*>(p);
+  const AnyVec v = *static_cast<const AnyVec*>(p);
+  return make_uint4(v.u[0], v.u[1], v.u[2], v.u[3]);
+}
+template <bool ALIGNED>
+__device__ __forceinline__ void store16(void* p, u32x4 v) {
+  if constexpr (ALIGNED) __builtin_nontemporal_store(v, static_cast<u32x4*>(p));
+  else *static_cast<AnyVec*>(p) = AnyVec{{v.x, v.y, v.z, v.w}};
+}
+
+template <int NV, bool ALIGNED = true>
 __device__ __forceinline__ void load_cols(const bf16_t* p, float (&f)[NV]) {
-  if constexpr (NV == 8) unpack8(*reinterpret_cast<const uint4*>(p), f);
+  if constexpr (NV == 8) unpack8(load16<ALIGNED>(p), f);
   else f[0] = bf2f(*p);
 }
-template <int NV>
+template <int NV, bool ALIGNED = true>
 __device__ __forceinline__ void load_cols(const float* p, float (&f)[NV]) {
   if constexpr (NV == 8) {
-    const float4 lo = reinterpret_cast<const float4*>(p)[0], hi = reinterpret_cast<const float4*>(p)[1];
-    f[0] = lo.x; f[1] = lo.y; f[2] = lo.z; f[3] = lo.w;
-    f[4] = hi.x; f[5] = hi.y; f[6] = hi.z; f[7] = hi.w;
+    const uint4 lo = load16<ALIGNED>(p), hi = load16<ALIGNED>(p + 4);
+    const uint32_t u[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = __uint_as_float(u[i]);
   } else {
     f[0] = *p;
   }
 }
-template <int NV>
+template <int NV, bool ALIGNED = true>
 __device__ __forceinline__ void store_cols(bf16_t* p, const float (&f)[NV]) {
   if constexpr (NV == 8) {
     const uint4 v = pack8(f);
-    __builtin_nontemporal_store(u32x4{v.x, v.y, v.z, v.w}, reinterpret_cast<u32x4*>(p));
+    store16<ALIGNED>(p, u32x4{v.x, v.y, v.z, v.w});
   } else {
     *p = (bf16_t)f2bf(f[0]);
   }
 }
-template <int NV>
+template <int NV, bool ALIGNED = true>
 __device__ __forceinline__ void store_cols(float* p, const float (&f)[NV]) {
   if constexpr (NV == 8) {
-    __builtin_nontemporal_store(f32x4{f[0], f[1], f[2], f[3]}, reinterpret_cast<f32x4*>(p));
-    __builtin_nontemporal_store(f32x4{f[4], f[5], f[6], f[7]}, reinterpret_cast<f32x4*>(p) + 1);
+    const f32x4 lo = {f[0], f[1], f[2], f[3]}, hi = {f[4], f[5], f[6], f[7]};
+    store16<ALIGNED>(p, __builtin_bit_cast(u32x4, lo));
+    store16<ALIGNED>(p + 4, __builtin_bit_cast(u32x4, hi));
   } else {
     *p = f[0];
   }
@@ -58,7 +77,7 @@ __device__ __forceinline__ const void* aux_base(const GemmEpilogue& e, int64_t* 
          : KIND == kGemmDgrad ? (e.act != kActNone ? e.z : nullptr)
                               : (e.accumulate ? e.out : nullptr);
 }
-template <int KIND, int NV>
+template <int KIND, int NV, bool ALIGNED = true>
 __device__ __forceinline__ void load_aux(const GemmEpilogue& e, int64_t row, int col, Aux<NV>& x) {
   int64_t ld;
   bool f32;
@@ -66,8 +85,8 @@ __device__ __forceinline__ void load_aux(const GemmEpilogue& e, int64_t row, int
   if (base == nullptr) return;
   const char* p = static_cast<const char*>(base) + (row * ld + col) * (f32 ? 4 : 2);
   if constexpr (NV == 8) {
-    x.lo = *reinterpret_cast<const uint4*>(p);
-    if (f32) x.hi = *reinterpret_cast<const uint4*>(p + 16);
+    x.lo = load16<ALIGNED>(p);
+    if (f32) x.hi = load16<ALIGNED>(p + 16);
   } else {
     x.lo.x = f32 ? *reinterpret_cast<const uint32_t*>(p) : *reinterpret_cast<const uint16_t*>(p);
   }
@@ -94,13 +113,13 @@ __device__ __forceinline__ void each(float (&f)[NV], F&& fn) {
 }
 
 // f: the sums; bias: those of the columns; x: loaded by load_aux
-template <int KIND, int NV>
+template <int KIND, int NV, bool ALIGNED = true>
 __device__ __forceinline__ void finish_cols(const GemmEpilogue& e, int64_t row, int col, float (&f)[NV],
                                             const float (&bias)[NV], const Aux<NV>& x) {
   float o[NV];
   if constexpr (KIND == kGemmFwd) {
     each(f, [&](int i) { return f[i] + bias[i]; });
-    if (e.z != nullptr) store_cols<NV>(e.z + row * e.ldz + col, f);
+    if (e.z != nullptr) store_cols<NV, ALIGNED>(e.z + row * e.ldz + col, f);
     // (one branch for the vector, not one per element)
     switch (e.act) {
       case kActRelu: each(f, [&](int i) { return act_apply(f[i], kActRelu); }); break;
@@ -113,8 +132,8 @@ __device__ __forceinline__ void finish_cols(const GemmEpilogue& e, int64_t row, 
       aux_values<NV>(x, e.out_f32, o);
       each(f, [&](int i) { return f[i] + o[i]; });
     }
-    if (e.out_f32) store_cols<NV>(static_cast<float*>(e.out) + row * e.ldo + col, f);
-    else store_cols<NV>(static_cast<bf16_t*>(e.out) + row * e.ldo + col, f);
+    if (e.out_f32) store_cols<NV, ALIGNED>(static_cast<float*>(e.out) + row * e.ldo + col, f);
+    else store_cols<NV, ALIGNED>(static_cast<bf16_t*>(e.out) + row * e.ldo + col, f);
   } else if constexpr (KIND == kGemmDgrad) {
     if (e.act != kActNone) aux_values<NV>(x, false, o);
     switch (e.act) {
@@ -126,25 +145,61 @@ __device__ __forceinline__ void finish_cols(const GemmEpilogue& e, int64_t row, 
     }
     bf16_t* p = static_cast<bf16_t*>(e.out) + row * e.ldo + col;
     if (e.accumulate) {
-      load_cols<NV>(p, o);
+      load_cols<NV, ALIGNED>(p, o);
       each(f, [&](int i) { return f[i] + o[i]; });
     }
-    store_cols<NV>(p, f);
+    store_cols<NV, ALIGNED>(p, f);
   } else {
     if (e.accumulate) {
       aux_values<NV>(x, true, o);
       each(f, [&](int i) { return f[i] + o[i]; });
     }
-    store_cols<NV>(static_cast<float*>(e.out) + row * e.ldo + col, f);
+    store_cols<NV, ALIGNED>(static_cast<float*>(e.out) + row * e.ldo + col, f);
   }
 }
 
+// (bias vectors start at any float; those past the last column are zeros)
 template <int KIND, int NV>
 __device__ __forceinline__ void load_bias(const GemmEpilogue& e, int col, int n, float (&b)[NV]) {
 #pragma unroll
   for (int i = 0; i < NV; ++i) b[i] = 0.f;
   if constexpr (KIND == kGemmFwd) {
-    if (e.bias != nullptr && col < n) load_cols<NV>(e.bias + col, b);
+    if (e.bias == nullptr) return;
+    if (NV > 1 && col + NV <= n) load_cols<NV, false>(e.bias + col, b);
+    else {
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+        if (col + i < n) b[i] = e.bias[col + i];
+    }
+  }
+}
+
+// Eight columns of which those past the last are not there (rows that are not whole vectors): a whole
+// vector as one, the last of a row by elements.
+template <int KIND>
+__device__ __forceinline__ void finish_any(const GemmEpilogue& e, int64_t row, int col, int n, float (&f)[8],
+                                           const float (&bias)[8]) {
+  if (col >= n) return;
+  if (col + 8 <= n) {
+    Aux<8> x;
+    load_aux<KIND, 8, false>(e, row, col, x);
+    finish_cols<KIND, 8, false>(e, row, col, f, bias, x);
+    return;
+  }
+  float rest[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) rest[j] = bias[j];
+#pragma unroll 1
+  for (int i = 0; col + i < n; ++i) {  // (registers shift down: none is indexed by a variable)
+    float g[1] = {f[0]}, b[1] = {rest[0]};
+    Aux<1> x;
+    load_aux<KIND, 1>(e, row, col + i, x);
+    finish_cols<KIND, 1>(e, row, col + i, g, b, x);
+#pragma unroll
+    for (int j = 0; j < 7; ++j) {
+      f[j] = f[j + 1];
+      rest[j] = rest[j + 1];
+    }
   }
 }
 

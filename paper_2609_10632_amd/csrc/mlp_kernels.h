@@ -48,7 +48,8 @@ struct GemmPlan {
   int splits;
   int64_t k_per_split;
 };
-GemmPlan gemm_pick(GemmKind kind, int64_t m, int n, int64_t k);
+// out_bytes: what the epilogue reads and writes for each element
+GemmPlan gemm_pick(GemmKind kind, int64_t m, int n, int64_t k, int out_bytes);
 // whether the plan's kernel takes operands whose rows start at any element
 bool gemm_any_rows(const GemmPlan& p);
 size_t gemm_part_bytes(const GemmPlan& p, int64_t m, int n);
@@ -60,9 +61,15 @@ constexpr int kLinearRows = 16;
 hipError_t linear_rows_launch(const GemmArgs& a, hipStream_t s);
 
 // rows x cols of src (row stride lds) into dst with row stride ldd = cols rounded up to 8, the
-// padding zero
-hipError_t gemm_pack_launch(const bf16_t* src, int64_t lds, int64_t rows, int32_t cols, bf16_t* dst, int64_t ldd,
-                            hipStream_t s);
+// padding zero; rows = 0 for none
+struct GemmPack {
+  const bf16_t* src;
+  int64_t lds, rows;
+  int32_t cols;
+  bf16_t* dst;
+  int64_t ldd;
+};
+hipError_t gemm_pack_launch(const GemmPack& a, const GemmPack& b, hipStream_t s);
 
 // out[c] (+)= sum over rows of src[r][c], fp32: per-block partials, then their sum in a fixed order
 size_t colsum_part_bytes(int64_t rows, int32_t cols);
