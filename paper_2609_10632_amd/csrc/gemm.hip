@@ -170,12 +170,12 @@ __global__ __launch_bounds__(C::NW * 64) void gemm_kernel(GemmArgs a) {
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const uint32_t tiles = (uint32_t)a.tiles_m * (uint32_t)a.tiles_n;
   uint32_t t = xcd_remap(blockIdx.x, gridDim.x);
-  const uint32_t split = t / tiles;
+  const uint32_t split = a.splits > 1 ? fdiv(t, a.div_tiles) : 0;
   t -= split * tiles;
-  const uint32_t per_group = 8u * (uint32_t)a.tiles_n;
-  const uint32_t grp = t / per_group, in_grp = t - grp * per_group;
-  const uint32_t gsize = (uint32_t)a.tiles_m - grp * 8u < 8u ? (uint32_t)a.tiles_m - grp * 8u : 8u;
-  const uint32_t tn = in_grp / gsize, tm = grp * 8u + (in_grp - tn * gsize);
+  const uint32_t grp = fdiv(t, a.div_group), in_grp = t - grp * a.div_group.d;
+  const uint32_t gsize = (uint32_t)a.tiles_m - grp * 8u;  // rows of tiles left: 8, or those of the last column
+  const uint32_t tn = gsize >= 8u ? in_grp >> 3 : fdiv(in_grp, a.div_last);
+  const uint32_t tm = grp * 8u + in_grp - tn * (gsize >= 8u ? 8u : gsize);
   const int64_t m0 = (int64_t)tm * BM;
   const int n0 = (int)tn * BN;
   const int64_t k0 = (int64_t)split * a.k_per_split;
@@ -189,16 +189,18 @@ __global__ __launch_bounds__(C::NW * 64) void gemm_kernel(GemmArgs a) {
   constexpr int JS = C::OW / 32, STRIPS = TN / JS * TM;
   constexpr int VPR = C::OW / 8, RPP = 64 / VPR, NP = 32 / RPP;  // vectors per row, rows per pass, passes
   constexpr int XB = STRIPS <= 2 ? STRIPS : 2, AHEAD = XB == STRIPS ? STRIPS : 1;
-  auto row_of = [&](int s) __attribute__((always_inline)) { return m0 + (wm * TM + s % TM) * 32; };
-  auto col_of = [&](int s) __attribute__((always_inline)) { return n0 + (wn * TN + s / TM * JS) * 32; };
+  const EpiloguePtr ep = epilogue_at<KIND>(a.e, m0, n0);
+  const int rows = (int)(a.m - m0 < BM ? a.m - m0 : BM), cols = a.n - n0;  // of the tile
+  auto row_of = [&](int s) __attribute__((always_inline)) { return (wm * TM + s % TM) * 32 + lane / VPR; };
+  auto col_of = [&](int s) __attribute__((always_inline)) { return (wn * TN + s / TM * JS) * 32 + lane % VPR * 8; };
   Aux<8> x[XB][NP];
   auto fetch = [&](auto sc) __attribute__((always_inline)) {
     constexpr int s = decltype(sc)::value;
-    const int vc = col_of(s) + (lane % VPR) * 8;
+    const int c = col_of(s);
 #pragma unroll
     for (int p = 0; p < NP; ++p) {
-      const int64_t row = row_of(s) + p * RPP + lane / VPR;
-      if (row < a.m && vc < a.n) load_aux<KIND, 8>(a.e, row, vc, x[s % XB][p]);
+      const int r = row_of(s) + p * RPP;
+      if (r < rows && c < cols) load_aux<8>(ep, r, c, x[s % XB][p]);
     }
   };
   if (a.splits == 1 && a.e.vec) static_for<0, AHEAD>(fetch);
@@ -308,19 +310,23 @@ __global__ __launch_bounds__(C::NW * 64) void gemm_kernel(GemmArgs a) {
       }
     __builtin_amdgcn_wave_barrier();
   };
+  // 8 columns of row p RPP + lane / VPR of the strip
+  auto take = [&](int p, float (&f)[8]) __attribute__((always_inline)) {
+    load_cols<8>(out + (p * RPP + lane / VPR) * C::OLD + lane % VPR * 8, f);
+  };
   if (a.splits > 1) {
+    float* part = a.part + ((int64_t)split * a.m + m0) * a.ldp + n0;
     static_for<0, STRIPS>([&](auto sc) __attribute__((always_inline)) {
       constexpr int s = decltype(sc)::value;
       put(sc);
-      const int vc = col_of(s) + (lane % VPR) * 8;
+      const int c = col_of(s);
 #pragma unroll
       for (int p = 0; p < NP; ++p) {
-        const int r = p * RPP + lane / VPR;
-        const int64_t row = row_of(s) + r;
+        const int r = row_of(s) + p * RPP;
         float f[8];
-        load_cols<8>(out + r * C::OLD + (lane % VPR) * 8, f);
+        take(p, f);
         // (the partials' rows are padded to whole vectors)
-        if (row < a.m && vc < a.n) store_cols<8>(a.part + ((int64_t)split * a.m + row) * a.ldp + vc, f);
+        if (r < rows && c < cols) store_cols<8>(part + (int64_t)r * a.ldp + c, f);
       }
       __builtin_amdgcn_wave_barrier();
     });
@@ -329,17 +335,16 @@ __global__ __launch_bounds__(C::NW * 64) void gemm_kernel(GemmArgs a) {
     float bias[8];
     static_for<0, STRIPS>([&](auto sc) __attribute__((always_inline)) {
       constexpr int s = decltype(sc)::value;
-      const int vc = col_of(s) + (lane % VPR) * 8;
-      if constexpr (s % TM == 0) load_bias<KIND, 8>(a.e, vc, a.n, bias);
+      const int c = col_of(s);
+      if constexpr (s % TM == 0) load_bias<KIND, 8>(a.e, n0 + c, a.n, bias);
       if constexpr (s + AHEAD < STRIPS) fetch(Ic<s + AHEAD>{});
       put(sc);
 #pragma unroll
       for (int p = 0; p < NP; ++p) {
-        const int r = p * RPP + lane / VPR;
-        const int64_t row = row_of(s) + r;
+        const int r = row_of(s) + p * RPP;
         float f[8];
-        load_cols<8>(out + r * C::OLD + (lane % VPR) * 8, f);
-        if (row < a.m && vc < a.n) finish_cols<KIND, 8>(a.e, row, vc, f, bias, x[s % XB][p]);
+        take(p, f);
+        if (r < rows && c < cols) finish_cols<KIND, 8>(a.e, ep, r, c, f, bias, x[s % XB][p]);
       }
       __builtin_amdgcn_wave_barrier();
     });
@@ -347,16 +352,15 @@ __global__ __launch_bounds__(C::NW * 64) void gemm_kernel(GemmArgs a) {
     float bias[8];
     static_for<0, STRIPS>([&](auto sc) __attribute__((always_inline)) {
       constexpr int s = decltype(sc)::value;
-      const int vc = col_of(s) + (lane % VPR) * 8;
-      if constexpr (s % TM == 0) load_bias<KIND, 8>(a.e, vc, a.n, bias);
+      const int c = col_of(s);
+      if constexpr (s % TM == 0) load_bias<KIND, 8>(a.e, n0 + c, a.n, bias);
       put(sc);
 #pragma unroll 1
       for (int p = 0; p < NP; ++p) {
-        const int r = p * RPP + lane / VPR;
-        const int64_t row = row_of(s) + r;
+        const int r = row_of(s) + p * RPP;
         float f[8];
-        load_cols<8>(out + r * C::OLD + (lane % VPR) * 8, f);
-        if (row < a.m) finish_any<KIND>(a.e, row, vc, a.n, f, bias);
+        take(p, f);
+        if (r < rows) finish_any<KIND>(a.e, ep, r, c, cols - c, f, bias);
       }
       __builtin_amdgcn_wave_barrier();
     });
@@ -380,10 +384,11 @@ __global__ __launch_bounds__(256) void gemm_finish_kernel(GemmArgs a) {
 #pragma unroll
       for (int e = 0; e < NV; ++e) f[e] += b[e];
     }
+    const EpiloguePtr ep = epilogue_at<KIND>(a.e, row, col);
     Aux<NV> x;
-    load_aux<KIND, NV>(a.e, row, col, x);
+    load_aux<NV>(ep, 0, 0, x);
     load_bias<KIND, NV>(a.e, col, a.n, b);
-    finish_cols<KIND, NV>(a.e, row, col, f, b, x);
+    finish_cols<KIND, NV>(a.e, ep, 0, 0, f, b, x);
   }
 }
 
@@ -590,6 +595,9 @@ hipError_t gemm_launch(GemmKind kind, GemmArgs a, const GemmPlan& p, hipStream_t
   a.tiles_m = (int32_t)((a.m + t.m - 1) / t.m);
   a.tiles_n = (a.n + t.n - 1) / t.n;
   a.splits = p.splits;
+  a.div_tiles = make_fastdiv((uint32_t)a.tiles_m * (uint32_t)a.tiles_n);
+  a.div_group = make_fastdiv(8u * (uint32_t)a.tiles_n);
+  a.div_last = make_fastdiv(a.tiles_m % 8 ? a.tiles_m % 8 : 8);
   a.k_per_split = p.k_per_split;
   a.ldp = (a.n + 7) / 8 * 8;
   return kind == kGemmFwd     ? launch_kind<kGemmFwd>(a, p.tile, s)

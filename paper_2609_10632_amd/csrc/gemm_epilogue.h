@@ -69,26 +69,45 @@ template <int NV>
 struct Aux {
   uint4 lo, hi;  // 8 bf16, or 8 fp32; element 0 alone for NV = 1
 };
+
+// The epilogue's matrices from one element of theirs, a tile's first as a rule: bases that are the
+// same for a whole block and 32-bit byte offsets from there (a tile is at most 256 rows of 2^21
+// elements), which cost a lane one multiply-add where 64-bit addresses cost it ten instructions.
+struct EpiloguePtr {
+  char *out, *z;
+  const char* aux;            // nullptr: none
+  uint32_t ldo, ldz, ldx;     // bytes between rows
+  bool out_f32, aux_f32;
+};
 template <int KIND>
-__device__ __forceinline__ const void* aux_base(const GemmEpilogue& e, int64_t* ld, bool* f32) {
-  *f32 = KIND == kGemmWgrad || (KIND == kGemmFwd && e.out_f32);
-  *ld = KIND == kGemmFwd ? e.ldr : KIND == kGemmDgrad ? e.ldz : e.ldo;
-  return KIND == kGemmFwd     ? e.res
-         : KIND == kGemmDgrad ? (e.act != kActNone ? e.z : nullptr)
-                              : (e.accumulate ? e.out : nullptr);
+__device__ __forceinline__ EpiloguePtr epilogue_at(const GemmEpilogue& e, int64_t row, int64_t col) {
+  EpiloguePtr p;
+  p.out_f32 = KIND == kGemmWgrad || (KIND == kGemmFwd && e.out_f32);
+  p.aux_f32 = KIND != kGemmDgrad && p.out_f32;
+  const int so = p.out_f32 ? 4 : 2, sx = p.aux_f32 ? 4 : 2;
+  const void* aux = KIND == kGemmFwd     ? e.res
+                    : KIND == kGemmDgrad ? (e.act != kActNone ? e.z : nullptr)
+                                         : (e.accumulate ? e.out : nullptr);
+  const int64_t ldx = KIND == kGemmFwd ? e.ldr : KIND == kGemmDgrad ? e.ldz : e.ldo;
+  p.ldo = (uint32_t)e.ldo * so;
+  p.ldz = (uint32_t)e.ldz * 2;
+  p.ldx = (uint32_t)ldx * sx;
+  p.out = static_cast<char*>(e.out) + (row * e.ldo + col) * so;
+  p.z = KIND == kGemmFwd && e.z != nullptr ? reinterpret_cast<char*>(e.z + row * e.ldz + col) : nullptr;
+  p.aux = aux != nullptr ? static_cast<const char*>(aux) + (row * ldx + col) * sx : nullptr;
+  return p;
 }
-template <int KIND, int NV, bool ALIGNED = true>
-__device__ __forceinline__ void load_aux(const GemmEpilogue& e, int64_t row, int col, Aux<NV>& x) {
-  int64_t ld;
-  bool f32;
-  const void* base = aux_base<KIND>(e, &ld, &f32);
-  if (base == nullptr) return;
-  const char* p = static_cast<const char*>(base) + (row * ld + col) * (f32 ? 4 : 2);
+
+// row r and column c count from the element that p points to
+template <int NV, bool ALIGNED = true>
+__device__ __forceinline__ void load_aux(const EpiloguePtr& p, uint32_t r, uint32_t c, Aux<NV>& x) {
+  if (p.aux == nullptr) return;
+  const char* at = p.aux + (uint32_t)(r * p.ldx + c * (p.aux_f32 ? 4 : 2));
   if constexpr (NV == 8) {
-    x.lo = load16<ALIGNED>(p);
-    if (f32) x.hi = load16<ALIGNED>(p + 16);
+    x.lo = load16<ALIGNED>(at);
+    if (p.aux_f32) x.hi = load16<ALIGNED>(at + 16);
   } else {
-    x.lo.x = f32 ? *reinterpret_cast<const uint32_t*>(p) : *reinterpret_cast<const uint16_t*>(p);
+    x.lo.x = p.aux_f32 ? *reinterpret_cast<const uint32_t*>(at) : *reinterpret_cast<const uint16_t*>(at);
   }
 }
 template <int NV>
@@ -114,12 +133,13 @@ __device__ __forceinline__ void each(float (&f)[NV], F&& fn) {
 
 // f: the sums; bias: those of the columns; x: loaded by load_aux
 template <int KIND, int NV, bool ALIGNED = true>
-__device__ __forceinline__ void finish_cols(const GemmEpilogue& e, int64_t row, int col, float (&f)[NV],
-                                            const float (&bias)[NV], const Aux<NV>& x) {
+__device__ __forceinline__ void finish_cols(const GemmEpilogue& e, const EpiloguePtr& p, uint32_t r, uint32_t c,
+                                            float (&f)[NV], const float (&bias)[NV], const Aux<NV>& x) {
   float o[NV];
+  char* out = p.out + (uint32_t)(r * p.ldo + c * (p.out_f32 ? 4 : 2));
   if constexpr (KIND == kGemmFwd) {
     each(f, [&](int i) { return f[i] + bias[i]; });
-    if (e.z != nullptr) store_cols<NV, ALIGNED>(e.z + row * e.ldz + col, f);
+    if (p.z != nullptr) store_cols<NV, ALIGNED>(reinterpret_cast<bf16_t*>(p.z + (uint32_t)(r * p.ldz + c * 2)), f);
     // (one branch for the vector, not one per element)
     switch (e.act) {
       case kActRelu: each(f, [&](int i) { return act_apply(f[i], kActRelu); }); break;
@@ -128,12 +148,10 @@ __device__ __forceinline__ void finish_cols(const GemmEpilogue& e, int64_t row, 
       case kActSilu: each(f, [&](int i) { return act_apply(f[i], kActSilu); }); break;
       default: break;
     }
-    if (e.res != nullptr) {
-      aux_values<NV>(x, e.out_f32, o);
+    if (p.aux != nullptr) {
+      aux_values<NV>(x, p.aux_f32, o);
       each(f, [&](int i) { return f[i] + o[i]; });
     }
-    if (e.out_f32) store_cols<NV, ALIGNED>(static_cast<float*>(e.out) + row * e.ldo + col, f);
-    else store_cols<NV, ALIGNED>(static_cast<bf16_t*>(e.out) + row * e.ldo + col, f);
   } else if constexpr (KIND == kGemmDgrad) {
     if (e.act != kActNone) aux_values<NV>(x, false, o);
     switch (e.act) {
@@ -143,19 +161,18 @@ __device__ __forceinline__ void finish_cols(const GemmEpilogue& e, int64_t row, 
       case kActSilu: each(f, [&](int i) { return f[i] * act_slope(o[i], kActSilu); }); break;
       default: break;
     }
-    bf16_t* p = static_cast<bf16_t*>(e.out) + row * e.ldo + col;
     if (e.accumulate) {
-      load_cols<NV, ALIGNED>(p, o);
+      load_cols<NV, ALIGNED>(reinterpret_cast<const bf16_t*>(out), o);
       each(f, [&](int i) { return f[i] + o[i]; });
     }
-    store_cols<NV, ALIGNED>(p, f);
   } else {
     if (e.accumulate) {
       aux_values<NV>(x, true, o);
       each(f, [&](int i) { return f[i] + o[i]; });
     }
-    store_cols<NV, ALIGNED>(static_cast<float*>(e.out) + row * e.ldo + col, f);
   }
+  if (p.out_f32) store_cols<NV, ALIGNED>(reinterpret_cast<float*>(out), f);
+  else store_cols<NV, ALIGNED>(reinterpret_cast<bf16_t*>(out), f);
 }
 
 // (bias vectors start at any float; those past the last column are zeros)
@@ -174,27 +191,26 @@ __device__ __forceinline__ void load_bias(const GemmEpilogue& e, int col, int n,
   }
 }
 
-// Eight columns of which those past the last are not there (rows that are not whole vectors): a whole
-// vector as one, the last of a row by elements.
+// Eight columns, of which `cols` are left in the row (rows that are not whole vectors): a whole vector
+// as one, the last of a row by elements.
 template <int KIND>
-__device__ __forceinline__ void finish_any(const GemmEpilogue& e, int64_t row, int col, int n, float (&f)[8],
-                                           const float (&bias)[8]) {
-  if (col >= n) return;
-  if (col + 8 <= n) {
+__device__ __forceinline__ void finish_any(const GemmEpilogue& e, const EpiloguePtr& p, uint32_t r, uint32_t c, int cols,
+                                           float (&f)[8], const float (&bias)[8]) {
+  if (cols >= 8) {
     Aux<8> x;
-    load_aux<KIND, 8, false>(e, row, col, x);
-    finish_cols<KIND, 8, false>(e, row, col, f, bias, x);
+    load_aux<8, false>(p, r, c, x);
+    finish_cols<KIND, 8, false>(e, p, r, c, f, bias, x);
     return;
   }
   float rest[8];
 #pragma unroll
   for (int j = 0; j < 8; ++j) rest[j] = bias[j];
 #pragma unroll 1
-  for (int i = 0; col + i < n; ++i) {  // (registers shift down: none is indexed by a variable)
+  for (int i = 0; i < cols; ++i) {  // (registers shift down: none is indexed by a variable)
     float g[1] = {f[0]}, b[1] = {rest[0]};
     Aux<1> x;
-    load_aux<KIND, 1>(e, row, col + i, x);
-    finish_cols<KIND, 1>(e, row, col + i, g, b, x);
+    load_aux<1>(p, r, c + i, x);
+    finish_cols<KIND, 1>(e, p, r, c + i, g, b, x);
 #pragma unroll
     for (int j = 0; j < 7; ++j) {
       f[j] = f[j + 1];

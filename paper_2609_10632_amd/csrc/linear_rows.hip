@@ -49,7 +49,8 @@ __global__ __launch_bounds__(NW * 64) void linear_rows_kernel(GemmArgs a) {
   float bias[1];
   Aux<1> aux;
   load_bias<kGemmFwd, 1>(a.e, oc, a.n, bias);
-  if (mine) load_aux<kGemmFwd, 1>(a.e, orow, oc, aux);
+  const EpiloguePtr ep = epilogue_at<kGemmFwd>(a.e, 0, n0);
+  if (mine) load_aux<1>(ep, orow, tid & 15, aux);
 
   // (rows past the end read the last one: their sums are not stored)
   const bf16_t* wrow = a.b + (int64_t)(n0 + l16 < a.n ? n0 + l16 : a.n - 1) * a.ldb;
@@ -92,7 +93,7 @@ __global__ __launch_bounds__(NW * 64) void linear_rows_kernel(GemmArgs a) {
   float f[1] = {s_sum[0][orow][tid & 15]};
 #pragma unroll
   for (int w = 1; w < NW; ++w) f[0] += s_sum[w][orow][tid & 15];
-  finish_cols<kGemmFwd, 1>(a.e, orow, oc, f, bias, aux);
+  finish_cols<kGemmFwd, 1>(a.e, ep, orow, tid & 15, f, bias, aux);
 }
 
 template <int NW>

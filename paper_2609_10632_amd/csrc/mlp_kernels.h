@@ -35,6 +35,7 @@ struct GemmArgs {
   int64_t m, k;
   int32_t n;
   int32_t tiles_m, tiles_n;
+  FastDiv div_tiles, div_group, div_last;  // by the tiles, by 8 rows of them, by the last rows (set by gemm_launch)
   int32_t splits;       // reduction ranges; above 1 the sums go to part
   int64_t k_per_split;  // a multiple of the reduction step
   float* part;          // [splits][m][ldp] fp32
