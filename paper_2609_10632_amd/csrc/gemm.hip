@@ -183,27 +183,40 @@ __global__ __launch_bounds__(C::NW * 64) void gemm_kernel(GemmArgs a) {
   const int nk = (int)((left + BK - 1) / BK);
 
   const int wm = wave / C::WN, wn = wave % C::WN;
-  // The epilogue goes by strips of 32 rows x OW columns of the wave's sums.  What it reads beside them
-  // for the first strips is loaded before anything else, so that it is there when the sums are (and
-  // these loads, the oldest, disturb no count of those in flight).
+  // The epilogue goes by strips of 32 rows x OW columns of the wave's sums, 16 bytes of results a lane
+  // (8 columns of bf16 or 4 of fp32).  What it reads beside the sums for the first strips is loaded
+  // before anything else, so that it is there when the sums are (and these loads, the oldest, disturb
+  // no count of those in flight).
   constexpr int JS = C::OW / 32, STRIPS = TN / JS * TM;
-  constexpr int VPR = C::OW / 8, RPP = 64 / VPR, NP = 32 / RPP;  // vectors per row, rows per pass, passes
   constexpr int XB = STRIPS <= 2 ? STRIPS : 2, AHEAD = XB == STRIPS ? STRIPS : 1;
   const EpiloguePtr ep = epilogue_at<KIND>(a.e, m0, n0);
   const int rows = (int)(a.m - m0 < BM ? a.m - m0 : BM), cols = a.n - n0;  // of the tile
-  auto row_of = [&](int s) __attribute__((always_inline)) { return (wm * TM + s % TM) * 32 + lane / VPR; };
-  auto col_of = [&](int s) __attribute__((always_inline)) { return (wn * TN + s / TM * JS) * 32 + lane % VPR * 8; };
-  Aux<8> x[XB][NP];
-  auto fetch = [&](auto sc) __attribute__((always_inline)) {
-    constexpr int s = decltype(sc)::value;
-    const int c = col_of(s);
+  Aux x[XB][C::OW / (KIND == kGemmDgrad ? 16 : 8)];
+  // row, column and passes of a strip with NV columns a lane
+  auto row_of = [&](int s, int nv) __attribute__((always_inline)) { return (wm * TM + s % TM) * 32 + lane / (C::OW / nv); };
+  auto col_of = [&](int s, int nv) __attribute__((always_inline)) {
+    return (wn * TN + s / TM * JS) * 32 + lane % (C::OW / nv) * nv;
+  };
+  auto fetch = [&](auto nvc, auto sc) __attribute__((always_inline)) {
+    constexpr int NV = decltype(nvc)::value, s = decltype(sc)::value, RPP = 64 * NV / C::OW;
+    const int c = col_of(s, NV);
 #pragma unroll
-    for (int p = 0; p < NP; ++p) {
-      const int r = row_of(s) + p * RPP;
-      if (r < rows && c < cols) load_aux<8>(ep, r, c, x[s % XB][p]);
+    for (int p = 0; p < 32 / RPP; ++p) {
+      const int r = row_of(s, NV) + p * RPP;
+      if (r < rows && c < cols) load_aux<NV>(ep, r, c, x[s % XB][p]);
     }
   };
-  if (a.splits == 1 && a.e.vec) static_for<0, AHEAD>(fetch);
+  // f(columns a lane): 8 or 4 by the type of the results
+  auto by_type = [&](auto&& f) __attribute__((always_inline)) {
+    if constexpr (KIND == kGemmDgrad) f(Ic<8>{});
+    else if constexpr (KIND == kGemmWgrad) f(Ic<4>{});
+    else if (ep.out_f32) f(Ic<4>{});
+    else f(Ic<8>{});
+  };
+  if (a.splits == 1 && a.e.vec)
+    by_type([&](auto nvc) __attribute__((always_inline)) {
+      static_for<0, AHEAD>([&](auto sc) __attribute__((always_inline)) { fetch(nvc, sc); });
+    });
 
   Operand<TA, BM, BK, NW, C::AI> oa;
   Operand<TB, BN, BK, NW, C::BI> ob;
@@ -310,85 +323,111 @@ __global__ __launch_bounds__(C::NW * 64) void gemm_kernel(GemmArgs a) {
       }
     __builtin_amdgcn_wave_barrier();
   };
-  // 8 columns of row p RPP + lane / VPR of the strip
-  auto take = [&](int p, float (&f)[8]) __attribute__((always_inline)) {
-    load_cols<8>(out + (p * RPP + lane / VPR) * C::OLD + lane % VPR * 8, f);
+  // NV columns of the lane's row of pass p of the strip
+  auto take = [&](int p, auto& f) __attribute__((always_inline)) {
+    constexpr int NV = sizeof(f) / 4, VPR = C::OW / NV, RPP = 64 / VPR;
+    const float4* at = reinterpret_cast<const float4*>(out + (p * RPP + lane / VPR) * C::OLD + lane % VPR * NV);
+#pragma unroll
+    for (int i = 0; i < NV / 4; ++i) {
+      const float4 v = at[i];
+      f[4 * i] = v.x;
+      f[4 * i + 1] = v.y;
+      f[4 * i + 2] = v.z;
+      f[4 * i + 3] = v.w;
+    }
   };
   if (a.splits > 1) {
+    constexpr int RPP = 256 / C::OW;
     float* part = a.part + ((int64_t)split * a.m + m0) * a.ldp + n0;
     static_for<0, STRIPS>([&](auto sc) __attribute__((always_inline)) {
       constexpr int s = decltype(sc)::value;
       put(sc);
-      const int c = col_of(s);
+      const int c = col_of(s, 4);
 #pragma unroll
-      for (int p = 0; p < NP; ++p) {
-        const int r = row_of(s) + p * RPP;
-        float f[8];
+      for (int p = 0; p < 32 / RPP; ++p) {
+        const int r = row_of(s, 4) + p * RPP;
+        float f[4];
         take(p, f);
         // (the partials' rows are padded to whole vectors)
-        if (r < rows && c < cols) store_cols<8>(part + (int64_t)r * a.ldp + c, f);
+        if (r < rows && c < cols) store_cols<4>(part + (int64_t)r * a.ldp + c, f);
       }
       __builtin_amdgcn_wave_barrier();
     });
-  } else if (a.e.vec) {
-    // the next strip's auxiliary loads are in flight while a strip is finished
-    float bias[8];
-    static_for<0, STRIPS>([&](auto sc) __attribute__((always_inline)) {
-      constexpr int s = decltype(sc)::value;
-      const int c = col_of(s);
-      if constexpr (s % TM == 0) load_bias<KIND, 8>(a.e, n0 + c, a.n, bias);
-      if constexpr (s + AHEAD < STRIPS) fetch(Ic<s + AHEAD>{});
-      put(sc);
-#pragma unroll
-      for (int p = 0; p < NP; ++p) {
-        const int r = row_of(s) + p * RPP;
-        float f[8];
-        take(p, f);
-        if (r < rows && c < cols) finish_cols<KIND, 8>(a.e, ep, r, c, f, bias, x[s % XB][p]);
-      }
-      __builtin_amdgcn_wave_barrier();
-    });
-  } else {
-    float bias[8];
-    static_for<0, STRIPS>([&](auto sc) __attribute__((always_inline)) {
-      constexpr int s = decltype(sc)::value;
-      const int c = col_of(s);
-      if constexpr (s % TM == 0) load_bias<KIND, 8>(a.e, n0 + c, a.n, bias);
-      put(sc);
-#pragma unroll 1
-      for (int p = 0; p < NP; ++p) {
-        const int r = row_of(s) + p * RPP;
-        float f[8];
-        take(p, f);
-        if (r < rows) finish_any<KIND>(a.e, ep, r, c, cols - c, f, bias);
-      }
-      __builtin_amdgcn_wave_barrier();
-    });
+    return;
   }
+  by_type([&](auto nvc) __attribute__((always_inline)) {
+    constexpr int NV = decltype(nvc)::value, RPP = 64 * NV / C::OW;
+    float bias[NV];
+    if (a.e.vec) {
+      // the next strip's auxiliary loads are in flight while a strip is finished
+      static_for<0, STRIPS>([&](auto sc) __attribute__((always_inline)) {
+        constexpr int s = decltype(sc)::value;
+        const int c = col_of(s, NV);
+        if constexpr (s % TM == 0) load_bias<KIND, NV>(a.e, n0 + c, a.n, bias);
+        if constexpr (s + AHEAD < STRIPS) fetch(nvc, Ic<s + AHEAD>{});
+        put(sc);
+#pragma unroll
+        for (int p = 0; p < 32 / RPP; ++p) {
+          const int r = row_of(s, NV) + p * RPP;
+          float f[NV];
+          take(p, f);
+          if (r < rows && c < cols) finish_cols<KIND, NV>(a.e, ep, r, c, f, bias, x[s % XB][p]);
+        }
+        __builtin_amdgcn_wave_barrier();
+      });
+    } else {
+      static_for<0, STRIPS>([&](auto sc) __attribute__((always_inline)) {
+        constexpr int s = decltype(sc)::value;
+        const int c = col_of(s, NV);
+        if constexpr (s % TM == 0) load_bias<KIND, NV>(a.e, n0 + c, a.n, bias);
+        put(sc);
+#pragma unroll 1
+        for (int p = 0; p < 32 / RPP; ++p) {
+          const int r = row_of(s, NV) + p * RPP;
+          float f[NV];
+          take(p, f);
+          if (r < rows) finish_any<KIND, NV>(a.e, ep, r, c, cols - c, f, bias);
+        }
+        __builtin_amdgcn_wave_barrier();
+      });
+    }
+  });
 }
 
-// the sums of the reduction ranges, added in order, then the epilogue
-template <int KIND, int NV>
+// the sums of the reduction ranges, added in order (eight ranges' loads in flight), then the epilogue
+template <int KIND, bool VEC>
 __global__ __launch_bounds__(256) void gemm_finish_kernel(GemmArgs a) {
-  const int per_row = (a.n + NV - 1) / NV;
-  const int64_t total = a.m * per_row;
+  const int per_row = (a.n + 3) / 4;
+  const int64_t total = a.m * per_row, step = a.m * a.ldp;
   for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < total; i += gridDim.x * 256ll) {
     const int64_t row = i / per_row;
-    const int col = (int)(i - row * per_row) * NV;
-    float f[NV], b[NV];
-#pragma unroll
-    for (int e = 0; e < NV; ++e) f[e] = 0.f;
+    const int col = (int)(i - row * per_row) * 4;
+    float f[4] = {}, b[4];
     const float* p = a.part + row * a.ldp + col;
-    for (int s = 0; s < a.splits; ++s, p += a.m * a.ldp) {
-      load_cols<NV>(p, b);
+    auto add = [&](auto countc) __attribute__((always_inline)) {
+      constexpr int COUNT = decltype(countc)::value;
+      float v[COUNT][4];
 #pragma unroll
-      for (int e = 0; e < NV; ++e) f[e] += b[e];
-    }
+      for (int s = 0; s < COUNT; ++s) load_cols<4>(p + s * step, v[s]);
+#pragma unroll
+      for (int s = 0; s < COUNT; ++s)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) f[e] += v[s][e];
+      p += COUNT * step;
+    };
+    int s = 0;
+    for (; s + 8 <= a.splits; s += 8) add(Ic<8>{});
+    for (; s + 2 <= a.splits; s += 2) add(Ic<2>{});
+    if (s < a.splits) add(Ic<1>{});
     const EpiloguePtr ep = epilogue_at<KIND>(a.e, row, col);
-    Aux<NV> x;
-    load_aux<NV>(ep, 0, 0, x);
-    load_bias<KIND, NV>(a.e, col, a.n, b);
-    finish_cols<KIND, NV>(a.e, ep, 0, 0, f, b, x);
+    load_bias<KIND, 4>(a.e, col, a.n, b);
+    if constexpr (VEC) {
+      Aux x;
+      load_aux<4>(ep, 0, 0, x);
+      finish_cols<KIND, 4>(a.e, ep, 0, 0, f, b, x);
+    } else {
+      finish_any<KIND, 4>(a.e, ep, 0, 0, a.n - col, f, b);
+    }
   }
 }
 
@@ -505,11 +544,12 @@ __global__ __launch_bounds__(256) void fill_zero_kernel(float* p, int64_t n) {
 unsigned grid_for(int64_t threads) { return (unsigned)std::min<int64_t>(4096, std::max<int64_t>(1, (threads + 255) / 256)); }
 
 using T256 = Tile<256, 256, 32, 4, 2, 4>;
+using T128W = Tile<128, 256, 64, 3, 2, 4>;
 using T128D = Tile<128, 128, 64, 4, 2, 4>;
 using T128 = Tile<128, 128, 64, 2, 2, 4>;
 using T64 = Tile<64, 64, 64, 4, 2, 2>;
 
-enum { kTile256, kTile128D, kTile128, kTile64, kTileRows };
+enum { kTile256, kTile128W, kTile128D, kTile128, kTile64, kTileRows };
 
 template <int KIND, typename C>
 hipError_t launch_tile(const GemmArgs& a, hipStream_t s) {
@@ -521,14 +561,16 @@ template <int KIND>
 hipError_t launch_kind(const GemmArgs& a, int tile, hipStream_t s) {
   trace_begin(KC_LINEAR);
   hipError_t e = tile == kTile256    ? launch_tile<KIND, T256>(a, s)
+                 : tile == kTile128W ? launch_tile<KIND, T128W>(a, s)
                  : tile == kTile128D ? launch_tile<KIND, T128D>(a, s)
                  : tile == kTile128  ? launch_tile<KIND, T128>(a, s)
                                      : launch_tile<KIND, T64>(a, s);
   trace_end(KC_LINEAR);
   if (e != hipSuccess || a.splits == 1) return e;
   trace_begin(KC_LINEAR_FINISH);
-  if (a.e.vec) NUMBAT_LAUNCH((gemm_finish_kernel<KIND, 8>), dim3(grid_for(a.m * ((a.n + 7) / 8))), dim3(256), 0, s, a);
-  else NUMBAT_LAUNCH((gemm_finish_kernel<KIND, 1>), dim3(grid_for(a.m * a.n)), dim3(256), 0, s, a);
+  const dim3 grid(grid_for(a.m * ((a.n + 3) / 4)));
+  if (a.e.vec) NUMBAT_LAUNCH((gemm_finish_kernel<KIND, true>), grid, dim3(256), 0, s, a);
+  else NUMBAT_LAUNCH((gemm_finish_kernel<KIND, false>), grid, dim3(256), 0, s, a);
   trace_end(KC_LINEAR_FINISH);
   return hipGetLastError();
 }
@@ -536,7 +578,7 @@ hipError_t launch_kind(const GemmArgs& a, int tile, hipStream_t s) {
 struct TileSize {
   int m, n;
 };
-constexpr TileSize kTiles[] = {{T256::BM, T256::BN}, {T128D::BM, T128D::BN}, {T128::BM, T128::BN}, {T64::BM, T64::BN}};
+constexpr TileSize kTiles[] = {{T256::BM, T256::BN}, {T128W::BM, T128W::BN}, {T128D::BM, T128D::BN}, {T128::BM, T128::BN}, {T64::BM, T64::BN}};
 int64_t tile_count(int tile, int64_t m, int n) {
   const TileSize t = kTiles[tile];
   return ((m + t.m - 1) / t.m) * ((n + t.n - 1) / t.n);
@@ -548,6 +590,7 @@ double tile_time(int tile, int64_t blocks, int64_t k, int out_bytes) {
   const double b = (double)blocks;
   switch (tile) {
     case kTile256: return std::ceil(b / 256) * (1.5 + 2.75 * out_bytes + 0.0255 * k);
+    case kTile128W: return std::ceil(b / 256) * (1.4 + 1.5 * out_bytes + (blocks <= 256 ? 0.012 : 0.0135) * k);
     case kTile128D: return std::ceil(b / 256) * (1.2 + 0.65 * out_bytes + 0.0079 * k);
     case kTile128:
       return blocks <= 256 ? 3.0 + 0.0115 * k : std::max(1.0, b / 512 + 0.25) * (2.5 + 0.75 * out_bytes + 0.015 * k);
@@ -557,7 +600,7 @@ double tile_time(int tile, int64_t blocks, int64_t k, int out_bytes) {
 }
 
 // and the second launch that adds the sums of the splits
-double finish_time(int splits, int64_t m, int n) { return splits == 1 ? 0.0 : 4.0 + (double)splits * m * n * 8 / 4e6; }
+double finish_time(int splits, int64_t m, int n) { return splits == 1 ? 0.0 : 4.0 + 0.1 * splits + (double)splits * m * n * 8 / 4e6; }
 
 }  // namespace
 

@@ -26,18 +26,36 @@ __device__ __forceinline__ void store16(void* p, u32x4 v) {
   else *static_cast<AnyVec*>(p) = AnyVec{{v.x, v.y, v.z, v.w}};
 }
 
+struct __attribute__((packed, aligned(2))) AnyHalf {
+  uint32_t u[2];
+};
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
+// NV consecutive columns: 8 or 4 of bf16, 4 of fp32 (16 bytes a lane, so that neighbouring lanes'
+// accesses join to whole lines), or 1
 template <int NV, bool ALIGNED = true>
 __device__ __forceinline__ void load_cols(const bf16_t* p, float (&f)[NV]) {
-  if constexpr (NV == 8) unpack8(load16<ALIGNED>(p), f);
-  else f[0] = bf2f(*p);
+  if constexpr (NV == 8) {
+    unpack8(load16<ALIGNED>(p), f);
+  } else if constexpr (NV == 4) {
+    const AnyHalf v = *reinterpret_cast<const AnyHalf*>(p);
+    f[0] = bf2f(v.u[0] & 0xffffu);
+    f[1] = bf2f(v.u[0] >> 16);
+    f[2] = bf2f(v.u[1] & 0xffffu);
+    f[3] = bf2f(v.u[1] >> 16);
+  } else {
+    f[0] = bf2f(*p);
+  }
 }
 template <int NV, bool ALIGNED = true>
 __device__ __forceinline__ void load_cols(const float* p, float (&f)[NV]) {
-  if constexpr (NV == 8) {
-    const uint4 lo = load16<ALIGNED>(p), hi = load16<ALIGNED>(p + 4);
-    const uint32_t u[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
-#pragma unroll
-    for (int i = 0; i < 8; ++i) f[i] = __uint_as_float(u[i]);
+  static_assert(NV == 4 || NV == 1, "four columns of fp32 at a time");
+  if constexpr (NV == 4) {
+    const uint4 v = load16<ALIGNED>(p);
+    f[0] = __uint_as_float(v.x);
+    f[1] = __uint_as_float(v.y);
+    f[2] = __uint_as_float(v.z);
+    f[3] = __uint_as_float(v.w);
   } else {
     f[0] = *p;
   }
@@ -47,28 +65,24 @@ __device__ __forceinline__ void store_cols(bf16_t* p, const float (&f)[NV]) {
   if constexpr (NV == 8) {
     const uint4 v = pack8(f);
     store16<ALIGNED>(p, u32x4{v.x, v.y, v.z, v.w});
+  } else if constexpr (NV == 4) {
+    const u32x2 v = {pack2(f[0], f[1]), pack2(f[2], f[3])};
+    if constexpr (ALIGNED) __builtin_nontemporal_store(v, reinterpret_cast<u32x2*>(p));
+    else *reinterpret_cast<AnyHalf*>(p) = AnyHalf{{v.x, v.y}};
   } else {
     *p = (bf16_t)f2bf(f[0]);
   }
 }
 template <int NV, bool ALIGNED = true>
 __device__ __forceinline__ void store_cols(float* p, const float (&f)[NV]) {
-  if constexpr (NV == 8) {
-    const f32x4 lo = {f[0], f[1], f[2], f[3]}, hi = {f[4], f[5], f[6], f[7]};
-    store16<ALIGNED>(p, __builtin_bit_cast(u32x4, lo));
-    store16<ALIGNED>(p + 4, __builtin_bit_cast(u32x4, hi));
-  } else {
-    *p = f[0];
-  }
+  if constexpr (NV == 4) store16<ALIGNED>(p, __builtin_bit_cast(u32x4, f32x4{f[0], f[1], f[2], f[3]}));
+  else if constexpr (NV == 1) *p = f[0];
 }
 
 // The matrix that the epilogue reads beside the sums: the residual (forward), z (data gradient
 // through an activation) or the old values (weight gradient that accumulates).  Raw, so that its
 // loads can be issued early and cost few registers.
-template <int NV>
-struct Aux {
-  uint4 lo, hi;  // 8 bf16, or 8 fp32; element 0 alone for NV = 1
-};
+typedef uint4 Aux;  // 8 or 4 bf16, 4 fp32, or one element
 
 // The epilogue's matrices from one element of theirs, a tile's first as a rule: bases that are the
 // same for a whole block and 32-bit byte offsets from there (a tile is at most 256 rows of 2^21
@@ -100,28 +114,34 @@ __device__ __forceinline__ EpiloguePtr epilogue_at(const GemmEpilogue& e, int64_
 
 // row r and column c count from the element that p points to
 template <int NV, bool ALIGNED = true>
-__device__ __forceinline__ void load_aux(const EpiloguePtr& p, uint32_t r, uint32_t c, Aux<NV>& x) {
+__device__ __forceinline__ void load_aux(const EpiloguePtr& p, uint32_t r, uint32_t c, Aux& x) {
   if (p.aux == nullptr) return;
   const char* at = p.aux + (uint32_t)(r * p.ldx + c * (p.aux_f32 ? 4 : 2));
   if constexpr (NV == 8) {
-    x.lo = load16<ALIGNED>(at);
-    if (p.aux_f32) x.hi = load16<ALIGNED>(at + 16);
+    x = load16<ALIGNED>(at);
+  } else if constexpr (NV == 4) {
+    if (p.aux_f32) {
+      x = load16<ALIGNED>(at);
+    } else {
+      const AnyHalf v = *reinterpret_cast<const AnyHalf*>(at);
+      x.x = v.u[0];
+      x.y = v.u[1];
+    }
   } else {
-    x.lo.x = p.aux_f32 ? *reinterpret_cast<const uint32_t*>(at) : *reinterpret_cast<const uint16_t*>(at);
+    x.x = p.aux_f32 ? *reinterpret_cast<const uint32_t*>(at) : *reinterpret_cast<const uint16_t*>(at);
   }
 }
 template <int NV>
-__device__ __forceinline__ void aux_values(const Aux<NV>& x, bool f32, float (&f)[NV]) {
+__device__ __forceinline__ void aux_values(const Aux& x, bool f32, float (&f)[NV]) {
   if constexpr (NV == 8) {
-    if (f32) {
-      const uint32_t u[8] = {x.lo.x, x.lo.y, x.lo.z, x.lo.w, x.hi.x, x.hi.y, x.hi.z, x.hi.w};
-#pragma unroll
-      for (int i = 0; i < 8; ++i) f[i] = __uint_as_float(u[i]);
-    } else {
-      unpack8(x.lo, f);
-    }
+    unpack8(x, f);
+  } else if constexpr (NV == 4) {
+    f[0] = f32 ? __uint_as_float(x.x) : bf2f(x.x & 0xffffu);
+    f[1] = f32 ? __uint_as_float(x.y) : bf2f(x.x >> 16);
+    f[2] = f32 ? __uint_as_float(x.z) : bf2f(x.y & 0xffffu);
+    f[3] = f32 ? __uint_as_float(x.w) : bf2f(x.y >> 16);
   } else {
-    f[0] = f32 ? __uint_as_float(x.lo.x) : bf2f(x.lo.x);
+    f[0] = f32 ? __uint_as_float(x.x) : bf2f(x.x);
   }
 }
 
@@ -134,7 +154,7 @@ __device__ __forceinline__ void each(float (&f)[NV], F&& fn) {
 // f: the sums; bias: those of the columns; x: loaded by load_aux
 template <int KIND, int NV, bool ALIGNED = true>
 __device__ __forceinline__ void finish_cols(const GemmEpilogue& e, const EpiloguePtr& p, uint32_t r, uint32_t c,
-                                            float (&f)[NV], const float (&bias)[NV], const Aux<NV>& x) {
+                                            float (&f)[NV], const float (&bias)[NV], const Aux& x) {
   float o[NV];
   char* out = p.out + (uint32_t)(r * p.ldo + c * (p.out_f32 ? 4 : 2));
   if constexpr (KIND == kGemmFwd) {
@@ -171,8 +191,10 @@ __device__ __forceinline__ void finish_cols(const GemmEpilogue& e, const Epilogu
       each(f, [&](int i) { return f[i] + o[i]; });
     }
   }
-  if (p.out_f32) store_cols<NV, ALIGNED>(reinterpret_cast<float*>(out), f);
-  else store_cols<NV, ALIGNED>(reinterpret_cast<bf16_t*>(out), f);
+  if constexpr (NV != 8) {  // (fp32 results never come in eights)
+    if (p.out_f32) return store_cols<NV, ALIGNED>(reinterpret_cast<float*>(out), f);
+  }
+  if constexpr (KIND != kGemmWgrad) store_cols<NV, ALIGNED>(reinterpret_cast<bf16_t*>(out), f);
 }
 
 // (bias vectors start at any float; those past the last column are zeros)
@@ -182,37 +204,33 @@ __device__ __forceinline__ void load_bias(const GemmEpilogue& e, int col, int n,
   for (int i = 0; i < NV; ++i) b[i] = 0.f;
   if constexpr (KIND == kGemmFwd) {
     if (e.bias == nullptr) return;
-    if (NV > 1 && col + NV <= n) load_cols<NV, false>(e.bias + col, b);
-    else {
 #pragma unroll
-      for (int i = 0; i < NV; ++i)
-        if (col + i < n) b[i] = e.bias[col + i];
-    }
+    for (int i = 0; i < NV; ++i)
+      if (col + i < n) b[i] = e.bias[col + i];
   }
 }
 
-// Eight columns, of which `cols` are left in the row (rows that are not whole vectors): a whole vector
-// as one, the last of a row by elements.
-template <int KIND>
+// NV columns, of which `cols` are left in the row (rows that are not whole vectors): a whole vector as
+// one, the last of a row by elements.
+template <int KIND, int NV>
 __device__ __forceinline__ void finish_any(const GemmEpilogue& e, const EpiloguePtr& p, uint32_t r, uint32_t c, int cols,
-                                           float (&f)[8], const float (&bias)[8]) {
-  if (cols >= 8) {
-    Aux<8> x;
-    load_aux<8, false>(p, r, c, x);
-    finish_cols<KIND, 8, false>(e, p, r, c, f, bias, x);
+                                           float (&f)[NV], const float (&bias)[NV]) {
+  Aux x;
+  if (cols >= NV) {
+    load_aux<NV, false>(p, r, c, x);
+    finish_cols<KIND, NV, false>(e, p, r, c, f, bias, x);
     return;
   }
-  float rest[8];
+  float rest[NV];
 #pragma unroll
-  for (int j = 0; j < 8; ++j) rest[j] = bias[j];
+  for (int j = 0; j < NV; ++j) rest[j] = bias[j];
 #pragma unroll 1
   for (int i = 0; i < cols; ++i) {  // (registers shift down: none is indexed by a variable)
     float g[1] = {f[0]}, b[1] = {rest[0]};
-    Aux<1> x;
     load_aux<1>(p, r, c + i, x);
     finish_cols<KIND, 1>(e, p, r, c + i, g, b, x);
 #pragma unroll
-    for (int j = 0; j < 7; ++j) {
+    for (int j = 0; j < NV - 1; ++j) {
       f[j] = f[j + 1];
       rest[j] = rest[j + 1];
     }

@@ -47,7 +47,7 @@ __global__ __launch_bounds__(NW * 64) void linear_rows_kernel(GemmArgs a) {
   const int oc = n0 + (tid & 15), orow = tid >> 4;
   const bool mine = orow < M && oc < a.n;
   float bias[1];
-  Aux<1> aux;
+  Aux aux;
   load_bias<kGemmFwd, 1>(a.e, oc, a.n, bias);
   const EpiloguePtr ep = epilogue_at<kGemmFwd>(a.e, 0, n0);
   if (mine) load_aux<1>(ep, orow, tid & 15, aux);
