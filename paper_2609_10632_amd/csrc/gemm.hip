@@ -188,10 +188,15 @@ __global__ __launch_bounds__(C::NW * 64) void gemm_kernel(GemmArgs a) {
   // before anything else, so that it is there when the sums are (and these loads, the oldest, disturb
   // no count of those in flight).
   constexpr int JS = C::OW / 32, STRIPS = TN / JS * TM;
-  constexpr int XB = STRIPS <= 2 ? STRIPS : 2, AHEAD = XB == STRIPS ? STRIPS : 1;
+  static_assert(TN == JS, "a lane's columns are the same in every strip");
+  // strips loaded ahead: all of two, one of more, and of fp32 operands, which take twice the
+  // registers, then none
+  constexpr auto ahead = [](int nv) { return STRIPS <= 2 ? STRIPS : nv == 8 ? 1 : 0; };
+  constexpr auto buffers = [](int nv) { return STRIPS <= 2 ? STRIPS : nv == 8 ? 2 : 1; };
   const EpiloguePtr ep = epilogue_at<KIND>(a.e, m0, n0);
   const int rows = (int)(a.m - m0 < BM ? a.m - m0 : BM), cols = a.n - n0;  // of the tile
-  Aux x[XB][C::OW / (KIND == kGemmDgrad ? 16 : 8)];
+  Aux x[STRIPS <= 2 && KIND != kGemmDgrad ? STRIPS * (C::OW / 8) : 2 * (C::OW / 16)];
+  float bias[8];
   // row, column and passes of a strip with NV columns a lane
   auto row_of = [&](int s, int nv) __attribute__((always_inline)) { return (wm * TM + s % TM) * 32 + lane / (C::OW / nv); };
   auto col_of = [&](int s, int nv) __attribute__((always_inline)) {
@@ -203,7 +208,7 @@ __global__ __launch_bounds__(C::NW * 64) void gemm_kernel(GemmArgs a) {
 #pragma unroll
     for (int p = 0; p < 32 / RPP; ++p) {
       const int r = row_of(s, NV) + p * RPP;
-      if (r < rows && c < cols) load_aux<NV>(ep, r, c, x[s % XB][p]);
+      if (r < rows && c < cols) load_aux<NV>(ep, r, c, x[s % buffers(NV) * (32 / RPP) + p]);
     }
   };
   // f(columns a lane): 8 or 4 by the type of the results
@@ -213,9 +218,11 @@ __global__ __launch_bounds__(C::NW * 64) void gemm_kernel(GemmArgs a) {
     else if (ep.out_f32) f(Ic<4>{});
     else f(Ic<8>{});
   };
-  if (a.splits == 1 && a.e.vec)
+  if (a.splits == 1)
     by_type([&](auto nvc) __attribute__((always_inline)) {
-      static_for<0, AHEAD>([&](auto sc) __attribute__((always_inline)) { fetch(nvc, sc); });
+      constexpr int NV = decltype(nvc)::value;
+      load_bias<KIND, NV>(a.e, n0 + col_of(0, NV), a.n, bias);
+      if (a.e.vec) static_for<0, ahead(NV)>([&](auto sc) __attribute__((always_inline)) { fetch(nvc, sc); });
     });
 
   Operand<TA, BM, BK, NW, C::AI> oa;
@@ -348,8 +355,8 @@ __global__ __launch_bounds__(C::NW * 64) void gemm_kernel(GemmArgs a) {
         const int r = row_of(s, 4) + p * RPP;
         float f[4];
         take(p, f);
-        // (the partials' rows are padded to whole vectors)
-        if (r < rows && c < cols) store_cols<4>(part + (int64_t)r * a.ldp + c, f);
+        // (the partials' rows are padded to whole lines)
+        if (r < rows && c < cols) store_cols<4, kStoreStream>(part + (int64_t)r * a.ldp + c, f);
       }
       __builtin_amdgcn_wave_barrier();
     });
@@ -357,29 +364,32 @@ __global__ __launch_bounds__(C::NW * 64) void gemm_kernel(GemmArgs a) {
   }
   by_type([&](auto nvc) __attribute__((always_inline)) {
     constexpr int NV = decltype(nvc)::value, RPP = 64 * NV / C::OW;
-    float bias[NV];
-    if (a.e.vec) {
-      // the next strip's auxiliary loads are in flight while a strip is finished
+    // the next strip's auxiliary loads are in flight while a strip is finished
+    auto vectors = [&](auto howc) __attribute__((always_inline)) {
       static_for<0, STRIPS>([&](auto sc) __attribute__((always_inline)) {
         constexpr int s = decltype(sc)::value;
         const int c = col_of(s, NV);
-        if constexpr (s % TM == 0) load_bias<KIND, NV>(a.e, n0 + c, a.n, bias);
-        if constexpr (s + AHEAD < STRIPS) fetch(nvc, Ic<s + AHEAD>{});
+        if constexpr (s + ahead(NV) < STRIPS) fetch(nvc, Ic<s + ahead(NV)>{});
         put(sc);
 #pragma unroll
         for (int p = 0; p < 32 / RPP; ++p) {
           const int r = row_of(s, NV) + p * RPP;
           float f[NV];
           take(p, f);
-          if (r < rows && c < cols) finish_cols<KIND, NV>(a.e, ep, r, c, f, bias, x[s % XB][p]);
+          if (r < rows && c < cols)
+            finish_cols<KIND, NV, decltype(howc)::value>(a.e, ep, r, c, f, bias, x[s % buffers(NV) * (32 / RPP) + p]);
         }
         __builtin_amdgcn_wave_barrier();
       });
+    };
+    if (a.e.vec && ep.stream) {
+      vectors(Ic<kStoreStream>{});
+    } else if (a.e.vec) {
+      vectors(Ic<kStoreVec>{});
     } else {
       static_for<0, STRIPS>([&](auto sc) __attribute__((always_inline)) {
         constexpr int s = decltype(sc)::value;
         const int c = col_of(s, NV);
-        if constexpr (s % TM == 0) load_bias<KIND, NV>(a.e, n0 + c, a.n, bias);
         put(sc);
 #pragma unroll 1
         for (int p = 0; p < 32 / RPP; ++p) {
@@ -629,7 +639,7 @@ GemmPlan gemm_pick(GemmKind kind, int64_t m, int n, int64_t k, int out_bytes) {
 bool gemm_any_rows(const GemmPlan& p) { return p.tile == kTileRows; }
 
 size_t gemm_part_bytes(const GemmPlan& p, int64_t m, int n) {
-  return p.splits > 1 ? (size_t)p.splits * (size_t)m * ((n + 7) / 8 * 8) * sizeof(float) : 0;
+  return p.splits > 1 ? (size_t)p.splits * (size_t)m * ((n + 31) / 32 * 32) * sizeof(float) : 0;
 }
 
 hipError_t gemm_launch(GemmKind kind, GemmArgs a, const GemmPlan& p, hipStream_t s) {
@@ -642,7 +652,7 @@ hipError_t gemm_launch(GemmKind kind, GemmArgs a, const GemmPlan& p, hipStream_t
   a.div_group = make_fastdiv(8u * (uint32_t)a.tiles_n);
   a.div_last = make_fastdiv(a.tiles_m % 8 ? a.tiles_m % 8 : 8);
   a.k_per_split = p.k_per_split;
-  a.ldp = (a.n + 7) / 8 * 8;
+  a.ldp = (a.n + 31) / 32 * 32;
   return kind == kGemmFwd     ? launch_kind<kGemmFwd>(a, p.tile, s)
          : kind == kGemmDgrad ? launch_kind<kGemmDgrad>(a, p.tile, s)
                               : launch_kind<kGemmWgrad>(a, p.tile, s);

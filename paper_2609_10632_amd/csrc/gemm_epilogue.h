@@ -20,17 +20,19 @@ __device__ __forceinline__ uint4 load16(const void* p) {
   const AnyVec v = *static_cast<const AnyVec*>(p);
   return make_uint4(v.u[0], v.u[1], v.u[2], v.u[3]);
 }
-template <bool ALIGNED>
+// how results are stored: at any address, in 16-byte vectors, or in those past the caches (see
+// EpiloguePtr)
+enum { kStoreAny, kStoreVec, kStoreStream };
+template <int HOW>
 __device__ __forceinline__ void store16(void* p, u32x4 v) {
-  if constexpr (ALIGNED) __builtin_nontemporal_store(v, static_cast<u32x4*>(p));
-  else *static_cast<AnyVec*>(p) = AnyVec{{v.x, v.y, v.z, v.w}};
+  if constexpr (HOW == kStoreAny) *static_cast<AnyVec*>(p) = AnyVec{{v.x, v.y, v.z, v.w}};
+  else if constexpr (HOW == kStoreStream) __builtin_nontemporal_store(v, static_cast<u32x4*>(p));
+  else *static_cast<u32x4*>(p) = v;
 }
 
 struct __attribute__((packed, aligned(2))) AnyHalf {
   uint32_t u[2];
 };
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-
 // NV consecutive columns: 8 or 4 of bf16, 4 of fp32 (16 bytes a lane, so that neighbouring lanes'
 // accesses join to whole lines), or 1
 template <int NV, bool ALIGNED = true>
@@ -60,22 +62,20 @@ __device__ __forceinline__ void load_cols(const float* p, float (&f)[NV]) {
     f[0] = *p;
   }
 }
-template <int NV, bool ALIGNED = true>
+template <int NV, int HOW = kStoreVec>
 __device__ __forceinline__ void store_cols(bf16_t* p, const float (&f)[NV]) {
   if constexpr (NV == 8) {
     const uint4 v = pack8(f);
-    store16<ALIGNED>(p, u32x4{v.x, v.y, v.z, v.w});
+    store16<HOW>(p, u32x4{v.x, v.y, v.z, v.w});
   } else if constexpr (NV == 4) {
-    const u32x2 v = {pack2(f[0], f[1]), pack2(f[2], f[3])};
-    if constexpr (ALIGNED) __builtin_nontemporal_store(v, reinterpret_cast<u32x2*>(p));
-    else *reinterpret_cast<AnyHalf*>(p) = AnyHalf{{v.x, v.y}};
+    *reinterpret_cast<AnyHalf*>(p) = AnyHalf{{pack2(f[0], f[1]), pack2(f[2], f[3])}};
   } else {
     *p = (bf16_t)f2bf(f[0]);
   }
 }
-template <int NV, bool ALIGNED = true>
+template <int NV, int HOW = kStoreVec>
 __device__ __forceinline__ void store_cols(float* p, const float (&f)[NV]) {
-  if constexpr (NV == 4) store16<ALIGNED>(p, __builtin_bit_cast(u32x4, f32x4{f[0], f[1], f[2], f[3]}));
+  if constexpr (NV == 4) store16<HOW>(p, __builtin_bit_cast(u32x4, f32x4{f[0], f[1], f[2], f[3]}));
   else if constexpr (NV == 1) *p = f[0];
 }
 
@@ -92,6 +92,11 @@ struct EpiloguePtr {
   const char* aux;            // nullptr: none
   uint32_t ldo, ldz, ldx;     // bytes between rows
   bool out_f32, aux_f32;
+  // Whether results go past the caches: they are written once and read by a later kernel, and 102400 x
+  // 192 -> 768 with z takes 84 us so against 111.  Only where rows are whole 128-byte lines: elsewhere
+  // neighbouring tiles write parts of the same lines, which the L2 then joins (24 x 11576 x 6712's fp32
+  // gradient 56 us against 133).
+  bool stream;
 };
 template <int KIND>
 __device__ __forceinline__ EpiloguePtr epilogue_at(const GemmEpilogue& e, int64_t row, int64_t col) {
@@ -108,6 +113,7 @@ __device__ __forceinline__ EpiloguePtr epilogue_at(const GemmEpilogue& e, int64_
   p.ldx = (uint32_t)ldx * sx;
   p.out = static_cast<char*>(e.out) + (row * e.ldo + col) * so;
   p.z = KIND == kGemmFwd && e.z != nullptr ? reinterpret_cast<char*>(e.z + row * e.ldz + col) : nullptr;
+  p.stream = (((uint32_t)(uintptr_t)e.out | p.ldo | (p.z != nullptr ? (uint32_t)(uintptr_t)e.z | p.ldz : 0)) & 127u) == 0;
   p.aux = aux != nullptr ? static_cast<const char*>(aux) + (row * ldx + col) * sx : nullptr;
   return p;
 }
@@ -152,14 +158,14 @@ __device__ __forceinline__ void each(float (&f)[NV], F&& fn) {
 }
 
 // f: the sums; bias: those of the columns; x: loaded by load_aux
-template <int KIND, int NV, bool ALIGNED = true>
+template <int KIND, int NV, int HOW = kStoreVec>
 __device__ __forceinline__ void finish_cols(const GemmEpilogue& e, const EpiloguePtr& p, uint32_t r, uint32_t c,
-                                            float (&f)[NV], const float (&bias)[NV], const Aux& x) {
+                                            float (&f)[NV], const float* bias, const Aux& x) {
   float o[NV];
   char* out = p.out + (uint32_t)(r * p.ldo + c * (p.out_f32 ? 4 : 2));
   if constexpr (KIND == kGemmFwd) {
     each(f, [&](int i) { return f[i] + bias[i]; });
-    if (p.z != nullptr) store_cols<NV, ALIGNED>(reinterpret_cast<bf16_t*>(p.z + (uint32_t)(r * p.ldz + c * 2)), f);
+    if (p.z != nullptr) store_cols<NV, HOW>(reinterpret_cast<bf16_t*>(p.z + (uint32_t)(r * p.ldz + c * 2)), f);
     // (one branch for the vector, not one per element)
     switch (e.act) {
       case kActRelu: each(f, [&](int i) { return act_apply(f[i], kActRelu); }); break;
@@ -182,7 +188,7 @@ __device__ __forceinline__ void finish_cols(const GemmEpilogue& e, const Epilogu
       default: break;
     }
     if (e.accumulate) {
-      load_cols<NV, ALIGNED>(reinterpret_cast<const bf16_t*>(out), o);
+      load_cols<NV, HOW != kStoreAny>(reinterpret_cast<const bf16_t*>(out), o);
       each(f, [&](int i) { return f[i] + o[i]; });
     }
   } else {
@@ -192,21 +198,32 @@ __device__ __forceinline__ void finish_cols(const GemmEpilogue& e, const Epilogu
     }
   }
   if constexpr (NV != 8) {  // (fp32 results never come in eights)
-    if (p.out_f32) return store_cols<NV, ALIGNED>(reinterpret_cast<float*>(out), f);
+    if (p.out_f32) return store_cols<NV, HOW>(reinterpret_cast<float*>(out), f);
   }
-  if constexpr (KIND != kGemmWgrad) store_cols<NV, ALIGNED>(reinterpret_cast<bf16_t*>(out), f);
+  if constexpr (KIND != kGemmWgrad) store_cols<NV, HOW>(reinterpret_cast<bf16_t*>(out), f);
 }
 
-// (bias vectors start at any float; those past the last column are zeros)
+// the bias of NV columns from col (it may start at any float; zeros past the last column)
 template <int KIND, int NV>
-__device__ __forceinline__ void load_bias(const GemmEpilogue& e, int col, int n, float (&b)[NV]) {
+__device__ __forceinline__ void load_bias(const GemmEpilogue& e, int col, int n, float* b) {
 #pragma unroll
   for (int i = 0; i < NV; ++i) b[i] = 0.f;
   if constexpr (KIND == kGemmFwd) {
     if (e.bias == nullptr) return;
+    if (NV >= 4 && col + NV <= n) {
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
-      if (col + i < n) b[i] = e.bias[col + i];
+      for (int i = 0; i < NV / 4; ++i) {
+        const uint4 v = load16<false>(e.bias + col + 4 * i);
+        b[4 * i] = __uint_as_float(v.x);
+        b[4 * i + 1] = __uint_as_float(v.y);
+        b[4 * i + 2] = __uint_as_float(v.z);
+        b[4 * i + 3] = __uint_as_float(v.w);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+        if (col + i < n) b[i] = e.bias[col + i];
+    }
   }
 }
 
@@ -214,11 +231,11 @@ __device__ __forceinline__ void load_bias(const GemmEpilogue& e, int col, int n,
 // one, the last of a row by elements.
 template <int KIND, int NV>
 __device__ __forceinline__ void finish_any(const GemmEpilogue& e, const EpiloguePtr& p, uint32_t r, uint32_t c, int cols,
-                                           float (&f)[NV], const float (&bias)[NV]) {
+                                           float (&f)[NV], const float* bias) {
   Aux x;
   if (cols >= NV) {
     load_aux<NV, false>(p, r, c, x);
-    finish_cols<KIND, NV, false>(e, p, r, c, f, bias, x);
+    finish_cols<KIND, NV, kStoreAny>(e, p, r, c, f, bias, x);
     return;
   }
   float rest[NV];
