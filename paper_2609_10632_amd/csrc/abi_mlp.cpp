@@ -79,11 +79,11 @@ size_t place(size_t* at, size_t bytes) {
   return here;
 }
 
-Product::Op operand(int64_t rows, int32_t cols, int64_t ld, bool any, size_t* at) {
-  Product::Op o{rows, cols, ld, !any && (cols % 8 != 0 || ld % 8 != 0), (int64_t)round_up((size_t)cols, 8), 0};
-  if (o.pack) o.at = place(at, (size_t)rows * o.ldp * sizeof(bf16_t));
-  return o;
+// pack: its rows are not whole aligned vectors
+Product::Op operand(int64_t rows, int32_t cols, int64_t ld) {
+  return Product::Op{rows, cols, ld, cols % 8 != 0 || ld % 8 != 0, (int64_t)round_up((size_t)cols, 8), 0};
 }
+double pack_bytes(const Product::Op& o) { return o.pack ? (double)o.rows * o.ldp * sizeof(bf16_t) : 0.0; }
 
 Product product(const LinearDesc& d, GemmKind kind) {
   Product p;
@@ -94,13 +94,17 @@ Product product(const LinearDesc& d, GemmKind kind) {
   if (kind == kGemmFwd) p.m = d.m, p.n = d.n, p.k = d.k;
   else if (kind == kGemmDgrad) p.m = d.m, p.n = d.k, p.k = d.n;
   else p.m = d.n, p.n = d.k, p.k = d.m;
+  p.a = kind == kGemmFwd ? operand(d.m, d.k, d.ldx) : operand(d.m, d.n, d.ldy);
+  p.b = kind == kGemmWgrad ? operand(d.m, d.k, d.ldx) : operand(d.n, d.k, d.k);
   // (the workspace depends on the problem alone, so that z is kept and read where there is an
   // activation is taken for granted here)
   const int z = d.act != NUMBAT_ACT_NONE ? 2 : 0;
-  p.plan = gemm_pick(kind, p.m, p.n, p.k, kind == kGemmFwd ? (d.y_f32 ? 4 : 2) + z : kind == kGemmDgrad ? 2 + z : 4);
-  const bool any = gemm_any_rows(p.plan);
-  p.a = kind == kGemmFwd ? operand(d.m, d.k, d.ldx, any, &at) : operand(d.m, d.n, d.ldy, any, &at);
-  p.b = kind == kGemmWgrad ? operand(d.m, d.k, d.ldx, any, &at) : operand(d.n, d.k, d.k, any, &at);
+  p.plan = gemm_pick(kind, p.m, p.n, p.k, kind == kGemmFwd ? (d.y_f32 ? 4 : 2) + z : kind == kGemmDgrad ? 2 + z : 4,
+                     pack_bytes(p.a) + pack_bytes(p.b));
+  for (Product::Op* o : {&p.a, &p.b}) {
+    o->pack = o->pack && !gemm_any_rows(p.plan);
+    if (o->pack) o->at = place(&at, (size_t)pack_bytes(*o));
+  }
   p.part_at = place(&at, gemm_part_bytes(p.plan, p.m, p.n));
   if (kind == kGemmWgrad) p.extra_at = place(&at, colsum_part_bytes(d.m, d.n));
   p.bytes = at;

@@ -48,8 +48,10 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t rsrc(const void* base) {
 }
 
 // ---------------------------------------------------------------------------
-template <int BM_, int BN_, int BK_, int S_, int WM_, int WN_>
+// ANY_: operands' rows may start at any element (they pass through registers to LDS)
+template <int BM_, int BN_, int BK_, int S_, int WM_, int WN_, bool ANY_ = false>
 struct Tile {
+  static constexpr bool ANY = ANY_;
   static constexpr int BM = BM_, BN = BN_, BK = BK_, S = S_, WM = WM_, WN = WN_, NW = WM * WN;
   static constexpr int TM = BM / WM / 32, TN = BN / WN / 32;   // 32 x 32 blocks per wave
   static constexpr int A_BYTES = BM * BK * 2, B_BYTES = BN * BK * 2, STAGE = A_BYTES + B_BYTES;
@@ -63,6 +65,7 @@ struct Tile {
   static_assert(WPS * OUT_BYTES <= STAGE, "the epilogue fits the stages");
   static_assert(KS % 2 == 0 && S >= 2 && S <= 4, "two fragment buffers, 2 to 4 stages");
   static_assert(TN == 1 || TN % 2 == 0, "whole staging strips");
+  static_assert(!ANY || S == 2, "two stages, two steps in registers");
 };
 
 // An operand tile of SIDE rows of C (or columns) by BK of the reduction, as LDS holds it.
@@ -109,6 +112,60 @@ struct Operand {
   __device__ __forceinline__ void load(unsigned char* stage, int q, int64_t left, int wave) const {
     const uint32_t vo = kpos[T ? q : 0] < left ? off[q] : kOob;
     __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc(base), (lds_void_t*)(stage + (q * NW + wave) * 1024), 16, vo, 0, 0, 0);
+  }
+};
+
+// The same tile from rows that start at any element: unaligned 16-byte loads into registers, two steps
+// ahead, and 16-byte writes into LDS.  A vector that the row or the reduction ends in is read by
+// elements, the rest of it zero.
+template <bool T, int SIDE, int BK, int NW, int NI>
+struct OperandAny {
+  using Op = Operand<T, SIDE, BK, NW, NI>;
+  const unsigned char* base;
+  int64_t step;
+  uint32_t off[NI];
+  int kpos[T ? NI : 1];
+  int whole[NI];  // elements of the lane's vector inside the matrix: T: columns left; else 8 or 0 by the row
+  uint4 v[2][NI];
+
+  __device__ __forceinline__ void init(const bf16_t* p, int64_t ld, int64_t r0, int64_t rows, int64_t k0, int wave,
+                                       int lane) {
+    base = reinterpret_cast<const unsigned char*>(T ? p + k0 * ld + r0 : p + r0 * ld + k0);
+    step = T ? 2 * BK * ld : 2 * BK;
+#pragma unroll
+    for (int q = 0; q < NI; ++q) {
+      const int byte = (q * NW + wave) * 1024 + lane * 16;
+      if constexpr (!T) {
+        const int row = byte / (2 * BK), chunk = (byte % (2 * BK)) / 16 ^ (row / Op::WIN % Op::CPR);
+        kpos[0] = chunk * 8;  // the same for every q: NW is even
+        off[q] = (uint32_t)(row * ld * 2) + chunk * 16;
+        whole[q] = r0 + row < rows ? 8 : 0;
+      } else {
+        const int row = byte / (2 * SIDE), chunk = (byte % (2 * SIDE)) / 16 ^ Op::swz(row);
+        const int64_t have = rows - r0 - chunk * 8;
+        kpos[q] = row;
+        off[q] = (uint32_t)(row * ld * 2) + chunk * 16;
+        whole[q] = have < 8 ? (have > 0 ? (int)have : 0) : 8;
+      }
+    }
+  }
+  __device__ __forceinline__ void load(int b, int q, int64_t left) {
+    const int64_t kleft = left - kpos[T ? q : 0];
+    const int count = T ? (kleft > 0 ? whole[q] : 0) : (kleft < whole[q] ? (int)kleft : whole[q]);
+    v[b][q] = make_uint4(0, 0, 0, 0);
+    const bf16_t* p = reinterpret_cast<const bf16_t*>(base + off[q]);
+    if (count >= 8) {
+      v[b][q] = load16<false>(p);
+    } else if (count > 0) {
+      uint32_t h[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) h[e] = e < count ? p[e] : 0;
+      v[b][q] = make_uint4(h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16);
+    }
+  }
+  __device__ __forceinline__ void put(unsigned char* stage, int b, int wave, int lane) const {
+#pragma unroll
+    for (int q = 0; q < NI; ++q) *reinterpret_cast<uint4*>(stage + (q * NW + wave) * 1024 + lane * 16) = v[b][q];
   }
 };
 
@@ -225,16 +282,27 @@ __global__ __launch_bounds__(C::NW * 64) void gemm_kernel(GemmArgs a) {
       if (a.e.vec) static_for<0, ahead(NV)>([&](auto sc) __attribute__((always_inline)) { fetch(nvc, sc); });
     });
 
-  Operand<TA, BM, BK, NW, C::AI> oa;
-  Operand<TB, BN, BK, NW, C::BI> ob;
+  std::conditional_t<C::ANY, OperandAny<TA, BM, BK, NW, C::AI>, Operand<TA, BM, BK, NW, C::AI>> oa;
+  std::conditional_t<C::ANY, OperandAny<TB, BN, BK, NW, C::BI>, Operand<TB, BN, BK, NW, C::BI>> ob;
   oa.init(a.a, a.lda, m0, a.m, k0, wave, lane);
   ob.init(a.b, a.ldb, n0, a.n, k0, wave, lane);
   // load instruction q of the step that `left` counts, A's first
   constexpr int L = C::AI + C::BI;
   auto load = [&](auto uc, int q) __attribute__((always_inline)) {
-    unsigned char* st = stage(uc);
-    if (q < C::AI) oa.load(st, q, left, wave);
-    else ob.load(st + C::A_BYTES, q - C::AI, left, wave);
+    if constexpr (C::ANY) {  // (into the registers of that parity)
+      if (q < C::AI) oa.load(decltype(uc)::value, q, left);
+      else ob.load(decltype(uc)::value, q - C::AI, left);
+    } else {
+      unsigned char* st = stage(uc);
+      if (q < C::AI) oa.load(st, q, left, wave);
+      else ob.load(st + C::A_BYTES, q - C::AI, left, wave);
+    }
+  };
+  auto put_stage = [&](auto uc) __attribute__((always_inline)) {
+    if constexpr (C::ANY) {
+      oa.put(stage(uc), decltype(uc)::value, wave, lane);
+      ob.put(stage(uc) + C::A_BYTES, decltype(uc)::value, wave, lane);
+    }
   };
   auto advance = [&]() __attribute__((always_inline)) {
     oa.base += oa.step;
@@ -289,9 +357,13 @@ __global__ __launch_bounds__(C::NW * 64) void gemm_kernel(GemmArgs a) {
   // have landed (those of later steps stay in flight); past the barrier that holds for every wave,
   // so the last slice can read the next stage.
   constexpr int PENDING = S == 2 ? 0 : (S - 3) * L + (KS - 1) * L / KS;
+  // (ANY: step kt + 1 goes from its registers to LDS first, and step kt + 3 is loaded into them)
   auto step = [&](auto uc) __attribute__((always_inline)) {
+    constexpr int u = decltype(uc)::value;
+    put_stage(Ic<(u + 1) % S>{});
     static_for<0, KS - 1>([&](auto kc) __attribute__((always_inline)) { slice(uc, kc); });
-    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(PENDING) : "memory");
+    if constexpr (C::ANY) __syncthreads();
+    else asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(PENDING) : "memory");
     slice(uc, Ic<KS - 1>{});
     advance();
   };
@@ -300,7 +372,18 @@ __global__ __launch_bounds__(C::NW * 64) void gemm_kernel(GemmArgs a) {
     for (int q = 0; q < L; ++q) load(uc, q);
     advance();
   });
-  asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((S - 2) * L) : "memory");
+  if constexpr (C::ANY) {
+#pragma unroll
+    for (int q = 0; q < L; ++q) load(Ic<1>{}, q);
+    advance();
+    put_stage(Ic<0>{});
+#pragma unroll
+    for (int q = 0; q < L; ++q) load(Ic<0>{}, q);
+    advance();
+    __syncthreads();
+  } else {
+    asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((S - 2) * L) : "memory");
+  }
 #pragma unroll
   for (int r = 0; r < TM + TN; ++r) rd(Ic<0>{}, r, 0, 0);
   int kt = 0;
@@ -465,12 +548,13 @@ __global__ __launch_bounds__(256) void gemm_pack_kernel(GemmPack a, GemmPack b) 
   }
 }
 
-// Bias gradient: a block sums a range of rows of 512 columns, a wave every fourth row of it with 8
-// columns per lane and four rows' loads in flight; colsum_finish adds the blocks' sums.
+// Bias gradient: a block of 16 waves sums a range of rows of 512 columns, a wave every sixteenth row of
+// it with 8 columns per lane and four rows' loads in flight.  One range is the result, several are
+// partials for column_sum_kernel.
 template <bool VEC>
-__global__ __launch_bounds__(256) void colsum_part_kernel(const bf16_t* src, int64_t lds, int64_t rows, int cols,
-                                                          int64_t rows_per, float* part) {
-  __shared__ float s_sum[4][512];
+__global__ __launch_bounds__(1024) void colsum_kernel(const bf16_t* src, int64_t lds, int64_t rows, int cols,
+                                                      int64_t rows_per, float* out, int accumulate) {
+  __shared__ float s_sum[16][512];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = blockIdx.x * 512 + lane * 8;
   const int64_t r0 = blockIdx.y * rows_per, r1 = r0 + rows_per < rows ? r0 + rows_per : rows;
   float s[8] = {};
@@ -482,7 +566,7 @@ __global__ __launch_bounds__(256) void colsum_part_kernel(const bf16_t* src, int
   };
   auto get = [&](int64_t r) __attribute__((always_inline)) -> uint4 {
     const bf16_t* p = src + r * lds + c;
-    if constexpr (VEC) return *reinterpret_cast<const uint4*>(p);
+    if (VEC || c + 8 <= cols) return load16<VEC>(p);
     uint32_t h[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) h[e] = c + e < cols ? p[e] : 0;
@@ -490,49 +574,67 @@ __global__ __launch_bounds__(256) void colsum_part_kernel(const bf16_t* src, int
   };
   if (c < cols) {
     int64_t r = r0 + wave;
-    for (; r + 12 < r1; r += 16) {
-      const uint4 v0 = get(r), v1 = get(r + 4), v2 = get(r + 8), v3 = get(r + 12);
+    for (; r + 48 < r1; r += 64) {
+      const uint4 v0 = get(r), v1 = get(r + 16), v2 = get(r + 32), v3 = get(r + 48);
       add(v0);
       add(v1);
       add(v2);
       add(v3);
     }
-    for (; r < r1; r += 4) add(get(r));
+    for (; r < r1; r += 16) add(get(r));
   }
 #pragma unroll
   for (int e = 0; e < 8; ++e) s_sum[wave][lane * 8 + e] = s[e];
   __syncthreads();
-  for (int i = threadIdx.x; i < 512; i += 256) {
-    const int col = blockIdx.x * 512 + i;
-    if (col < cols) part[(int64_t)blockIdx.y * cols + col] = (s_sum[0][i] + s_sum[1][i]) + (s_sum[2][i] + s_sum[3][i]);
+  const int i = threadIdx.x, col = blockIdx.x * 512 + i;
+  if (i < 512 && col < cols) {
+    float t = s_sum[0][i];
+#pragma unroll
+    for (int w = 1; w < 16; ++w) t += s_sum[w][i];
+    float* o = out + (int64_t)blockIdx.y * cols + col;
+    *o = accumulate ? *o + t : t;
   }
 }
 
 // The sums of the columns of a [rows][ld] matrix of partials, in a fixed order: the first cols0 go to
-// out0, the others to out1 (each may be nullptr).  A block takes 64 columns, each of its 16 waves every
-// sixteenth row, eight loads in flight.
+// out0, the others to out1 (each may be nullptr).  A block takes CW columns; its waves' lanes in groups
+// of CW take every (1024 / CW)th row, eight loads in flight.  16 columns a block spread few columns
+// over more CUs (1024 x 384 partials 4.9 us with 64).
+template <int CW>
 __global__ __launch_bounds__(1024) void column_sum_kernel(const float* part, int rows, int64_t ld, int cols, int cols0,
                                                           float* out0, float* out1, int accumulate) {
-  __shared__ float s_sum[16][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = blockIdx.x * 64 + lane;
+  constexpr int G = 1024 / CW;
+  __shared__ float s_sum[G][CW + 1];
+  const int i = threadIdx.x % CW, g = threadIdx.x / CW, c = blockIdx.x * CW + i;
   float s = 0.f;
   if (c < cols) {
-    int r = wave;
-    for (; r + 112 < rows; r += 128) {
+    int r = g;
+    for (; r + 7 * G < rows; r += 8 * G) {
       float v[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = part[(int64_t)(r + 16 * e) * ld + c];
+      for (int e = 0; e < 8; ++e) v[e] = part[(int64_t)(r + G * e) * ld + c];
 #pragma unroll
       for (int e = 0; e < 8; ++e) s += v[e];
     }
-    for (; r < rows; r += 16) s += part[(int64_t)r * ld + c];
+    for (; r < rows; r += G) s += part[(int64_t)r * ld + c];
   }
-  s_sum[wave][lane] = s;
+  s_sum[g][i] = s;
   __syncthreads();
-  if (wave == 0 && c < cols) {
-    s = s_sum[0][lane];
+  // 16 groups at a time, then the 16 (or fewer) sums of those
+  if (G > 16 && g < 16) {
+    s = s_sum[g][i];
 #pragma unroll
-    for (int w = 1; w < 16; ++w) s += s_sum[w][lane];
+    for (int k = 1; k < G / 16; ++k) s += s_sum[g + 16 * k][i];
+  }
+  if (G > 16) {
+    __syncthreads();
+    if (g < 16) s_sum[g][i] = s;
+    __syncthreads();
+  }
+  if (g == 0 && c < cols) {
+    s = s_sum[0][i];
+#pragma unroll
+    for (int w = 1; w < 16; ++w) s += s_sum[w][i];
     float* out = c < cols0 ? out0 : out1;
     if (out != nullptr) {
       out += c < cols0 ? c : c - cols0;
@@ -541,9 +643,10 @@ __global__ __launch_bounds__(1024) void column_sum_kernel(const float* part, int
   }
 }
 
-// ranges of rows: enough blocks for the chip, at least 32 rows each
+// ranges of rows: one of up to 256 rows, which needs no second launch, else enough blocks for the chip
 int64_t colsum_rows_per(int64_t rows, int cols) {
-  const int64_t ranges = std::max<int64_t>(1, std::min<int64_t>(2048 / ((cols + 511) / 512), (rows + 31) / 32));
+  const int64_t blocks = (cols + 511) / 512;
+  const int64_t ranges = rows <= 256 ? 1 : std::max<int64_t>(1, std::min<int64_t>((2048 + blocks - 1) / blocks, rows / 64));
   return (rows + ranges - 1) / ranges;
 }
 
@@ -558,8 +661,9 @@ using T128W = Tile<128, 256, 64, 3, 2, 4>;
 using T128D = Tile<128, 128, 64, 4, 2, 4>;
 using T128 = Tile<128, 128, 64, 2, 2, 4>;
 using T64 = Tile<64, 64, 64, 4, 2, 2>;
+using T64Any = Tile<64, 64, 64, 2, 2, 2, true>;
 
-enum { kTile256, kTile128W, kTile128D, kTile128, kTile64, kTileRows };
+enum { kTile256, kTile128W, kTile128D, kTile128, kTile64, kTile64Any, kTileRows };
 
 template <int KIND, typename C>
 hipError_t launch_tile(const GemmArgs& a, hipStream_t s) {
@@ -574,7 +678,8 @@ hipError_t launch_kind(const GemmArgs& a, int tile, hipStream_t s) {
                  : tile == kTile128W ? launch_tile<KIND, T128W>(a, s)
                  : tile == kTile128D ? launch_tile<KIND, T128D>(a, s)
                  : tile == kTile128  ? launch_tile<KIND, T128>(a, s)
-                                     : launch_tile<KIND, T64>(a, s);
+                 : tile == kTile64   ? launch_tile<KIND, T64>(a, s)
+                                     : launch_tile<KIND, T64Any>(a, s);
   trace_end(KC_LINEAR);
   if (e != hipSuccess || a.splits == 1) return e;
   trace_begin(KC_LINEAR_FINISH);
@@ -588,7 +693,7 @@ hipError_t launch_kind(const GemmArgs& a, int tile, hipStream_t s) {
 struct TileSize {
   int m, n;
 };
-constexpr TileSize kTiles[] = {{T256::BM, T256::BN}, {T128W::BM, T128W::BN}, {T128D::BM, T128D::BN}, {T128::BM, T128::BN}, {T64::BM, T64::BN}};
+constexpr TileSize kTiles[] = {{T256::BM, T256::BN}, {T128W::BM, T128W::BN}, {T128D::BM, T128D::BN}, {T128::BM, T128::BN}, {T64::BM, T64::BN}, {T64Any::BM, T64Any::BN}};
 int64_t tile_count(int tile, int64_t m, int n) {
   const TileSize t = kTiles[tile];
   return ((m + t.m - 1) / t.m) * ((n + t.n - 1) / t.n);
@@ -604,6 +709,8 @@ double tile_time(int tile, int64_t blocks, int64_t k, int out_bytes) {
     case kTile128D: return std::ceil(b / 256) * (1.2 + 0.65 * out_bytes + 0.0079 * k);
     case kTile128:
       return blocks <= 256 ? 3.0 + 0.0115 * k : std::max(1.0, b / 512 + 0.25) * (2.5 + 0.75 * out_bytes + 0.015 * k);
+    case kTile64Any:
+      return std::max(1.0, b / 1024 + 0.25) * (2.0 + 0.4 * out_bytes + (0.006 + 0.0045 * std::min(4.0, b / 256)) * k);
     default:
       return blocks <= 256 ? 2.5 + 0.0031 * k : std::max(1.0, b / 512 + 0.25) * (1.7 + 0.4 * out_bytes + 0.0058 * k);
   }
@@ -614,17 +721,18 @@ double finish_time(int splits, int64_t m, int n) { return splits == 1 ? 0.0 : 4.
 
 }  // namespace
 
-GemmPlan gemm_pick(GemmKind kind, int64_t m, int n, int64_t k, int out_bytes) {
+GemmPlan gemm_pick(GemmKind kind, int64_t m, int n, int64_t k, int out_bytes, double pack_bytes) {
   GemmPlan p{kTile64, 1, 0};
   if (kind == kGemmFwd && m <= kLinearRows) return GemmPlan{kTileRows, 1, k};
   const int64_t steps = (k + 63) / 64;
   double best = 1e30;
-  for (int tile = kTile256; tile <= kTile64; ++tile) {
+  for (int tile = kTile256; tile <= (pack_bytes > 0 ? kTile64Any : kTile64); ++tile) {
     const int64_t tiles = tile_count(tile, m, n);
+    const double pack = pack_bytes > 0 && tile != kTile64Any ? 3.5 + 2 * pack_bytes / 4e6 : 0.0;
     for (int s : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
       if (s > 1 && (steps / s < 4 || tiles * s > 1024)) break;
       const int64_t kps = (steps + s - 1) / s;
-      const double t = tile_time(tile, tiles * s, kps * 64, s > 1 ? 4 : out_bytes) + finish_time(s, m, n);
+      const double t = tile_time(tile, tiles * s, kps * 64, s > 1 ? 4 : out_bytes) + finish_time(s, m, n) + pack;
       if (t < best) {
         best = t;
         p.tile = tile;
@@ -636,7 +744,7 @@ GemmPlan gemm_pick(GemmKind kind, int64_t m, int n, int64_t k, int out_bytes) {
   return p;
 }
 
-bool gemm_any_rows(const GemmPlan& p) { return p.tile == kTileRows; }
+bool gemm_any_rows(const GemmPlan& p) { return p.tile == kTileRows || p.tile == kTile64Any; }
 
 size_t gemm_part_bytes(const GemmPlan& p, int64_t m, int n) {
   return p.splits > 1 ? (size_t)p.splits * (size_t)m * ((n + 31) / 32 * 32) * sizeof(float) : 0;
@@ -675,20 +783,26 @@ hipError_t colsum_launch(const bf16_t* src, int64_t lds, int64_t rows, int32_t c
   const int64_t per = colsum_rows_per(rows, cols);
   const unsigned ranges = (unsigned)((rows + per - 1) / per);
   const dim3 grid((unsigned)((cols + 511) / 512), ranges);
+  float* to = ranges == 1 ? out : part;
+  const int acc = ranges == 1 ? accumulate : 0;
   trace_begin(KC_LINEAR_BIAS_GRAD);
-  if (cols % 8 == 0 && lds % 8 == 0)
-    NUMBAT_LAUNCH(colsum_part_kernel<true>, grid, dim3(256), 0, s, src, lds, rows, cols, per, part);
-  else NUMBAT_LAUNCH(colsum_part_kernel<false>, grid, dim3(256), 0, s, src, lds, rows, cols, per, part);
+  if (cols % 8 == 0 && lds % 8 == 0) NUMBAT_LAUNCH(colsum_kernel<true>, grid, dim3(1024), 0, s, src, lds, rows, cols, per, to, acc);
+  else NUMBAT_LAUNCH(colsum_kernel<false>, grid, dim3(1024), 0, s, src, lds, rows, cols, per, to, acc);
   const hipError_t e = hipGetLastError();
-  if (e == hipSuccess) column_sum_launch(part, (int)ranges, cols, cols, cols, out, nullptr, accumulate, s);
+  if (e == hipSuccess && ranges > 1) column_sum_launch(part, (int)ranges, cols, cols, cols, out, nullptr, accumulate, s);
   trace_end(KC_LINEAR_BIAS_GRAD);
   return e != hipSuccess ? e : hipGetLastError();
 }
 
 void column_sum_launch(const float* part, int rows, int64_t ld, int cols, int cols0, float* out0, float* out1,
                        int accumulate, hipStream_t s) {
-  NUMBAT_LAUNCH(column_sum_kernel, dim3((unsigned)((cols + 63) / 64)), dim3(1024), 0, s, part, rows, ld, cols, cols0,
-                out0, out1, accumulate);
+  if (cols <= 4096) {
+    NUMBAT_LAUNCH(column_sum_kernel<16>, dim3((unsigned)((cols + 15) / 16)), dim3(1024), 0, s, part, rows, ld, cols, cols0,
+                  out0, out1, accumulate);
+  } else {
+    NUMBAT_LAUNCH(column_sum_kernel<64>, dim3((unsigned)((cols + 63) / 64)), dim3(1024), 0, s, part, rows, ld, cols, cols0,
+                  out0, out1, accumulate);
+  }
 }
 
 hipError_t fill_zero_launch(float* p, int64_t n, hipStream_t s) {

@@ -49,8 +49,9 @@ struct GemmPlan {
   int splits;
   int64_t k_per_split;
 };
-// out_bytes: what the epilogue reads and writes for each element
-GemmPlan gemm_pick(GemmKind kind, int64_t m, int n, int64_t k, int out_bytes);
+// out_bytes: what the epilogue reads and writes for each element; pack_bytes: size of the operands that
+// would have to be padded (0: none)
+GemmPlan gemm_pick(GemmKind kind, int64_t m, int n, int64_t k, int out_bytes, double pack_bytes);
 // whether the plan's kernel takes operands whose rows start at any element
 bool gemm_any_rows(const GemmPlan& p);
 size_t gemm_part_bytes(const GemmPlan& p, int64_t m, int n);

@@ -70,11 +70,11 @@ def test_linear_refusals(which):
         assert status_of(call, ok, **{arg: None}) == nb.ERR_NULL, arg
         if which != "weight" or arg != "y":
             assert status_of(call, ok, **{arg: P + 8}) == nb.ERR_ALIGN, arg
-    # operands with odd rows are padded in the workspace
+    # large operands with odd rows are padded in the workspace
     op = {"fwd": nb.OP_LINEAR_FWD, "data": nb.OP_LINEAR_BWD_DATA, "weight": nb.OP_LINEAR_BWD_WEIGHT}[which]
-    odd = nb.linear_problem(400, 17, 25)
+    odd = nb.linear_problem(20001, 2049, 1025)
     need = nb.numbat_workspace_size(op, odd)
-    assert need >= 256 + 400 * 24 * 2
+    assert need >= 256 + 20001 * 1032 * 2
     assert status_of(call, odd) == nb.ERR_WORKSPACE
     assert status_of(call, odd, ws=P, b=need - 1) == nb.ERR_WORKSPACE
     assert status_of(call, odd, ws=P + 4, b=need) == nb.ERR_ALIGN
