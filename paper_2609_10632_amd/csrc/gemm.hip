@@ -699,25 +699,29 @@ int64_t tile_count(int tile, int64_t m, int n) {
   return ((m + t.m - 1) / t.m) * ((n + t.n - 1) / t.n);
 }
 
-// What a product takes on a tile, in us, as measured: rounds of blocks over the 256 CUs, each a fixed
-// part (first loads, epilogue: out_bytes for each element of C) and a part per k.
-double tile_time(int tile, int64_t blocks, int64_t k, int out_bytes) {
-  const double b = (double)blocks;
+// What a product takes on a tile, in us, as measured: the blocks that fall to one of the 256 CUs (one,
+// two or four at a time), each a fixed part (first loads, epilogue: out_bytes for each element of C)
+// and a part per k.
+double tile_time(GemmKind kind, int tile, int64_t blocks, int64_t k, int out_bytes) {
+  // small tiles of operands that run across the reduction: twice the LDS reads, shorter rows
+  const double across = kind == kGemmFwd ? 1.0 : kind == kGemmDgrad ? 1.35 : tile == kTile64Any ? 2.0 : 1.4;
+  const double b = (double)blocks, per_cu = std::ceil(b / 256);
   switch (tile) {
-    case kTile256: return std::ceil(b / 256) * (1.5 + 2.75 * out_bytes + 0.0255 * k);
-    case kTile128W: return std::ceil(b / 256) * (1.4 + 1.5 * out_bytes + (blocks <= 256 ? 0.012 : 0.0135) * k);
-    case kTile128D: return std::ceil(b / 256) * (1.2 + 0.65 * out_bytes + 0.0079 * k);
+    case kTile256: return per_cu * (1.5 + 2.75 * out_bytes + 0.0255 * k);
+    case kTile128W: return per_cu * (1.4 + 1.5 * out_bytes + (blocks <= 256 ? 0.012 : 0.0135) * k);
+    case kTile128D: return per_cu * (1.2 + 0.65 * out_bytes + 0.0079 * k);
     case kTile128:
-      return blocks <= 256 ? 3.0 + 0.0115 * k : std::max(1.0, b / 512 + 0.25) * (2.5 + 0.75 * out_bytes + 0.015 * k);
+      return std::floor(per_cu / 2) * (2.5 + 0.75 * out_bytes + 0.015 * k) + std::fmod(per_cu, 2) * (3.0 + 0.0115 * k);
     case kTile64Any:
-      return std::max(1.0, b / 1024 + 0.25) * (2.0 + 0.4 * out_bytes + (0.006 + 0.0045 * std::min(4.0, b / 256)) * k);
+      return std::max(1.0, b / 1024 + 0.25) * (2.0 + 0.4 * out_bytes + (0.009 * across + 0.002 * std::min(4.0, b / 256)) * k);
     default:
-      return blocks <= 256 ? 2.5 + 0.0031 * k : std::max(1.0, b / 512 + 0.25) * (1.7 + 0.4 * out_bytes + 0.0058 * k);
+      return blocks <= 256 ? 2.5 + 0.0031 * across * k
+                           : std::max(1.0, b / 512 + 0.25) * (1.7 + 0.4 * out_bytes + 0.0058 * across * k);
   }
 }
 
 // and the second launch that adds the sums of the splits
-double finish_time(int splits, int64_t m, int n) { return splits == 1 ? 0.0 : 4.0 + 0.1 * splits + (double)splits * m * n * 8 / 4e6; }
+double finish_time(int splits, int64_t m, int n) { return splits == 1 ? 0.0 : 4.0 + 0.1 * splits + (double)splits * m * n * 8 / 6e6; }
 
 }  // namespace
 
@@ -732,7 +736,7 @@ GemmPlan gemm_pick(GemmKind kind, int64_t m, int n, int64_t k, int out_bytes, do
     for (int s : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
       if (s > 1 && (steps / s < 4 || tiles * s > 1024)) break;
       const int64_t kps = (steps + s - 1) / s;
-      const double t = tile_time(tile, tiles * s, kps * 64, s > 1 ? 4 : out_bytes) + finish_time(s, m, n) + pack;
+      const double t = tile_time(kind, tile, tiles * s, kps * 64, s > 1 ? 4 : out_bytes) + finish_time(s, m, n) + pack;
       if (t < best) {
         best = t;
         p.tile = tile;
