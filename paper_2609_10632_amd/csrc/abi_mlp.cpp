@@ -70,7 +70,8 @@ struct Product {
     size_t at;
   } a, b;
   GemmPlan plan;
-  size_t part_at, extra_at, bytes;  // extra: the bias gradient's partials
+  bool sums_rows;  // the bias gradient comes with the weight gradient
+  size_t part_at, db_at, bytes;  // db: the bias gradient's partials
 };
 
 size_t place(size_t* at, size_t bytes) {
@@ -106,7 +107,11 @@ Product product(const LinearDesc& d, GemmKind kind) {
     if (o->pack) o->at = place(&at, (size_t)pack_bytes(*o));
   }
   p.part_at = place(&at, gemm_part_bytes(p.plan, p.m, p.n));
-  if (kind == kGemmWgrad) p.extra_at = place(&at, colsum_part_bytes(d.m, d.n));
+  if (kind == kGemmWgrad) {
+    p.sums_rows = gemm_sums_rows(p.plan);
+    if (!p.sums_rows) p.db_at = place(&at, colsum_part_bytes(d.m, d.n));
+    else if (p.plan.splits > 1) p.db_at = place(&at, (size_t)p.plan.splits * (size_t)p.m * sizeof(float));
+  }
   p.bytes = at;
   return p;
 }
@@ -120,7 +125,7 @@ GemmPack packed(const Product::Op& o, const void* src, char* ws, const bf16_t** 
   return GemmPack{s, o.ld, o.pack ? o.rows : 0, o.cols, dst, o.ldp};
 }
 
-hipError_t run_product(const Product& p, const void* a, const void* b, const GemmEpilogue& e, void* ws,
+hipError_t run_product(const Product& p, const void* a, const void* b, const GemmEpilogue& e, float* db, void* ws,
                        hipStream_t s) {
   GemmArgs g;
   std::memset(&g, 0, sizeof g);
@@ -134,6 +139,8 @@ hipError_t run_product(const Product& p, const void* a, const void* b, const Gem
   g.n = p.n;
   g.k = p.k;
   g.part = reinterpret_cast<float*>(body + p.part_at);
+  g.db = db;
+  g.db_part = reinterpret_cast<float*>(body + p.db_at);
   g.e = e;
   return gemm_launch(p.kind, g, p.plan, s);
 }
@@ -230,7 +237,7 @@ numbat_status numbat_linear_fwd(const numbat_linear_problem* p, const void* x, c
   e.ldz = d.ldz;
   e.ldo = d.ldy;
   e.vec = d.n % 8 == 0 && d.ldy % 8 == 0 && (residual == nullptr || d.ldr % 8 == 0) && (z == nullptr || d.ldz % 8 == 0);
-  const hipError_t err = run_product(pr, x, w, e, ws_body(ws), static_cast<hipStream_t>(stream));
+  const hipError_t err = run_product(pr, x, w, e, nullptr, ws_body(ws), static_cast<hipStream_t>(stream));
   return err == hipSuccess ? ok() : hip_fail(err, "linear forward launch");
 }
 
@@ -257,7 +264,7 @@ numbat_status numbat_linear_bwd_data(const numbat_linear_problem* p, const void*
   e.ldz = d.ldz;
   e.ldo = d.ldx;
   e.vec = d.k % 8 == 0 && d.ldx % 8 == 0 && (d.act == NUMBAT_ACT_NONE || d.ldz % 8 == 0);
-  const hipError_t err = run_product(pr, dy, w, e, ws_body(ws), static_cast<hipStream_t>(stream));
+  const hipError_t err = run_product(pr, dy, w, e, nullptr, ws_body(ws), static_cast<hipStream_t>(stream));
   return err == hipSuccess ? ok() : hip_fail(err, "linear data gradient launch");
 }
 
@@ -286,10 +293,10 @@ numbat_status numbat_linear_bwd_weight(const numbat_linear_problem* p, const voi
   e.out = dw;
   e.ldo = d.k;
   e.vec = d.k % 8 == 0 && aligned16(dw);
-  err = run_product(pr, dy, x, e, ws_body(ws), s);
-  if (err == hipSuccess && db != nullptr)
+  err = run_product(pr, dy, x, e, pr.sums_rows ? db : nullptr, ws_body(ws), s);
+  if (err == hipSuccess && db != nullptr && !pr.sums_rows)
     err = colsum_launch(static_cast<const bf16_t*>(dy), d.ldy, d.m, d.n,
-                        reinterpret_cast<float*>(static_cast<char*>(ws_body(ws)) + pr.extra_at), db, accumulate != 0, s);
+                        reinterpret_cast<float*>(static_cast<char*>(ws_body(ws)) + pr.db_at), db, accumulate != 0, s);
   return err == hipSuccess ? ok() : hip_fail(err, "linear weight gradient launch");
 }
 

@@ -47,6 +47,13 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t rsrc(const void* base) {
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), (short)0, kRecords, 0x00020000);
 }
 
+// the sum of 8 bf16 values
+__device__ __forceinline__ float sum8(u32x4 v) {
+  float f[8];
+  unpack8(make_uint4(v.x, v.y, v.z, v.w), f);
+  return ((f[0] + f[1]) + (f[2] + f[3])) + ((f[4] + f[5]) + (f[6] + f[7]));
+}
+
 // ---------------------------------------------------------------------------
 // ANY_: operands' rows may start at any element (they pass through registers to LDS)
 template <int BM_, int BN_, int BK_, int S_, int WM_, int WN_, bool ANY_ = false>
@@ -324,6 +331,12 @@ __global__ __launch_bounds__(C::NW * 64) void gemm_kernel(GemmArgs a) {
       for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
 
   u32x4 af[2][TM], bf[2][TN];
+  // The bias gradient is the sum of the weight gradient's first operand over the reduction: the blocks
+  // of the first column of tiles add up the fragments that they multiply anyway, each of the waves that
+  // share TM of them one.  (Not where a.db is left out: see gemm_sums_rows.)
+  static_assert(TM <= C::WN, "a wave for each fragment");
+  const bool sums = __builtin_amdgcn_readfirstlane(KIND == kGemmWgrad && a.db != nullptr && tn == 0 ? 1 : 0) != 0;
+  float rowsum = 0.f;
   // fragment r of slice ks of a stage, A's first, into buffer b
   auto rd = [&](auto uc, int r, int ks, int b) __attribute__((always_inline)) {
     const unsigned char* st = stage(uc);
@@ -335,7 +348,7 @@ __global__ __launch_bounds__(C::NW * 64) void gemm_kernel(GemmArgs a) {
   // compiler sinks each read to its use, and a SIMD with one wave then waits out the LDS's latency
   // in every slice.
   constexpr int LOADING = S == 2 ? KS - 1 : KS;  // slices that carry loads
-  auto slice = [&](auto uc, auto kc) __attribute__((always_inline)) {
+  auto slice = [&](auto uc, auto kc, auto sumc) __attribute__((always_inline)) {
     constexpr int u = decltype(uc)::value, ks = decltype(kc)::value, b = ks & 1;
     constexpr bool last = ks == KS - 1;
     constexpr int L0 = ks < LOADING ? ks * L / LOADING : L, L1 = ks < LOADING ? (ks + 1) * L / LOADING : L;
@@ -349,6 +362,8 @@ __global__ __launch_bounds__(C::NW * 64) void gemm_kernel(GemmArgs a) {
 #pragma unroll
       for (int q = l0; q < l1; ++q) load(Ic<(u + S - 1) % S>{}, q);
       acc[t / TN][t % TN] = mfma32x32x16(bf[b][t % TN], af[b][t / TN], acc[t / TN][t % TN]);
+      if constexpr (decltype(sumc)::value != 0 && t % TN == 0)
+        if (wn == t / TN) rowsum += sum8(af[b][t / TN]);
       __builtin_amdgcn_sched_barrier(0);
     });
   };
@@ -358,13 +373,13 @@ __global__ __launch_bounds__(C::NW * 64) void gemm_kernel(GemmArgs a) {
   // so the last slice can read the next stage.
   constexpr int PENDING = S == 2 ? 0 : (S - 3) * L + (KS - 1) * L / KS;
   // (ANY: step kt + 1 goes from its registers to LDS first, and step kt + 3 is loaded into them)
-  auto step = [&](auto uc) __attribute__((always_inline)) {
+  auto step = [&](auto uc, auto sumc) __attribute__((always_inline)) {
     constexpr int u = decltype(uc)::value;
     put_stage(Ic<(u + 1) % S>{});
-    static_for<0, KS - 1>([&](auto kc) __attribute__((always_inline)) { slice(uc, kc); });
+    static_for<0, KS - 1>([&](auto kc) __attribute__((always_inline)) { slice(uc, kc, sumc); });
     if constexpr (C::ANY) __syncthreads();
     else asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(PENDING) : "memory");
-    slice(uc, Ic<KS - 1>{});
+    slice(uc, Ic<KS - 1>{}, sumc);
     advance();
   };
   static_for<0, S - 1>([&](auto uc) {
@@ -386,11 +401,21 @@ __global__ __launch_bounds__(C::NW * 64) void gemm_kernel(GemmArgs a) {
   }
 #pragma unroll
   for (int r = 0; r < TM + TN; ++r) rd(Ic<0>{}, r, 0, 0);
-  int kt = 0;
-  for (; kt + S <= nk; kt += S) static_for<0, S>([&](auto uc) { step(uc); });
-  static_for<0, S - 1>([&](auto uc) {
-    if (kt + decltype(uc)::value < nk) step(uc);
-  });
+  // (a loop of its own for the blocks that add up fragments: the branch in its slices would cost every
+  // 256 x 256 tile 5%)
+  auto walk = [&](auto sumc) __attribute__((always_inline)) {
+    int kt = 0;
+    for (; kt + S <= nk; kt += S) static_for<0, S>([&](auto uc) { step(uc, sumc); });
+    static_for<0, S - 1>([&](auto uc) {
+      if (kt + decltype(uc)::value < nk) step(uc, sumc);
+    });
+  };
+  if constexpr (KIND == kGemmWgrad) {
+    if (sums) walk(Ic<1>{});
+    else walk(Ic<0>{});
+  } else {
+    walk(Ic<0>{});
+  }
   // the loads issued past the last step land before the stages become staging space
   asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
 
@@ -426,6 +451,14 @@ __global__ __launch_bounds__(C::NW * 64) void gemm_kernel(GemmArgs a) {
       f[4 * i + 3] = v.w;
     }
   };
+  if constexpr (KIND == kGemmWgrad) {
+    if (sums && wn < TM) {
+      float* db = (a.splits > 1 ? a.db_part + split * a.m : a.db) + m0;
+      const float s = rowsum + __shfl_xor(rowsum, 32);  // (the halves hold different k)
+      const int r = (wm * TM + wn) * 32 + l32;
+      if (half == 0 && r < rows) db[r] = a.splits == 1 && a.e.accumulate ? db[r] + s : s;
+    }
+  }
   if (a.splits > 1) {
     constexpr int RPP = 256 / C::OW;
     float* part = a.part + ((int64_t)split * a.m + m0) * a.ldp + n0;
@@ -492,7 +525,14 @@ template <int KIND, bool VEC>
 __global__ __launch_bounds__(256) void gemm_finish_kernel(GemmArgs a) {
   const int per_row = (a.n + 3) / 4;
   const int64_t total = a.m * per_row, step = a.m * a.ldp;
-  for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < total; i += gridDim.x * 256ll) {
+  for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < total + (KIND == kGemmWgrad && a.db != nullptr ? a.m : 0);
+       i += gridDim.x * 256ll) {
+    if (KIND == kGemmWgrad && i >= total) {  // the bias gradient's ranges
+      float t = 0.f;
+      for (int s = 0; s < a.splits; ++s) t += a.db_part[s * a.m + i - total];
+      a.db[i - total] = a.e.accumulate ? a.db[i - total] + t : t;
+      continue;
+    }
     const int64_t row = i / per_row;
     const int col = (int)(i - row * per_row) * 4;
     float f[4] = {}, b[4];
@@ -549,11 +589,10 @@ __global__ __launch_bounds__(256) void gemm_pack_kernel(GemmPack a, GemmPack b) 
 }
 
 // Bias gradient: a block of 16 waves sums a range of rows of 512 columns, a wave every sixteenth row of
-// it with 8 columns per lane and four rows' loads in flight.  One range is the result, several are
-// partials for column_sum_kernel.
+// it with 8 columns per lane and four rows' loads in flight; column_sum_kernel adds the ranges' sums.
 template <bool VEC>
 __global__ __launch_bounds__(1024) void colsum_kernel(const bf16_t* src, int64_t lds, int64_t rows, int cols,
-                                                      int64_t rows_per, float* out, int accumulate) {
+                                                      int64_t rows_per, float* part) {
   __shared__ float s_sum[16][512];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = blockIdx.x * 512 + lane * 8;
   const int64_t r0 = blockIdx.y * rows_per, r1 = r0 + rows_per < rows ? r0 + rows_per : rows;
@@ -591,8 +630,7 @@ __global__ __launch_bounds__(1024) void colsum_kernel(const bf16_t* src, int64_t
     float t = s_sum[0][i];
 #pragma unroll
     for (int w = 1; w < 16; ++w) t += s_sum[w][i];
-    float* o = out + (int64_t)blockIdx.y * cols + col;
-    *o = accumulate ? *o + t : t;
+    part[(int64_t)blockIdx.y * cols + col] = t;
   }
 }
 
@@ -643,10 +681,10 @@ __global__ __launch_bounds__(1024) void column_sum_kernel(const float* part, int
   }
 }
 
-// ranges of rows: one of up to 256 rows, which needs no second launch, else enough blocks for the chip
+// ranges of rows: enough blocks for the chip
 int64_t colsum_rows_per(int64_t rows, int cols) {
   const int64_t blocks = (cols + 511) / 512;
-  const int64_t ranges = rows <= 256 ? 1 : std::max<int64_t>(1, std::min<int64_t>((2048 + blocks - 1) / blocks, rows / 64));
+  const int64_t ranges = std::max<int64_t>(1, std::min<int64_t>((2048 + blocks - 1) / blocks, rows / 64));
   return (rows + ranges - 1) / ranges;
 }
 
@@ -683,7 +721,7 @@ hipError_t launch_kind(const GemmArgs& a, int tile, hipStream_t s) {
   trace_end(KC_LINEAR);
   if (e != hipSuccess || a.splits == 1) return e;
   trace_begin(KC_LINEAR_FINISH);
-  const dim3 grid(grid_for(a.m * ((a.n + 3) / 4)));
+  const dim3 grid(grid_for(a.m * ((a.n + 3) / 4) + (a.db != nullptr ? a.m : 0)));
   if (a.e.vec) NUMBAT_LAUNCH((gemm_finish_kernel<KIND, true>), grid, dim3(256), 0, s, a);
   else NUMBAT_LAUNCH((gemm_finish_kernel<KIND, false>), grid, dim3(256), 0, s, a);
   trace_end(KC_LINEAR_FINISH);
@@ -750,6 +788,12 @@ GemmPlan gemm_pick(GemmKind kind, int64_t m, int n, int64_t k, int out_bytes, do
 
 bool gemm_any_rows(const GemmPlan& p) { return p.tile == kTileRows || p.tile == kTile64Any; }
 
+// Adding up fragments slows a long block of 256 columns by a tenth, and a block's time grows with its
+// range, where a pass over A of its own takes about 10 us: 20000 x 4096 x 2048's gradients 302 us with
+// the pass and 328 without, 1000 x 2048 x 2048's 21 and 18.  Narrower tiles never lose by it (20000 x
+// 4096 x 2048 on 128 x 128: 368 and 346).
+bool gemm_sums_rows(const GemmPlan& p) { return kTiles[p.tile].n < 256 || p.k_per_split <= 4096; }
+
 size_t gemm_part_bytes(const GemmPlan& p, int64_t m, int n) {
   return p.splits > 1 ? (size_t)p.splits * (size_t)m * ((n + 31) / 32 * 32) * sizeof(float) : 0;
 }
@@ -787,13 +831,11 @@ hipError_t colsum_launch(const bf16_t* src, int64_t lds, int64_t rows, int32_t c
   const int64_t per = colsum_rows_per(rows, cols);
   const unsigned ranges = (unsigned)((rows + per - 1) / per);
   const dim3 grid((unsigned)((cols + 511) / 512), ranges);
-  float* to = ranges == 1 ? out : part;
-  const int acc = ranges == 1 ? accumulate : 0;
   trace_begin(KC_LINEAR_BIAS_GRAD);
-  if (cols % 8 == 0 && lds % 8 == 0) NUMBAT_LAUNCH(colsum_kernel<true>, grid, dim3(1024), 0, s, src, lds, rows, cols, per, to, acc);
-  else NUMBAT_LAUNCH(colsum_kernel<false>, grid, dim3(1024), 0, s, src, lds, rows, cols, per, to, acc);
+  if (cols % 8 == 0 && lds % 8 == 0) NUMBAT_LAUNCH(colsum_kernel<true>, grid, dim3(1024), 0, s, src, lds, rows, cols, per, part);
+  else NUMBAT_LAUNCH(colsum_kernel<false>, grid, dim3(1024), 0, s, src, lds, rows, cols, per, part);
   const hipError_t e = hipGetLastError();
-  if (e == hipSuccess && ranges > 1) column_sum_launch(part, (int)ranges, cols, cols, cols, out, nullptr, accumulate, s);
+  if (e == hipSuccess) column_sum_launch(part, (int)ranges, cols, cols, cols, out, nullptr, accumulate, s);
   trace_end(KC_LINEAR_BIAS_GRAD);
   return e != hipSuccess ? e : hipGetLastError();
 }

@@ -40,6 +40,7 @@ struct GemmArgs {
   int64_t k_per_split;  // a multiple of the reduction step
   float* part;          // [splits][m][ldp] fp32
   int64_t ldp;
+  float *db, *db_part;  // weight gradient: sums of A over the reduction [m] or nullptr, their ranges' [splits][m]
   GemmEpilogue e;
 };
 
@@ -54,6 +55,8 @@ struct GemmPlan {
 GemmPlan gemm_pick(GemmKind kind, int64_t m, int n, int64_t k, int out_bytes, double pack_bytes);
 // whether the plan's kernel takes operands whose rows start at any element
 bool gemm_any_rows(const GemmPlan& p);
+// whether a weight gradient's plan adds up its first operand on the way (GemmArgs::db)
+bool gemm_sums_rows(const GemmPlan& p);
 size_t gemm_part_bytes(const GemmPlan& p, int64_t m, int n);
 // a.part holds gemm_part_bytes; every dimension is at least 1
 hipError_t gemm_launch(GemmKind kind, GemmArgs a, const GemmPlan& p, hipStream_t s);
