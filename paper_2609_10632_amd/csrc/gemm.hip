@@ -15,7 +15,9 @@
 // Per step a block reads (BM + BN) * BK * 2 bytes of operands and issues BM * BN * BK
 // multiply-adds: a 256 x 256 tile needs 1/64 byte per flop, which the L2s deliver at the
 // matrix cores' rate; what bounds long reductions is the matrix cores, short ones (maps of
-// few channels) the bytes of x, z and y.
+// few channels) the bytes of x, z and y.  8192 rows, 4096 -> 16384 with GELU and z: 976 us, 1126 TFLOP/s
+// (without an epilogue's work 1195; dx 1130, dw 1340; the largest library product of this card reaches
+// 1385); 102400 rows, 192 -> 768 with SiLU and z: 81 us, 4.4 TB/s of 5.1.
 #include <algorithm>
 #include <cmath>
 
@@ -694,6 +696,17 @@ __global__ __launch_bounds__(256) void fill_zero_kernel(float* p, int64_t n) {
 
 unsigned grid_for(int64_t threads) { return (unsigned)std::min<int64_t>(4096, std::max<int64_t>(1, (threads + 255) / 256)); }
 
+// The tiles, largest first (us of each where its neighbours were measured too; m x k -> n, forward):
+//   256 x 256   the least operand bytes per flop: 8192 x 4096 -> 16384 920 (128 x 256: 968, 128 x 128: 1110)
+//   128 x 256   the same where 256 x 256 leaves CUs idle: 2048 x 4096 -> 4096 56.6 (75.0, 60.5)
+//   128 x 128, four stages, one block to a CU: few blocks with long reductions, whose latency the
+//               stages hide: 4096 x 2048 -> 1024 18.9 (128 x 256: 23.3, two stages: 25.1)
+//   128 x 128, two stages, two blocks to a CU: short reductions, where one block's epilogue runs
+//               beside the other's products: 102400 x 192 -> 768 59.9 (four stages: 75.8)
+//   64 x 64     little work: 1024 x 512 -> 768 4.8 (128 x 128: 6.5); 64 x 1024 -> 1024 5.7 (8.3)
+//   64 x 64 of any rows, through registers: 334 x 441 -> 329 7.7 (copies and the above: 8.1); larger
+//               products of odd rows are faster from copies: 1531 x 1003 -> 2049 23.2 (29.8)
+// Split reductions add blocks where there are few: 24 x 8192 -> 4096 16 us on 64 tiles of 4 ranges.
 using T256 = Tile<256, 256, 32, 4, 2, 4>;
 using T128W = Tile<128, 256, 64, 3, 2, 4>;
 using T128D = Tile<128, 128, 64, 4, 2, 4>;
@@ -758,6 +771,15 @@ double tile_time(GemmKind kind, int tile, int64_t blocks, int64_t k, int out_byt
   }
 }
 
+// and on the kernel for few rows: a block streams 16 rows of w past its rows of x; odd rows (unaligned
+// loads) make x the longer part (us there and on the best tile; m x k -> n): 16 x 2048 -> 2048 5.9 and 7.7,
+// 4 x 4096 -> 4096 8.4 and 10.7, 16 x 8192 -> 1024 16.4 and 11.9, 16 x 4096 -> 16384 37 and 31,
+// 16 x 5441 -> 345 36 and 12
+double rows_time(int64_t m, int n, int64_t k, bool odd) {
+  const double per_cu = std::ceil(n / 4096.0);
+  return 3.0 + per_cu * k * (odd ? 2.5 + 0.22 * m : 1.0 + 0.04 * m + 0.3 * std::min(1.0, n / 4096.0)) / 1000;
+}
+
 // and the second launch that adds the sums of the splits
 double finish_time(int splits, int64_t m, int n) { return splits == 1 ? 0.0 : 4.0 + 0.1 * splits + (double)splits * m * n * 8 / 6e6; }
 
@@ -765,7 +787,6 @@ double finish_time(int splits, int64_t m, int n) { return splits == 1 ? 0.0 : 4.
 
 GemmPlan gemm_pick(GemmKind kind, int64_t m, int n, int64_t k, int out_bytes, double pack_bytes) {
   GemmPlan p{kTile64, 1, 0};
-  if (kind == kGemmFwd && m <= kLinearRows) return GemmPlan{kTileRows, 1, k};
   const int64_t steps = (k + 63) / 64;
   double best = 1e30;
   for (int tile = kTile256; tile <= (pack_bytes > 0 ? kTile64Any : kTile64); ++tile) {
@@ -783,6 +804,9 @@ GemmPlan gemm_pick(GemmKind kind, int64_t m, int n, int64_t k, int out_bytes, do
       }
     }
   }
+  // no tile is faster than w's bytes come
+  if (kind == kGemmFwd && m <= kLinearRows && rows_time(m, n, k, pack_bytes > 0) <= std::max(best, 2.5 + 2.0 * n * k / 5e6))
+    return GemmPlan{kTileRows, 1, k};
   return p;
 }
 

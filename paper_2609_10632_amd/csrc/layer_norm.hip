@@ -7,7 +7,8 @@
 // (no cancellation).  Lanes hold 16-byte vectors where the rows allow them and single elements
 // otherwise; a lane's columns are the same for every row, so the backward adds dgamma and dbeta in
 // registers over all rows of a block and writes one partial per block, which a second kernel sums
-// in a fixed order.  Everything is bound by the bytes of the rows.
+// in a fixed order.  Everything is bound by the bytes of the rows: gradients of 102400 x 192 bf16 with the
+// residual's 35 us (4.5 TB/s), of 16384 x 8192 fp32 346 us (5.4 TB/s); 16 x 4096 forward 3.4 us, a launch.
 #include <algorithm>
 
 #include "mlp_kernels.h"
@@ -378,7 +379,9 @@ int group_lanes(int c) {
 int bwd_blocks(const LnArgs& a) {
   if (a.c > kLongest) return (int)std::min<int64_t>(kLongRanges, a.m);
   const int g = group_lanes(a.c), rpb = (g > 256 ? g : 256) / g;
-  // four blocks to a CU of short rows; a partial is as long as two rows, so long ones take fewer
+  // four blocks to a CU of short rows; a partial is as long as two rows, so long ones take fewer (us on
+  // 512, 1024 and 2048 blocks: 102400 x 192 37.2, 29.6, 34.1; 16384 x 1024 30.3, 31.0, 38.8; 16384 x 8192
+  // 346, 366, 399)
   return (int)std::min<int64_t>(g <= 128 ? 1024 : 512, (a.m + rpb - 1) / rpb);
 }
 

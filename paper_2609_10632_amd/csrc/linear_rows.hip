@@ -1,6 +1,7 @@
 // The forward of a linear layer for few rows (one token, a decode batch) on gfx950:
 //   y[m][n] = epilogue(sum_k x[m][k] w[n][k]),  m at most 16.
-// Bound by the bytes of w, which every launch reads once.  A block takes 16 rows of w and its waves
+// Bound by the bytes of w, which every launch reads once (one row of 2048 -> 8192 in 8.0 us: 34 MB at
+// 4.2 TB/s with the launch in it, where a large copy moves 5.1 TB/s).  A block takes 16 rows of w and its waves
 // split the reduction, so that all 256 CUs stream w even for narrow layers and each wave has
 // 4 x 2 KiB of it in flight; the matrix core multiplies 16 rows of w by 16 rows of x per
 // instruction (a 16 x 16 x 32 product, most of it idle for one token: the arithmetic is free here).
@@ -107,10 +108,13 @@ void launch_rows(const GemmArgs& a, hipStream_t s) {
 
 hipError_t linear_rows_launch(const GemmArgs& a, hipStream_t s) {
   trace_begin(KC_LINEAR);
-  // a wave of at least 256 k: with less its sums cost more than its loads hide
-  if (a.k >= 4096) launch_rows<16>(a, s);
-  else if (a.k >= 1024) launch_rows<8>(a, s);
-  else launch_rows<4>(a, s);
+  // More waves to a block hide more of w's latency where there are few blocks and their share of k is
+  // long, and cost more sums (us for one row on 4, 8 and 16 waves; k -> n): 512 -> 4096 4.5, 5.4, 5.5;
+  // 2048 -> 4096 5.2, 5.2, 7.7; 8192 -> 1024 13.3, 11.9, 11.1; 8192 -> 4096 14.7, 13.6, 14.7;
+  // 2048 -> 16384 12.3, 14.8, 24.8.
+  if (a.k < 2048 || a.n >= 8192) launch_rows<4>(a, s);
+  else if (a.k < 4096 || a.n >= 4096) launch_rows<8>(a, s);
+  else launch_rows<16>(a, s);
   trace_end(KC_LINEAR);
   return hipGetLastError();
 }
