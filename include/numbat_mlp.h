@@ -39,7 +39,8 @@ typedef enum {
 } numbat_act;
 
 /* One linear layer: x [m][k], w [n][k] (dense, out features first), y [m][n].  n, k and row
- * strides are at most 2^21.  Strides are in elements; 0 means dense. */
+ * strides are at most 2^21; products of more tiles than one launch takes (past 2^38 outputs, or
+ * 2^30 rows of a narrow layer) are NUMBAT_ERR_UNSUPPORTED.  Strides are in elements; 0 means dense. */
 typedef struct {
   uint32_t struct_size;  /* = sizeof(numbat_linear_problem) */
   int32_t n, k;          /* output and input features */
@@ -136,7 +137,8 @@ typedef struct {
  * state_bits: 32 or 8.  In 8 bits the update uses the new moments before they are rounded; a
  * block whose unit would be below the smallest normal number is stored as zeros, and a v above
  * zero never rounds to zero within its block; a moment that is not finite takes the largest code.  total_norm: NULL, or a device float that receives
- * the norm (only with max_norm > 0).  A non-finite norm does not clip.
+ * the norm (only with max_norm > 0).  Of a gradient that is not finite: a NaN norm
+ * does not clip, an infinite one gives c = 0 (its infinite elements then become NaN).
  * ws: numbat_workspace_size(NUMBAT_OP_ADAMW), problem ignored. */
 numbat_status numbat_adamw_step(const numbat_adamw_tensor* tensors, int32_t count, const numbat_sgd_group* groups,
                                 int32_t ngroups, int32_t state_bits, double beta1, double beta2, double eps,

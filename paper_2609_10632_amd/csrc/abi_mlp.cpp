@@ -116,6 +116,12 @@ Product product(const LinearDesc& d, GemmKind kind) {
   return p;
 }
 
+numbat_status check_grid(const Product& p) {
+  if (p.m > 0 && !gemm_fits(p.plan, p.m, p.n))
+    return fail(NUMBAT_ERR_UNSUPPORTED, "the product has more tiles than one launch takes (%lld x %d)", (long long)p.m, p.n);
+  return NUMBAT_OK;
+}
+
 // the operand as the product reads it: where it lies, or its padded copy to be made
 GemmPack packed(const Product::Op& o, const void* src, char* ws, const bf16_t** out, int64_t* ld) {
   const bf16_t* s = static_cast<const bf16_t*>(src);
@@ -189,10 +195,12 @@ bool mlp_workspace_size(int op, const void* problem, size_t* bytes, numbat_statu
       LinearDesc d;
       *st = check_linear(static_cast<const numbat_linear_problem*>(problem), op == NUMBAT_OP_LINEAR_FWD, &d);
       if (*st != NUMBAT_OK) return true;
-      *bytes = with_header(product(d, op == NUMBAT_OP_LINEAR_FWD        ? kGemmFwd
-                                      : op == NUMBAT_OP_LINEAR_BWD_DATA ? kGemmDgrad
-                                                                        : kGemmWgrad)
-                               .bytes);
+      const Product pr = product(d, op == NUMBAT_OP_LINEAR_FWD        ? kGemmFwd
+                                    : op == NUMBAT_OP_LINEAR_BWD_DATA ? kGemmDgrad
+                                                                      : kGemmWgrad);
+      *st = check_grid(pr);
+      if (*st != NUMBAT_OK) return true;
+      *bytes = with_header(pr.bytes);
       break;
     }
     case NUMBAT_OP_LAYER_NORM_BWD: {
@@ -223,6 +231,8 @@ numbat_status numbat_linear_fwd(const numbat_linear_problem* p, const void* x, c
   if (!aligned16(x) || !aligned16(w) || !aligned16(y) || !aligned16(residual) || !aligned16(z))
     return fail(NUMBAT_ERR_ALIGN, "x, w, y, residual and z must be 16-byte aligned");
   const Product pr = product(d, kGemmFwd);
+  st = check_grid(pr);
+  if (st != NUMBAT_OK) return st;
   st = check_ws(ws, ws_bytes, with_header(pr.bytes));
   if (st != NUMBAT_OK) return st;
   GemmEpilogue e;
@@ -253,6 +263,8 @@ numbat_status numbat_linear_bwd_data(const numbat_linear_problem* p, const void*
   if (!aligned16(dy) || !aligned16(w) || !aligned16(dx) || !aligned16(z))
     return fail(NUMBAT_ERR_ALIGN, "dy, w, dx and z must be 16-byte aligned");
   const Product pr = product(d, kGemmDgrad);
+  st = check_grid(pr);
+  if (st != NUMBAT_OK) return st;
   st = check_ws(ws, ws_bytes, with_header(pr.bytes));
   if (st != NUMBAT_OK) return st;
   GemmEpilogue e;
@@ -277,6 +289,8 @@ numbat_status numbat_linear_bwd_weight(const numbat_linear_problem* p, const voi
     return fail(NUMBAT_ERR_NULL, "x, dy and dw are required");
   if (!aligned16(x) || !aligned16(dy)) return fail(NUMBAT_ERR_ALIGN, "x and dy must be 16-byte aligned");
   const Product pr = product(d, kGemmWgrad);
+  st = check_grid(pr);
+  if (st != NUMBAT_OK) return st;
   st = check_ws(ws, ws_bytes, with_header(pr.bytes));
   if (st != NUMBAT_OK) return st;
   const hipStream_t s = static_cast<hipStream_t>(stream);

@@ -810,6 +810,11 @@ GemmPlan gemm_pick(GemmKind kind, int64_t m, int n, int64_t k, int out_bytes, do
   return p;
 }
 
+// a launch takes fewer than 2^32 threads
+bool gemm_fits(const GemmPlan& p, int64_t m, int n) {
+  return p.tile == kTileRows || tile_count(p.tile, m, n) * p.splits < (1ll << 32) / (p.tile >= kTile64 ? 256 : 512);
+}
+
 bool gemm_any_rows(const GemmPlan& p) { return p.tile == kTileRows || p.tile == kTile64Any; }
 
 // Adding up fragments slows a long block of 256 columns by a tenth, and a block's time grows with its

@@ -413,9 +413,18 @@ void fwd_typed(const LnArgs& a, const void* x, const float* gamma, const float* 
   }
   with_group(a.c, [&](auto gc, auto vc) {
     constexpr int G = decltype(gc)::value, V = decltype(vc)::value, NT = ln_threads<G>();
-    const dim3 grid((unsigned)((a.m + NT / G - 1) / (NT / G)));
-    if (a.vec) NUMBAT_LAUNCH((ln_fwd_kernel<G, V, true, TX, TY>), grid, dim3(NT), 0, s, a, xp, gamma, beta, yp, mean, rstd);
-    else NUMBAT_LAUNCH((ln_fwd_kernel<G, V, false, TX, TY>), grid, dim3(NT), 0, s, a, xp, gamma, beta, yp, mean, rstd);
+    // a launch takes fewer than 2^32 threads: more rows than that in several
+    constexpr int64_t RPB = NT / G, MOST = ((1ll << 31) / NT) * RPB;
+    for (int64_t r = 0; r < a.m; r += MOST) {
+      LnArgs b = a;
+      b.m = std::min(a.m - r, MOST);
+      const dim3 grid((unsigned)((b.m + RPB - 1) / RPB));
+      const TX* xr = xp + r * a.ldx;
+      TY* yr = yp + r * a.ldy;
+      float *mr = mean != nullptr ? mean + r : nullptr, *sr = rstd != nullptr ? rstd + r : nullptr;
+      if (a.vec) NUMBAT_LAUNCH((ln_fwd_kernel<G, V, true, TX, TY>), grid, dim3(NT), 0, s, b, xr, gamma, beta, yr, mr, sr);
+      else NUMBAT_LAUNCH((ln_fwd_kernel<G, V, false, TX, TY>), grid, dim3(NT), 0, s, b, xr, gamma, beta, yr, mr, sr);
+    }
   });
 }
 

@@ -53,6 +53,8 @@ struct GemmPlan {
 // out_bytes: what the epilogue reads and writes for each element; pack_bytes: size of the operands that
 // would have to be padded (0: none)
 GemmPlan gemm_pick(GemmKind kind, int64_t m, int n, int64_t k, int out_bytes, double pack_bytes);
+// whether the plan's grid is one that a launch takes
+bool gemm_fits(const GemmPlan& p, int64_t m, int n);
 // whether the plan's kernel takes operands whose rows start at any element
 bool gemm_any_rows(const GemmPlan& p);
 // whether a weight gradient's plan adds up its first operand on the way (GemmArgs::db)

@@ -127,10 +127,10 @@ class MlpBlock:
         if g_rows != rows:
             raise ValueError("g: one row for each of x")
         up, _, down, ln = self._problems(rows, stride, g_stride)
+        up.act = nb.ACT_NONE  # (the norm's output went into it as it is)
         ws = self._workspace(*[(o, p) for o in (nb.OP_LINEAR_BWD_DATA, nb.OP_LINEAR_BWD_WEIGHT) for p in (up, down)],
                              (nb.OP_LAYER_NORM_BWD, ln))
         c, d = self.copies, self.grads
-        up.act = nb.ACT_NONE  # (the norm's output went into it as it is)
         nb.numbat_linear_bwd_data(down, g, c["w2"], self.z, self.dwide, False, ws)
         nb.numbat_linear_bwd_weight(down, self.wide, g, d["w2"], d["b2"], accumulate, ws)
         nb.numbat_linear_bwd_data(up, self.dwide, c["w1"], None, self.dnormed, False, ws)

@@ -257,3 +257,22 @@ def test_in_place_streams_and_graph():
         torch.cuda.synchronize()
         for a, b in zip(want, (y, dx, dg, db)):
             assert torch.equal(a, b)
+
+
+def test_forward_of_more_rows_than_one_launch():
+    """2^31 threads a launch: 2^27 rows of at most 128 features."""
+    m, c = (1 << 27) + 21, 2
+    x = torch.randint(-8, 8, (m, c), device="cuda", dtype=torch.int16).bfloat16()
+    x[-3:] = torch.tensor([[1.0, 3.0], [5.0, 5.0], [-2.0, 6.0]])
+    y = torch.full_like(x, float("nan"))
+    mean, rstd = (torch.full((m,), float("nan"), device="cuda") for _ in range(2))
+    nb.numbat_layer_norm_fwd(nb.layer_norm_problem(m, c, eps=1.0), x, None, None, y, mean, rstd)
+    assert mean[-3:].tolist() == [2.0, 5.0, 2.0]
+    # half-sums of small integers and their squares are exact; a root and a quotient round once or twice
+    half = (x[:, 0].float() - x[:, 1].float()) * 0.5
+    assert torch.equal(mean, (x[:, 0].float() + x[:, 1].float()) * 0.5)
+    want = 1.0 / torch.sqrt(half * half + 1.0)
+    assert bool(((rstd - want).abs() <= 2 ** -22 * want).all())
+    half *= want
+    assert bool(((y[:, 0].float() - half).abs() <= (2 ** -8 + 2 ** -20) * half.abs()).all())
+    assert bool(((y[:, 1].float() + half).abs() <= (2 ** -8 + 2 ** -20) * half.abs()).all())

@@ -153,3 +153,15 @@ def test_adamw_refusals():
         args = [P] * 6
         args[i] = None
         assert status_of(values, 8, *args) == nb.ERR_NULL
+
+
+def test_products_past_one_launch_are_refused():
+    """A launch takes fewer than 2^32 threads: a 64 x 64 tile's 256 threads, 2^24 tiles."""
+    big = nb.linear_problem((1 << 31) - 1, 8, 8)
+    for op, which in ((nb.OP_LINEAR_FWD, "fwd"), (nb.OP_LINEAR_BWD_DATA, "data")):
+        assert status_of(nb.numbat_workspace_size, op, big) == nb.ERR_UNSUPPORTED
+        assert status_of(LINEAR[which], big, ws=P, b=1 << 40) == nb.ERR_UNSUPPORTED
+    wide = nb.linear_problem(8, 1 << 21, 1 << 21)
+    assert status_of(LINEAR["weight"], wide, ws=P, b=1 << 62) == nb.ERR_UNSUPPORTED
+    # the sums over as many rows are few tiles
+    assert nb.numbat_workspace_size(nb.OP_LINEAR_BWD_WEIGHT, big) > 0
