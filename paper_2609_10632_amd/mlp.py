@@ -75,6 +75,7 @@ class MlpBlock:
         self.dwide, self.dnormed, self.dx = bf(rows, hidden), bf(rows, width), bf(rows, width)
         self.mean, self.rstd = new(rows, torch.float32), new(rows, torch.float32)
         self.norm = new(1, torch.float32)
+        self.kept = None  # rows of the forward whose activations, statistics and weights are at hand
         up, down, down_grad, ln = self._problems(rows, width, width)
         size = nb.numbat_workspace_size
         # all calls of the block are on one stream, one after another: they share a workspace
@@ -108,8 +109,10 @@ class MlpBlock:
     def forward(self, x, keep=True):
         """x: bf16 [rows][width], rows as far apart as its stride says (``map[..., a:b].flatten(0, 2)``
         of an NHWC map).  keep: for backward(); without, as in serving, neither z nor the norm's
-        statistics are written.  Returns a view of the block's output buffer."""
+        statistics are written, and backward() refuses what an earlier forward has kept, as other
+        activations are overwritten.  Returns a view of the block's output buffer."""
         rows, stride = self._check(x, "x")
+        self.kept = None
         up, down, _, ln = self._problems(rows, stride, self.width)
         ws = self._workspace((nb.OP_LINEAR_FWD, up), (nb.OP_LINEAR_FWD, down))
         c = self.copies
@@ -117,15 +120,18 @@ class MlpBlock:
                                  self.mean if keep else None, self.rstd if keep else None)
         nb.numbat_linear_fwd(up, self.normed, c["w1"], self.params["b1"], None, self.z if keep else None, self.wide, ws)
         nb.numbat_linear_fwd(down, self.wide, c["w2"], self.params["b2"], x, None, self.y, ws)
+        self.kept = rows if keep else None
         return self.y[:rows]
 
     def backward(self, x, g, accumulate=False):
-        """The gradients of sum(g y) after forward(x): parameters' into ``grads`` (accumulate: added),
-        x's into the returned buffer."""
+        """The gradients of sum(g y): parameters' into ``grads`` (accumulate: added), x's into the
+        returned buffer.  The last forward has to be forward(x, keep=True), with no step() since."""
         rows, stride = self._check(x, "x")
         g_rows, g_stride = self._check(g, "g")
         if g_rows != rows:
             raise ValueError("g: one row for each of x")
+        if self.kept != rows:
+            raise RuntimeError(f"backward of {rows} rows: the last forward kept {self.kept or 'nothing'}, or a step followed it")
         up, _, down, ln = self._problems(rows, stride, g_stride)
         up.act = nb.ACT_NONE  # (the norm's output went into it as it is)
         ws = self._workspace(*[(o, p) for o in (nb.OP_LINEAR_BWD_DATA, nb.OP_LINEAR_BWD_WEIGHT) for p in (up, down)],
@@ -142,6 +148,7 @@ class MlpBlock:
     def step(self, lr, weight_decay=0.1, betas=(0.9, 0.95), eps=1e-8, max_norm=1.0):
         """One AdamW step from ``grads``; returns the device float that receives the gradients' norm
         (with max_norm > 0)."""
+        self.kept = None
         self.steps += 1
         nb.numbat_adamw_step(self.table, self.count, ((lr, weight_decay), (lr, 0.0)), self.state_bits, betas[0],
                              betas[1], eps, self.steps, max_norm, self.norm if max_norm > 0 else None, self.ws)

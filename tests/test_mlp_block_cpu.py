@@ -1,0 +1,53 @@
+"""The residual MLP block's own bookkeeping, without a GPU: its calls into the library are replaced by
+ones that compute nothing, and what it refuses is looked at."""
+import pytest
+
+torch = pytest.importorskip("torch")
+
+from paper_2609_10632_amd import mlp  # noqa: E402
+
+CALLS = ("numbat_linear_fwd", "numbat_linear_bwd_data", "numbat_linear_bwd_weight", "numbat_layer_norm_fwd",
+         "numbat_layer_norm_bwd", "numbat_adamw_step")
+
+
+@pytest.fixture
+def block(monkeypatch):
+    for name in CALLS:
+        monkeypatch.setattr(mlp.nb, name, lambda *a, **k: None)
+    return mlp.MlpBlock(10, 16, 32, device="cpu")
+
+
+def rows(n):
+    return torch.zeros((n, 16), dtype=torch.bfloat16)
+
+
+def test_backward_takes_what_a_forward_has_kept(block):
+    with pytest.raises(RuntimeError):
+        block.backward(rows(10), rows(10))  # no forward yet
+    block.forward(rows(10))
+    block.backward(rows(10), rows(10))
+    block.backward(rows(10), rows(10), accumulate=True)  # as often as wanted
+    block.forward(rows(10), keep=False)  # the buffers now hold another input's activations
+    with pytest.raises(RuntimeError):
+        block.backward(rows(10), rows(10))
+    block.forward(rows(10))
+    block.forward(rows(7))
+    with pytest.raises(RuntimeError):
+        block.backward(rows(10), rows(10))
+    block.backward(rows(7), rows(7))
+    block.step(1e-3)  # the weights are no longer those of the forward
+    with pytest.raises(RuntimeError):
+        block.backward(rows(7), rows(7))
+
+
+def test_a_forward_that_fails_keeps_nothing(block, monkeypatch):
+    block.forward(rows(10))
+
+    def fail(*a, **k):
+        raise ValueError
+
+    monkeypatch.setattr(mlp.nb, "numbat_linear_fwd", fail)
+    with pytest.raises(ValueError):
+        block.forward(rows(10))
+    with pytest.raises(RuntimeError):
+        block.backward(rows(10), rows(10))
