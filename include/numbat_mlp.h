@@ -72,7 +72,8 @@ typedef struct {
 /* Forward of a linear layer, everything on the fp32 sums, each output rounded once:
  *   t = x w^T + bias;  z = t;  y = act(t) + residual
  * x, w: bf16; bias: fp32 [n] or NULL; residual: [m][n] of y's type or NULL; z: bf16 [m][n] or
- * NULL (what the backward of act reads); y: y_type.  y may be the residual's buffer.
+ * NULL (what the backward of act reads); y: y_type.  y may be the residual's buffer if their strides
+ * agree (NUMBAT_ERR_BAD_DESC otherwise).
  * ws: numbat_workspace_size(NUMBAT_OP_LINEAR_FWD), which may be 0. */
 numbat_status numbat_linear_fwd(const numbat_linear_problem* p, const void* x, const void* w, const float* bias,
                                 const void* residual, void* z, void* y, void* ws, size_t ws_bytes, void* stream);
@@ -97,7 +98,8 @@ numbat_status numbat_linear_bwd_weight(const numbat_linear_problem* p, const voi
  *   mean = sum_c x / c,  var = sum_c (x - mean)^2 / c,  rstd = 1 / sqrt(var + eps)
  *   y = gamma (x - mean) rstd + beta
  * gamma, beta: fp32 [c], NULL for 1 and 0; mean, rstd: fp32 [m], each NULL where it is not
- * wanted (the backward reads both).  y may be x's buffer if types and strides agree. */
+ * wanted (the backward reads both).  y may be x's buffer if types and strides agree
+ * (NUMBAT_ERR_BAD_DESC otherwise). */
 numbat_status numbat_layer_norm_fwd(const numbat_layer_norm_problem* p, const void* x, const float* gamma,
                                     const float* beta, void* y, float* mean, float* rstd, void* stream);
 
@@ -105,7 +107,7 @@ numbat_status numbat_layer_norm_fwd(const numbat_layer_norm_problem* p, const vo
  *   dx = rstd (h - sum_c h / c - xh sum_c(h xh) / c) + residual_grad
  *   dgamma = sum_rows dy xh,  dbeta = sum_rows dy          (fp32 [c]; accumulate: added)
  * gamma NULL: 1.  residual_grad [m][c] or NULL: the gradient that reaches x around the norm; dx
- * may be its buffer.  Each of dx, dgamma, dbeta may be NULL where it is not wanted.
+ * may be its buffer if their strides agree (NUMBAT_ERR_BAD_DESC otherwise).  Each of dx, dgamma, dbeta may be NULL where it is not wanted.
  * ws: numbat_workspace_size(NUMBAT_OP_LAYER_NORM_BWD). */
 numbat_status numbat_layer_norm_bwd(const numbat_layer_norm_problem* p, const void* dy, const void* x,
                                     const float* mean, const float* rstd, const float* gamma,

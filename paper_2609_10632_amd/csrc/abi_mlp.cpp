@@ -23,6 +23,12 @@ struct LinearDesc {
 
 bool stride_ok(int64_t stride, int64_t width) { return stride == 0 || (stride >= width && stride <= kMaxFeatures); }
 
+// A result in an operand's buffer lies where the operand does, element for element; otherwise one
+// block's rows would overwrite what another has yet to read.
+bool in_place_ok(const void* operand, const void* result, int64_t rows, int64_t ld_operand, int64_t ld_result) {
+  return operand == nullptr || operand != result || rows <= 1 || ld_operand == ld_result;
+}
+
 numbat_status check_linear(const numbat_linear_problem* p, bool fwd, LinearDesc* d) {
   if (p == nullptr) return fail(NUMBAT_ERR_NULL, "problem descriptor is NULL");
   if (p->struct_size != sizeof(numbat_linear_problem))
@@ -230,6 +236,9 @@ numbat_status numbat_linear_fwd(const numbat_linear_problem* p, const void* x, c
   if (x == nullptr || w == nullptr || y == nullptr) return fail(NUMBAT_ERR_NULL, "x, w and y are required");
   if (!aligned16(x) || !aligned16(w) || !aligned16(y) || !aligned16(residual) || !aligned16(z))
     return fail(NUMBAT_ERR_ALIGN, "x, w, y, residual and z must be 16-byte aligned");
+  if (!in_place_ok(residual, y, d.m, d.ldr, d.ldy))
+    return fail(NUMBAT_ERR_BAD_DESC, "y in the residual's buffer needs its row stride (y %lld, residual %lld)",
+                (long long)d.ldy, (long long)d.ldr);
   const Product pr = product(d, kGemmFwd);
   st = check_grid(pr);
   if (st != NUMBAT_OK) return st;
@@ -322,6 +331,9 @@ numbat_status numbat_layer_norm_fwd(const numbat_layer_norm_problem* p, const vo
   if (a.m == 0) return ok();
   if (x == nullptr || y == nullptr) return fail(NUMBAT_ERR_NULL, "x and y are required");
   if (!aligned16(x) || !aligned16(y)) return fail(NUMBAT_ERR_ALIGN, "x and y must be 16-byte aligned");
+  if (x == y && (a.x_f32 != a.y_f32 || !in_place_ok(x, y, a.m, a.ldx, a.ldy)))
+    return fail(NUMBAT_ERR_BAD_DESC, "y in x's buffer needs its type and row stride (y %lld, x %lld)", (long long)a.ldy,
+                (long long)a.ldx);
   a.vec = a.c % 8 == 0 && a.ldx % 8 == 0 && a.ldy % 8 == 0 && aligned16(gamma) && aligned16(beta);
   const hipError_t e = ln_fwd_launch(a, x, gamma, beta, y, mean, rstd, static_cast<hipStream_t>(stream));
   return e == hipSuccess ? ok() : hip_fail(e, "layer norm forward launch");
@@ -348,6 +360,9 @@ numbat_status numbat_layer_norm_bwd(const numbat_layer_norm_problem* p, const vo
   if (dx == nullptr && residual_grad != nullptr) return fail(NUMBAT_ERR_NULL, "residual_grad needs dx");
   if (!aligned16(dy) || !aligned16(x) || !aligned16(residual_grad) || !aligned16(dx))
     return fail(NUMBAT_ERR_ALIGN, "dy, x, residual_grad and dx must be 16-byte aligned");
+  if (!in_place_ok(residual_grad, dx, a.m, a.ldr, a.lddx))
+    return fail(NUMBAT_ERR_BAD_DESC, "dx in residual_grad's buffer needs its row stride (dx %lld, residual_grad %lld)",
+                (long long)a.lddx, (long long)a.ldr);
   st = check_ws(ws, ws_bytes, with_header(ln_bwd_ws(a)));
   if (st != NUMBAT_OK) return st;
   a.vec = a.c % 8 == 0 && a.ldx % 8 == 0 && a.ldy % 8 == 0 && (residual_grad == nullptr || a.ldr % 8 == 0) &&
