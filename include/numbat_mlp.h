@@ -135,6 +135,8 @@ typedef struct {
  *   c = 1, or with max_norm > 0:  min(1, max_norm / (norm + 1e-6)), norm the L2 norm of every gradient
  *   g = c grad;  m = beta1 m + (1 - beta1) g;  v = beta2 v + (1 - beta2) g^2
  *   w = w (1 - lr weight_decay) - lr / (1 - beta1^step) * m / (sqrt(v / (1 - beta2^step)) + eps)
+ * beta1, beta2: 0 or more, below 1; eps, and max_norm unless it is 0: at least 2^-126 (fp32's smallest
+ * normal number) and below 3e38.
  * tensors: DEVICE array of count (1 .. 1024) entries; groups: HOST array of ngroups (1 .. 8).
  * state_bits: 32 or 8.  In 8 bits the update uses the new moments before they are rounded; a
  * block whose unit would be below the smallest normal number is stored as zeros, and a v above

@@ -1,5 +1,6 @@
 // C ABI of the residual MLP block's operators (numbat_mlp.h): descriptor validation, workspace
 // layout and dispatch.  Every check runs before anything is enqueued.
+#include <cfloat>
 #include <cmath>
 #include <cstddef>
 #include <cstring>
@@ -392,10 +393,12 @@ numbat_status numbat_adamw_step(const numbat_adamw_tensor* tensors, int32_t coun
   if (state_bits != 32 && state_bits != 8) return fail(NUMBAT_ERR_UNSUPPORTED, "state_bits = %d: 32 or 8", state_bits);
   if (!(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0))
     return fail(NUMBAT_ERR_BAD_DESC, "beta1 and beta2 must be in [0, 1)");
-  if (!(eps > 0.0 && eps < 3.0e38)) return fail(NUMBAT_ERR_BAD_DESC, "eps must be positive and finite");
+  // (the kernels take both in fp32: an eps that is no normal number there has no finite reciprocal)
+  if (!((float)eps >= FLT_MIN && eps < 3.0e38))
+    return fail(NUMBAT_ERR_BAD_DESC, "eps must be at least 2^-126 and finite");
   if (step < 1) return fail(NUMBAT_ERR_BAD_DESC, "step = %lld: the first step is 1", (long long)step);
-  if (!(max_norm >= 0.0 && max_norm < 3.0e38))
-    return fail(NUMBAT_ERR_BAD_DESC, "max_norm must be positive and finite, or 0 for no clipping");
+  if (!(max_norm == 0.0 || ((float)max_norm >= FLT_MIN && max_norm < 3.0e38)))
+    return fail(NUMBAT_ERR_BAD_DESC, "max_norm must be at least 2^-126 and finite, or 0 for no clipping");
   if (total_norm != nullptr && max_norm == 0.0)
     return fail(NUMBAT_ERR_BAD_DESC, "total_norm is formed only with max_norm > 0");
   AdamArgs a;
