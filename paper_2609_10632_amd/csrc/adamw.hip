@@ -361,7 +361,11 @@ __device__ __forceinline__ void update_quad(const AdamArgs& a, const AdamTensor&
   // reciprocal, 1 ulp each)
   if constexpr (BITS == 32) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) root[e] = __builtin_amdgcn_sqrtf(v[e]);
+    for (int e = 0; e < 4; ++e) {
+      // (the hardware's root takes a v below the normal numbers for zero: scaled by powers of two, exact)
+      const bool small = v[e] < 0x1p-126f;
+      root[e] = __builtin_amdgcn_sqrtf(small ? v[e] * 0x1p48f : v[e]) * (small ? 0x1p-24f : 1.0f);
+    }
   } else {
     sqrt4(v, root);
   }
