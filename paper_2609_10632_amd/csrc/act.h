@@ -54,8 +54,9 @@ __device__ __forceinline__ float act_slope(float z, int act) {
       return __builtin_fmaf(z * kInvSqrt2Pi, e, z > 0.f ? 1.0f - q : q);
     }
     case kActGeluTanh: {
-      const float q = sigmoidf_fast(kGeluTanhA * z * __builtin_fmaf(kGeluTanhB * z, z, 1.0f));
-      return __builtin_fmaf(z * q * (1.0f - q), kGeluTanhA * __builtin_fmaf(3.0f * kGeluTanhB * z, z, 1.0f), q);
+      const float q = sigmoidf_fast(kGeluTanhA * z * __builtin_fmaf(kGeluTanhB * z, z, 1.0f)), p = z * q * (1.0f - q);
+      // (p is 0 long before z^2 passes fp32's range; its factor stays finite, so that the product is 0 too)
+      return __builtin_fmaf(p, kGeluTanhA * fminf(__builtin_fmaf(3.0f * kGeluTanhB * z, z, 1.0f), 1e38f), q);
     }
     case kActSilu: {
       const float q = sigmoidf_fast(z);
