@@ -51,7 +51,8 @@ typedef struct {
   int64_t x_row_stride;  /* x and dx */
   int64_t y_row_stride;  /* y and dy */
   int64_t r_row_stride;  /* residual */
-  int64_t z_row_stride;  /* z */
+  int64_t z_row_stride;  /* z: at least n in the forward, k in the data gradient (also where no z is given);
+                          * the weight gradient takes either's descriptor */
 } numbat_linear_problem;
 
 /* Layer norm over the c features of each of m rows. */

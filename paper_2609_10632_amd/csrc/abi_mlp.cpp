@@ -1,5 +1,6 @@
 // C ABI of the residual MLP block's operators (numbat_mlp.h): descriptor validation, workspace
 // layout and dispatch.  Every check runs before anything is enqueued.
+#include <algorithm>
 #include <cfloat>
 #include <cmath>
 #include <cstddef>
@@ -19,7 +20,7 @@ struct LinearDesc {
   int64_t m;
   int32_t n, k, act;
   bool y_f32;
-  int64_t ldx, ldy, ldr, ldz;  // ldz: 0 for dense (n wide in the forward, k in the backward)
+  int64_t ldx, ldy, ldr, ldz;  // z is n wide in the forward, k in the data gradient
 };
 
 bool stride_ok(int64_t stride, int64_t width) { return stride == 0 || (stride >= width && stride <= kMaxFeatures); }
@@ -30,7 +31,7 @@ bool in_place_ok(const void* operand, const void* result, int64_t rows, int64_t 
   return operand == nullptr || operand != result || rows <= 1 || ld_operand == ld_result;
 }
 
-numbat_status check_linear(const numbat_linear_problem* p, bool fwd, LinearDesc* d) {
+numbat_status check_linear(const numbat_linear_problem* p, GemmKind kind, LinearDesc* d) {
   if (p == nullptr) return fail(NUMBAT_ERR_NULL, "problem descriptor is NULL");
   if (p->struct_size != sizeof(numbat_linear_problem))
     return fail(NUMBAT_ERR_VERSION, "numbat_linear_problem.struct_size is %u, this library expects %zu", p->struct_size,
@@ -44,7 +45,8 @@ numbat_status check_linear(const numbat_linear_problem* p, bool fwd, LinearDesc*
   if (p->m > kMaxIndex || p->n > kMaxFeatures || p->k > kMaxFeatures)
     return fail(NUMBAT_ERR_UNSUPPORTED, "at most 2^31-1 rows and 2^21 features (m=%lld n=%d k=%d)", (long long)p->m, p->n,
                 p->k);
-  const int64_t zw = fwd ? p->n : p->k;
+  // (the weight gradient has no z: it takes the forward's descriptor and the data gradient's)
+  const int64_t zw = kind == kGemmFwd ? p->n : kind == kGemmDgrad ? p->k : std::min(p->n, p->k);
   if (!stride_ok(p->x_row_stride, p->k) || !stride_ok(p->y_row_stride, p->n) || !stride_ok(p->r_row_stride, p->n) ||
       !stride_ok(p->z_row_stride, zw))
     return fail(NUMBAT_ERR_BAD_DESC, "a row stride is smaller than its row or above 2^21 (x %lld y %lld r %lld z %lld)",
@@ -199,12 +201,13 @@ bool mlp_workspace_size(int op, const void* problem, size_t* bytes, numbat_statu
     case NUMBAT_OP_LINEAR_FWD:
     case NUMBAT_OP_LINEAR_BWD_DATA:
     case NUMBAT_OP_LINEAR_BWD_WEIGHT: {
+      const GemmKind kind = op == NUMBAT_OP_LINEAR_FWD        ? kGemmFwd
+                            : op == NUMBAT_OP_LINEAR_BWD_DATA ? kGemmDgrad
+                                                              : kGemmWgrad;
       LinearDesc d;
-      *st = check_linear(static_cast<const numbat_linear_problem*>(problem), op == NUMBAT_OP_LINEAR_FWD, &d);
+      *st = check_linear(static_cast<const numbat_linear_problem*>(problem), kind, &d);
       if (*st != NUMBAT_OK) return true;
-      const Product pr = product(d, op == NUMBAT_OP_LINEAR_FWD        ? kGemmFwd
-                                    : op == NUMBAT_OP_LINEAR_BWD_DATA ? kGemmDgrad
-                                                                      : kGemmWgrad);
+      const Product pr = product(d, kind);
       *st = check_grid(pr);
       if (*st != NUMBAT_OK) return true;
       *bytes = with_header(pr.bytes);
@@ -231,7 +234,7 @@ extern "C" {
 numbat_status numbat_linear_fwd(const numbat_linear_problem* p, const void* x, const void* w, const float* bias,
                                 const void* residual, void* z, void* y, void* ws, size_t ws_bytes, void* stream) {
   LinearDesc d;
-  numbat_status st = check_linear(p, true, &d);
+  numbat_status st = check_linear(p, kGemmFwd, &d);
   if (st != NUMBAT_OK) return st;
   if (d.m == 0) return ok();
   if (x == nullptr || w == nullptr || y == nullptr) return fail(NUMBAT_ERR_NULL, "x, w and y are required");
@@ -264,7 +267,7 @@ numbat_status numbat_linear_fwd(const numbat_linear_problem* p, const void* x, c
 numbat_status numbat_linear_bwd_data(const numbat_linear_problem* p, const void* dy, const void* w, const void* z,
                                      void* dx, int accumulate, void* ws, size_t ws_bytes, void* stream) {
   LinearDesc d;
-  numbat_status st = check_linear(p, false, &d);
+  numbat_status st = check_linear(p, kGemmDgrad, &d);
   if (st != NUMBAT_OK) return st;
   if (d.m == 0) return ok();
   if (dy == nullptr || w == nullptr || dx == nullptr) return fail(NUMBAT_ERR_NULL, "dy, w and dx are required");
@@ -293,7 +296,7 @@ numbat_status numbat_linear_bwd_data(const numbat_linear_problem* p, const void*
 numbat_status numbat_linear_bwd_weight(const numbat_linear_problem* p, const void* x, const void* dy, float* dw,
                                        float* db, int accumulate, void* ws, size_t ws_bytes, void* stream) {
   LinearDesc d;
-  numbat_status st = check_linear(p, false, &d);
+  numbat_status st = check_linear(p, kGemmWgrad, &d);
   if (st != NUMBAT_OK) return st;
   if (dw == nullptr || (d.m > 0 && (x == nullptr || dy == nullptr)))
     return fail(NUMBAT_ERR_NULL, "x, dy and dw are required");
