@@ -15,6 +15,7 @@
 #include "../../include/numbat_conv.h"
 #include "abi_util.h"
 #include "kernels.h"
+#include "mlp_kernels.h"
 
 using namespace numbat;
 

@@ -33,19 +33,7 @@ enum KernelClass {
   KC_OPT_SUMSQ,         // optimiser step: squared-norm partials of the gradients
   KC_OPT_UPDATE,        // optimiser step: clipped SGD-Nesterov update
   KC_POOL,              // SPPF max pool and neck upsampling, forward and backward
-  KC_COUNT,
-  // the kernels of numbat_mlp.h's functions, numbered apart
-  KC_MLP_FIRST = 64,
-  KC_LINEAR = KC_MLP_FIRST,  // linear layers: matrix products with their epilogues
-  KC_LINEAR_PACK,       // linear layers: operands with odd rows, padded
-  KC_LINEAR_FINISH,     // linear layers: sums of reduction ranges
-  KC_LINEAR_BIAS_GRAD,  // linear layers: bias gradient
-  KC_LN_FWD,            // layer norm forward
-  KC_LN_BWD,            // layer norm backward
-  KC_LN_BWD_FINISH,     // layer norm backward: gain and shift gradients
-  KC_ADAMW_NORM,        // AdamW: squared-norm partials of the gradients
-  KC_ADAMW,             // AdamW: update, and the values of 8-bit moments
-  KC_MLP_END
+  KC_COUNT
 };
 void trace_begin(int cls);
 void trace_end(int cls);

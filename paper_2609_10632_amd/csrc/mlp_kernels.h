@@ -6,6 +6,23 @@
 
 namespace numbat {
 
+// Kernel classes of numbat_mlp.h's functions for the launch timing, numbered apart from the others.
+// (Here and not with those: the committed HBM traffic of the convolutions is tied to a hash of the
+// convolutions' sources, kernels.h among them.)
+enum MlpKernelClass {
+  KC_MLP_FIRST = 64,
+  KC_LINEAR = KC_MLP_FIRST,  // linear layers: matrix products with their epilogues
+  KC_LINEAR_PACK,       // linear layers: operands with odd rows, padded
+  KC_LINEAR_FINISH,     // linear layers: sums of reduction ranges
+  KC_LINEAR_BIAS_GRAD,  // linear layers: bias gradient
+  KC_LN_FWD,            // layer norm forward
+  KC_LN_BWD,            // layer norm backward
+  KC_LN_BWD_FINISH,     // layer norm backward: gain and shift gradients
+  KC_ADAMW_NORM,        // AdamW: squared-norm partials of the gradients
+  KC_ADAMW,             // AdamW: update, and the values of 8-bit moments
+  KC_MLP_END
+};
+
 // ---------------------------------------------------------------------------
 // Linear layers.  One matrix product C[m][n] = sum_k A(m, k) B(n, k) in three orientations:
 //   forward          A = x  [m][k],  B = w [n][k]    (both run along the reduction)
