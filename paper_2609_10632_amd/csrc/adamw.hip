@@ -222,27 +222,6 @@ __device__ __forceinline__ uint32_t largest_of(const float (&f)[4]) {
   return x;
 }
 
-// IEEE square roots.  The hardware's is within one unit in the last place, so the rounded root is it
-// or a neighbour: s moves down where the midpoint below it is at or above the root, which is where
-// x - s (s - ulp) <= 0 (products and x are integers in units of ulp^2 / 4), and up likewise.  Below
-// 2^-96, where the hardware's root may flush, the library's.
-__device__ __forceinline__ void sqrt4(const float (&x)[4], float (&r)[4]) {
-  if (fminf(fminf(x[0], x[1]), fminf(x[2], x[3])) >= 0x1p-96f) {
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const float s = __builtin_amdgcn_sqrtf(x[e]);
-      const float lo = __uint_as_float(__float_as_uint(s) - 1u), hi = __uint_as_float(__float_as_uint(s) + 1u);
-      const float dlo = __builtin_fmaf(-lo, s, x[e]), dhi = __builtin_fmaf(-hi, s, x[e]);
-      float t = dlo <= 0.f ? lo : s;
-      t = dhi > 0.f ? hi : t;
-      r[e] = x[e] < INFINITY ? t : x[e];
-    }
-  } else {
-#pragma unroll
-    for (int e = 0; e < 4; ++e) r[e] = sqrtf(x[e]);
-  }
-}
-
 // Codes: rint(sqrt(x inv)) of the IEEE root, at most `most`, for four x >= 0.  The hardware's root
 // gives the same integer unless it lies next to a half; then, for about one wave in twenty, all four
 // are formed again from the library's.
@@ -367,7 +346,8 @@ __device__ __forceinline__ void update_quad(const AdamArgs& a, const AdamTensor&
       root[e] = __builtin_amdgcn_sqrtf(small ? v[e] * 0x1p48f : v[e]) * (small ? 0x1p-24f : 1.0f);
     }
   } else {
-    sqrt4(v, root);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) root[e] = sqrtf(v[e]);
   }
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
