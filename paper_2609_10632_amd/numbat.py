@@ -412,12 +412,15 @@ def adamw_table(entries):
     """numbat_adamw_tensor entries as bytes laid out like the C array (upload them to the device
     to pass as `tensors`).  Each entry is a dict of the tensors ``w``, ``grad``, ``m``, ``v`` and the
     ``group``; with 8-bit state ``m_unit`` and ``v_unit``; ``w_copy`` where a bf16 copy is wanted.
-    The gradient's type is its tensor's, fp32 or bf16 (TypeError)."""
+    The gradient's type is its tensor's, fp32 or bf16 (TypeError); 8-bit moments without units are a
+    ValueError, as the kernels would follow the missing pointers."""
     types = {"torch.float32": F32, "torch.bfloat16": BF16}
     arr = (numbat_adamw_tensor * len(entries))()
     for e, d in zip(arr, entries):
         if str(d["grad"].dtype) not in types:
             raise TypeError(f"adamw_table: a gradient of {d['grad'].dtype}, expected float32 or bfloat16")
+        if str(getattr(d["m"], "dtype", "")) == "torch.int8" and (d.get("m_unit") is None or d.get("v_unit") is None):
+            raise ValueError("adamw_table: 8-bit moments need m_unit and v_unit")
         for f in ("w", "grad", "m", "v", "m_unit", "v_unit", "w_copy"):
             setattr(e, f, _ptr(d.get(f)))
         e.n, e.group = d["w"].numel(), d["group"]

@@ -37,3 +37,9 @@ def test_entries(bits):
 def test_gradients_of_other_types(dtype):
     with pytest.raises(TypeError):
         nb.adamw_table([entry(), entry(grad=dtype)])
+
+
+@pytest.mark.parametrize("unit", ("m_unit", "v_unit"))
+def test_8_bit_moments_without_units(unit):
+    with pytest.raises(ValueError):
+        nb.adamw_table([entry(bits=8, **{unit: None})])
