@@ -51,3 +51,21 @@ def test_a_forward_that_fails_keeps_nothing(block, monkeypatch):
         block.forward(rows(10))
     with pytest.raises(RuntimeError):
         block.backward(rows(10), rows(10))
+
+
+def test_a_step_that_is_refused_is_not_counted(block, monkeypatch):
+    took = []
+    monkeypatch.setattr(mlp.nb, "numbat_adamw_step", lambda *a, **k: took.append(a[7]))
+    block.step(1e-3)
+
+    def refuse(*a, **k):
+        raise mlp.nb.NumbatError(mlp.nb.ERR_BAD_DESC, "bad", "detail", "numbat_adamw_step")
+
+    block.forward(rows(10))
+    with monkeypatch.context() as m:
+        m.setattr(mlp.nb, "numbat_adamw_step", refuse)
+        with pytest.raises(mlp.nb.NumbatError):
+            block.step(float("nan"))
+    block.backward(rows(10), rows(10))  # nor has it changed the weights
+    block.step(1e-3)
+    assert took == [1, 2]  # the bias corrections go by the steps taken
