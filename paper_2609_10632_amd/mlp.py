@@ -146,13 +146,13 @@ class MlpBlock:
         return self.dx[:rows]
 
     def step(self, lr, weight_decay=0.1, betas=(0.9, 0.95), eps=1e-8, max_norm=1.0):
-        """One AdamW step from ``grads``; returns the device float that receives the gradients' norm
-        (with max_norm > 0)."""
+        """One AdamW step from ``grads``; returns the device float that receives the gradients'
+        norm, or None with max_norm = 0, which forms none."""
         nb.numbat_adamw_step(self.table, self.count, ((lr, weight_decay), (lr, 0.0)), self.state_bits, betas[0],
                              betas[1], eps, self.steps + 1, max_norm, self.norm if max_norm > 0 else None, self.ws)
         self.steps += 1
         self.kept = None
-        return self.norm
+        return self.norm if max_norm > 0 else None
 
 
 def main(argv=None):

@@ -69,3 +69,8 @@ def test_a_step_that_is_refused_is_not_counted(block, monkeypatch):
     block.backward(rows(10), rows(10))  # nor has it changed the weights
     block.step(1e-3)
     assert took == [1, 2]  # the bias corrections go by the steps taken
+
+
+def test_a_step_without_a_clip_has_no_norm(block):
+    assert block.step(1e-3, max_norm=1.0) is block.norm
+    assert block.step(1e-3, max_norm=0.0) is None  # not that of an earlier step
