@@ -110,8 +110,12 @@ class MlpBlock:
         """x: bf16 [rows][width], rows as far apart as its stride says (``map[..., a:b].flatten(0, 2)``
         of an NHWC map).  keep: for backward(); without, as in serving, neither z nor the norm's
         statistics are written, and backward() refuses what an earlier forward has kept, as other
-        activations are overwritten.  Returns a view of the block's output buffer."""
+        activations are overwritten.  Returns a view of the block's output buffer, which x may
+        be only without keep."""
         rows, stride = self._check(x, "x")
+        if rows and x.untyped_storage().data_ptr() == self.y.untyped_storage().data_ptr():
+            if keep or x.data_ptr() != self.y.data_ptr():
+                raise ValueError("x: lies in the block's own output, which this forward overwrites")
         self.kept = None
         up, down, _, ln = self._problems(rows, stride, self.width)
         ws = self._workspace((nb.OP_LINEAR_FWD, up), (nb.OP_LINEAR_FWD, down))

@@ -74,3 +74,18 @@ def test_a_step_that_is_refused_is_not_counted(block, monkeypatch):
 def test_a_step_without_a_clip_has_no_norm(block):
     assert block.step(1e-3, max_norm=1.0) is block.norm
     assert block.step(1e-3, max_norm=0.0) is None  # not that of an earlier step
+
+
+def test_a_forward_over_its_own_output_keeps_nothing(block):
+    """Its last call writes y over the rows that a backward would read as x."""
+    y = block.forward(rows(10))
+    with pytest.raises(ValueError):
+        block.forward(y)
+    with pytest.raises(ValueError):
+        block.forward(y[2:7])
+    block.forward(y, keep=False)  # serving: nothing reads x afterwards
+    with pytest.raises(ValueError):
+        block.forward(y[2:7], keep=False)  # but each row of it has to lie where its result goes
+    mlp.MlpBlock(0, 16, 32, device="cpu").forward(rows(0))
+    block.forward(y.clone())
+    block.backward(rows(10), rows(10))
