@@ -75,6 +75,9 @@ typedef struct {
  * x, w: bf16; bias: fp32 [n] or NULL; residual: [m][n] of y's type or NULL; z: bf16 [m][n] or
  * NULL (what the backward of act reads); y: y_type.  y may be the residual's buffer if their strides
  * agree (NUMBAT_ERR_BAD_DESC otherwise).
+ * Activations take the hardware's reciprocal and exponential, and GELU a polynomial for erf: within
+ * 2^-20 of |t|.  Relative to y, GELU's tail is off by up to 5e-4 below t = -3, 4e-3 at t = -6 and 3e-2
+ * at t = -12 (y of -4e-3, -6e-9 and -2e-32).
  * ws: numbat_workspace_size(NUMBAT_OP_LINEAR_FWD), which may be 0. */
 numbat_status numbat_linear_fwd(const numbat_linear_problem* p, const void* x, const void* w, const float* bias,
                                 const void* residual, void* z, void* y, void* ws, size_t ws_bytes, void* stream);
@@ -108,7 +111,8 @@ numbat_status numbat_layer_norm_fwd(const numbat_layer_norm_problem* p, const vo
  *   dx = rstd (h - sum_c h / c - xh sum_c(h xh) / c) + residual_grad
  *   dgamma = sum_rows dy xh,  dbeta = sum_rows dy          (fp32 [c]; accumulate: added)
  * gamma NULL: 1.  residual_grad [m][c] or NULL: the gradient that reaches x around the norm; dx
- * may be its buffer if their strides agree (NUMBAT_ERR_BAD_DESC otherwise).  Each of dx, dgamma, dbeta may be NULL where it is not wanted.
+ * may be its buffer if their strides agree (NUMBAT_ERR_BAD_DESC otherwise).  Each of dx, dgamma,
+ * dbeta may be NULL where it is not wanted; the workspace is required all the same.
  * ws: numbat_workspace_size(NUMBAT_OP_LAYER_NORM_BWD). */
 numbat_status numbat_layer_norm_bwd(const numbat_layer_norm_problem* p, const void* dy, const void* x,
                                     const float* mean, const float* rstd, const float* gamma,
@@ -141,9 +145,12 @@ typedef struct {
  * tensors: DEVICE array of count (1 .. 1024) entries; groups: HOST array of ngroups (1 .. 8).
  * state_bits: 32 or 8.  In 8 bits the update uses the new moments before they are rounded; a
  * block whose unit would be below the smallest normal number is stored as zeros, and a v above
- * zero never rounds to zero within its block; a moment that is not finite takes the largest code.  total_norm: NULL, or a device float that receives
- * the norm (only with max_norm > 0).  Of a gradient that is not finite: a NaN norm
- * does not clip, an infinite one gives c = 0 (its infinite elements then become NaN).
+ * zero never rounds to zero within its block; a moment that is not finite takes the largest code.
+ * The step's reciprocal, and with 32-bit state its root, are the hardware's, good to one unit in the
+ * last place each; moments, units and codes are formed by IEEE operations.
+ * total_norm: NULL, or a device float that receives the norm (only with max_norm > 0).  Of a
+ * gradient that is not finite: a NaN norm does not clip, an infinite one gives c = 0 (its infinite
+ * elements then become NaN).
  * ws: numbat_workspace_size(NUMBAT_OP_ADAMW), problem ignored. */
 numbat_status numbat_adamw_step(const numbat_adamw_tensor* tensors, int32_t count, const numbat_sgd_group* groups,
                                 int32_t ngroups, int32_t state_bits, double beta1, double beta2, double eps,

@@ -18,9 +18,9 @@
 // reduction; 4096-element chunks of all tensors are numbered in table order and dealt to thread
 // blocks in contiguous ranges.  A thread loads everything of its four rounds of a whole, aligned
 // chunk before it computes any of it.  Bound by the bytes, read and written: 30 per element with fp32
-// moments, gradients and a bf16 copy (25.9 million elements of 243 tensors 142 us, 5.5 TB/s; the norm's
-// pass over 104 MB of gradients 38 us, what reading alone reaches here), 16 with 8-bit moments and bf16
-// gradients (134 million 463 us, 4.6 TB/s).
+// moments, gradients and a bf16 copy (25.9 million elements of 243 tensors 143 us, 5.5 TB/s; the norm's
+// pass over 104 MB of gradients 32 to 38 us, what reading alone reaches here), 16 with 8-bit moments and bf16
+// gradients (134 million 470 us, 4.6 TB/s).
 #include <type_traits>
 
 #include "mlp_kernels.h"

@@ -13,11 +13,11 @@
 // m, which the epilogue stages through LDS with 16-byte writes and stores as rows.
 //
 // Per step a block reads (BM + BN) * BK * 2 bytes of operands and issues BM * BN * BK
-// multiply-adds: a 256 x 256 tile needs 1/64 byte per flop, which the L2s deliver at the
+// multiply-adds: a 256 x 256 tile needs 1/64 byte per multiply-add, which the L2s deliver at the
 // matrix cores' rate; what bounds long reductions is the matrix cores, short ones (maps of
-// few channels) the bytes of x, z and y.  8192 rows, 4096 -> 16384 with GELU and z: 976 us, 1126 TFLOP/s
+// few channels) the bytes of x, z and y.  8192 rows, 4096 -> 16384 with GELU and z: 973 us, 1130 TFLOP/s
 // (without an epilogue's work 1195; dx 1130, dw 1340; the largest library product of this card reaches
-// 1385); 102400 rows, 192 -> 768 with SiLU and z: 81 us, 4.4 TB/s of 5.1.
+// 1395); 102400 rows, 192 -> 768 with SiLU and z: 80 us, 4.4 TB/s of 5.1.
 #include <algorithm>
 #include <cmath>
 

@@ -8,7 +8,6 @@ namespace numbat {
 
 namespace {
 
-// The epilogue on NV consecutive columns of one row (NV = 8: 16-byte accesses, or 1).
 // A vector of columns whose row starts at any element: unaligned 16-byte accesses, which the hardware
 // splits where they cross a line.
 struct __attribute__((packed, aligned(2))) AnyVec {

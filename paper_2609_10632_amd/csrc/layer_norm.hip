@@ -4,7 +4,9 @@
 //             dgamma = sum_rows dy xh,  dbeta = sum_rows dy
 // A row belongs to a group of G lanes (part of a wave, a wave, or a block of waves) which keeps
 // it in registers: one pass over memory, the mean first and the variance from the centred values
-// (no cancellation).  Lanes hold 16-byte vectors where the rows allow them and single elements
+// (no cancellation).  (The backward of 8193 to 16384 features, whose 1024 threads have 128 registers
+// each, spills 60 to 188 bytes a lane in its loop; of 4097 to 8192 those of bf16 x with fp32 y, 28, and of
+// fp32 x with odd rows, 8 or 16.)  Lanes hold 16-byte vectors where the rows allow them and single elements
 // otherwise; a lane's columns are the same for every row, so the backward adds dgamma and dbeta in
 // registers over all rows of a block and writes one partial per block, which a second kernel sums
 // in a fixed order.  Everything is bound by the bytes of the rows: gradients of 102400 x 192 bf16 with the

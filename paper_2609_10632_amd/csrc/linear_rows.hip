@@ -2,8 +2,9 @@
 //   y[m][n] = epilogue(sum_k x[m][k] w[n][k]),  m at most 16.
 // Bound by the bytes of w, which every launch reads once (one row of 2048 -> 8192 in 8.0 us: 34 MB at
 // 4.2 TB/s with the launch in it, where a large copy moves 5.1 TB/s).  A block takes 16 rows of w and its waves
-// split the reduction, so that all 256 CUs stream w even for narrow layers and each wave has
-// 4 x 2 KiB of it in flight; the matrix core multiplies 16 rows of w by 16 rows of x per
+// split the reduction, each with 4 x 2 KiB of it in flight.  Layers below 4096 outputs have fewer
+// blocks than there are CUs and fall short of that (one row of 8192 -> 1024 on 64 blocks 11.1 us, 3.3
+// us of bytes); the reduction is not split over blocks.  The matrix core multiplies 16 rows of w by 16 rows of x per
 // instruction (a 16 x 16 x 32 product, most of it idle for one token: the arithmetic is free here).
 // The reduction's order within a 64-element step is chosen for the loads: a lane takes 16
 // consecutive k of its row, so a step reads whole 128-byte lines.  x comes from the L2 straight into

@@ -32,7 +32,9 @@ class MlpBlock:
     """A block of `width` features, widened to `hidden`, and the buffers of steps of up to `rows` rows.
 
     Parameters (fp32, views of one flat buffer): ``w1`` [hidden][width], ``b1``, ``w2``
-    [width][hidden], ``b2``, ``gamma``, ``beta``; gradients of the same names in ``grads``."""
+    [width][hidden], ``b2``, ``gamma``, ``beta``; gradients of the same names in ``grads``.  The
+    products read the bf16 ``copies`` of ``w1`` and ``w2``, which step() writes: who writes parameters by
+    hand (a checkpoint's) writes those too."""
 
     def __init__(self, rows, width, hidden, act="gelu", eps=1e-5, state_bits=32, seed=0, device=DEV):
         self.rows, self.width, self.hidden, self.eps, self.device = rows, width, hidden, eps, device
