@@ -81,7 +81,13 @@ typedef enum {
   NUMBAT_OP_LINEAR_BWD_DATA = 8,
   NUMBAT_OP_LINEAR_BWD_WEIGHT = 9,
   NUMBAT_OP_LAYER_NORM_BWD = 10,
-  NUMBAT_OP_ADAMW = 11
+  NUMBAT_OP_ADAMW = 11,
+  /* the functions of numbat_attention.h (problem: a numbat_group_norm_problem* or a
+   * numbat_attention_problem*) */
+  NUMBAT_OP_GROUP_NORM_FWD = 12,
+  NUMBAT_OP_GROUP_NORM_BWD = 13,
+  NUMBAT_OP_ATTENTION_FWD = 14,
+  NUMBAT_OP_ATTENTION_BWD = 15
 } numbat_op;
 
 /* One 2-D convolution (dilation 1, one group).  Output size

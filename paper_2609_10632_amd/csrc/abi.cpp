@@ -15,6 +15,7 @@
 #include "../../include/numbat_conv.h"
 #include "abi_util.h"
 #include "kernels.h"
+#include "attention_kernels.h"
 #include "mlp_kernels.h"
 
 using namespace numbat;
@@ -55,10 +56,14 @@ const char* const kClassNames[KC_COUNT] = {
 const char* const kMlpClassNames[KC_MLP_END - KC_MLP_FIRST] = {
     "linear", "linear_pack", "linear_finish", "linear_bias_grad", "layer_norm_fwd", "layer_norm_bwd",
     "layer_norm_bwd_finish", "adamw_norm", "adamw"};
+const char* const kAttentionClassNames[KC_ATTENTION_END - KC_ATTENTION_FIRST] = {
+    "group_norm_stats", "group_norm_fwd", "group_norm_bwd_sums", "group_norm_bwd", "group_norm_bwd_finish", "rotary",
+    "attention_fwd", "attention_join", "attention_bwd_rows", "attention_bwd"};
 
 const char* class_name(int c) {
   if (c >= 0 && c < KC_COUNT) return kClassNames[c];
-  return c >= KC_MLP_FIRST && c < KC_MLP_END ? kMlpClassNames[c - KC_MLP_FIRST] : nullptr;
+  if (c >= KC_MLP_FIRST && c < KC_MLP_END) return kMlpClassNames[c - KC_MLP_FIRST];
+  return c >= KC_ATTENTION_FIRST && c < KC_ATTENTION_END ? kAttentionClassNames[c - KC_ATTENTION_FIRST] : nullptr;
 }
 
 }  // namespace
@@ -750,7 +755,7 @@ numbat_status numbat_workspace_size(numbat_op op, const void* problem, size_t* b
     }
     default: {
       numbat_status st;
-      if (mlp_workspace_size(op, problem, bytes, &st)) return st;
+      if (mlp_workspace_size(op, problem, bytes, &st) || attention_workspace_size(op, problem, bytes, &st)) return st;
     }
   }
   return fail(NUMBAT_ERR_BAD_DESC, "unknown op %d", (int)op);

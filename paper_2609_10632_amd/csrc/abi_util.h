@@ -30,5 +30,7 @@ constexpr int64_t kMaxIndex = (1ll << 31) - 1;
 
 // numbat_workspace_size of the ops of numbat_mlp.h; false for another op
 bool mlp_workspace_size(int op, const void* problem, size_t* bytes, numbat_status* st);
+// and of numbat_attention.h
+bool attention_workspace_size(int op, const void* problem, size_t* bytes, numbat_status* st);
 
 }  // namespace numbat

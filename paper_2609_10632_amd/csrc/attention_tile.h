@@ -1,0 +1,253 @@
+// What the attention kernels share: tiles of rows of one head in LDS, the matrix instructions' operands
+// out of them, and the stores of their results.
+//
+// A tile has 64 rows (keys, or queries) of DP features, d rounded up, zeros past d and past the rows that
+// count.  It is loaded by direct-to-LDS loads and read in two ways: along the features, 16 bytes a lane
+// (a product that sums over features), and across them, four rows of one feature a lane, by transposing
+// reads (a product that sums over the rows).  The second kind meets the accumulators of a 32 x 32 product as
+// they are: a lane holds rows 8 j + 4 h + 0..3 of its column, h = lane / 32, and so a slice of 16 rows
+// of the next product takes rows 4 h + 0..3 and 8 + 4 h + 0..3 of both operands.  Weights never leave
+// their registers.
+#pragma once
+
+#include "attention_kernels.h"
+
+namespace numbat {
+
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr uint32_t kOob = 0x80000000u;  // a buffer offset past every range: zeros are loaded
+constexpr int kRecords = 0x7ffffff0;
+constexpr int kTile = 64;               // rows of a tile
+
+typedef __attribute__((address_space(3))) void lds_void_t;
+typedef short v4s_t __attribute__((ext_vector_type(4)));
+typedef unsigned v2u_t __attribute__((ext_vector_type(2)));
+typedef __attribute__((address_space(3))) v4s_t lds_v4s_t;
+
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rsrc(const void* base) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), (short)0, kRecords, 0x00020000);
+}
+
+// A lane's 16-byte chunk c of row r lies in slot c ^ swizzle(r) of the row.  Reading along the features, 16
+// consecutive rows take one chunk each: the swizzle (with the row's place in the 256 bytes of the
+// banks) spreads them over all 16 chunk positions.  Reading across, 4 consecutive rows take four
+// neighbouring chunks each: the swizzle's upper bits differ among them.
+template <int DP>
+struct Head {
+  static constexpr int KS = DP / 16, FB = DP / 32;                   // slices of 16 and blocks of 32 features
+  static constexpr int CPR = DP <= 32 ? 4 : DP <= 64 ? 8 : 16;       // chunks of a stored row
+  static constexpr int ROW = CPR * 16, TILE = kTile * ROW;           // bytes
+  static __device__ __forceinline__ int swizzle(int r) {
+    if constexpr (CPR == 16) return (r & 3) << 2 | (r >> 2 & 3);
+    else if constexpr (CPR == 8) return (r >> 1 & 1) << 2 | (r >> 2 & 3);
+    else return r >> 2 & 3;
+  }
+};
+
+// loads of a tile, shared by NW waves
+template <int DP, int NW>
+struct TileLoad {
+  using H = Head<DP>;
+  static constexpr int N = H::TILE / 1024 / NW;  // load instructions of a wave
+  static_assert(H::TILE % (1024 * NW) == 0, "whole load instructions");
+  uint32_t off[N];  // this lane's bytes from the tile's first row, kOob past d
+  __device__ __forceinline__ static int row(int q, int wave, int lane) { return ((q * NW + wave) * 64 + lane) / H::CPR; }
+  __device__ __forceinline__ static int chunk(int q, int wave, int lane) {
+    return lane % H::CPR ^ H::swizzle(row(q, wave, lane));
+  }
+  __device__ __forceinline__ void init(int64_t ld, int d, int wave, int lane) {
+#pragma unroll
+    for (int q = 0; q < N; ++q) {
+      const int c = chunk(q, wave, lane);
+      off[q] = c * 8 < d ? (uint32_t)(row(q, wave, lane) * ld * 2) + c * 16 : kOob;
+    }
+  }
+  // `left` rows of the tile count
+  __device__ __forceinline__ void load(unsigned char* tile, const bf16_t* base, int left, int wave, int lane) const {
+    const auto r = rsrc(base);
+#pragma unroll
+    for (int q = 0; q < N; ++q)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void_t*)(tile + (q * NW + wave) * 1024), 16,
+                                               row(q, wave, lane) < left ? off[q] : kOob, 0, 0, 0);
+  }
+};
+
+// The wave's loads have landed and its reads are done, and so are the block's other waves'.  (By builtins: the
+// compiler does not see a wait inside assembly and would wait for the next stage's loads as well.)
+__device__ __forceinline__ void stage_ready() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0x0070);  // vmcnt(0) lgkmcnt(0)
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
+// operand rows of 32 along the features
+template <int DP>
+struct Along {
+  using H = Head<DP>;
+  uint32_t at[H::KS];
+  __device__ __forceinline__ void init(int lane) {
+    const int r = lane & 31;
+#pragma unroll
+    for (int k = 0; k < H::KS; ++k) at[k] = r * H::ROW + ((2 * k + (lane >> 5)) ^ H::swizzle(r)) * 16;
+  }
+  __device__ __forceinline__ u32x4 read(const unsigned char* tile, int block, int k) const {
+    return *reinterpret_cast<const u32x4*>(tile + at[k] + block * 32 * H::ROW);
+  }
+};
+
+// 32 features across 16 rows, in the accumulators' order of rows
+template <int DP>
+struct Across {
+  using H = Head<DP>;
+  uint32_t at[H::FB][2];
+  __device__ __forceinline__ void init(int lane) {
+    // lanes of 16 read 4 rows x 16 features: lane 4 e + q of them 4 features of row e
+    const int g = lane >> 4, e = lane >> 2 & 3, q = lane & 3;
+#pragma unroll
+    for (int f = 0; f < H::FB; ++f)
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const int r = 8 * u + 4 * (g >> 1) + e, c = 4 * f + 2 * (g & 1) + (q >> 1);
+        at[f][u] = r * H::ROW + (c ^ H::swizzle(r)) * 16 + (q & 1) * 8;
+      }
+  }
+  __device__ __forceinline__ u32x4 read(const unsigned char* tile, int f, int slice) const {
+    const v2u_t lo = __builtin_bit_cast(
+        v2u_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s_t*)(tile + at[f][0] + slice * 16 * H::ROW)));
+    const v2u_t hi = __builtin_bit_cast(
+        v2u_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s_t*)(tile + at[f][1] + slice * 16 * H::ROW)));
+    return u32x4{lo.x, lo.y, hi.x, hi.y};
+  }
+};
+
+// slice s (16 rows) of a 32 x 32 product's accumulators as an operand
+__device__ __forceinline__ u32x4 operand(const f32x16& x, int s) {
+  return u32x4{pack2(x[8 * s], x[8 * s + 1]), pack2(x[8 * s + 2], x[8 * s + 3]), pack2(x[8 * s + 4], x[8 * s + 5]),
+               pack2(x[8 * s + 6], x[8 * s + 7])};
+}
+
+__device__ __forceinline__ f32x16 zeros16() {
+  f32x16 x;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) x[i] = 0.f;
+  return x;
+}
+
+// a lane's 16 bytes of a row of d features in memory: features 16 k + 8 h .. + 7
+__device__ __forceinline__ u32x4 row_chunk(const bf16_t* row, bool valid, int d, int k, int half) {
+  const int c = 16 * k + 8 * half;
+  return valid && c < d ? *reinterpret_cast<const u32x4*>(row + c) : u32x4{0, 0, 0, 0};
+}
+
+// the other half wave's value beside one's own, in the halves' order
+__device__ __forceinline__ v2u_t both_halves(uint32_t x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+  return v2u_t{r[0], r[1]};
+}
+__device__ __forceinline__ float half_max(float x) {
+  const v2u_t r = both_halves(__float_as_uint(x));
+  return fmaxf(__uint_as_float(r.x), __uint_as_float(r.y));
+}
+__device__ __forceinline__ float half_sum(float x) {
+  const v2u_t r = both_halves(__float_as_uint(x));
+  return __uint_as_float(r.x) + __uint_as_float(r.y);
+}
+
+// Stores the lane's column of DP / 32 accumulators, times `by`, as a row of d bf16 features.  A lane has 4
+// of every 8 features; the halves trade them so that each stores 8.
+template <int FB>
+__device__ __forceinline__ void store_row(bf16_t* row, bool valid, int d, const f32x16 (&x)[FB], float by, int half) {
+#pragma unroll
+  for (int f = 0; f < FB; ++f)
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const int i = 8 * j;
+      const uint32_t a0 = pack2(x[f][i] * by, x[f][i + 1] * by), a1 = pack2(x[f][i + 2] * by, x[f][i + 3] * by);
+      const uint32_t b0 = pack2(x[f][i + 4] * by, x[f][i + 5] * by), b1 = pack2(x[f][i + 6] * by, x[f][i + 7] * by);
+      const auto r0 = __builtin_amdgcn_permlane32_swap(a0, b0, false, false);
+      const auto r1 = __builtin_amdgcn_permlane32_swap(a1, b1, false, false);
+      const int c = 32 * f + 16 * j + 8 * half;
+      if (valid && c < d) *reinterpret_cast<u32x4*>(row + c) = u32x4{r0[0], r1[0], r0[1], r1[1]};
+    }
+}
+// the same as fp32 (dense rows of d, a multiple of 8)
+template <int FB>
+__device__ __forceinline__ void store_part(float* row, bool valid, int d, const f32x16 (&x)[FB], float by, int half) {
+#pragma unroll
+  for (int f = 0; f < FB; ++f)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int c = 32 * f + 8 * j + 4 * half;
+      if (valid && c < d)
+        *reinterpret_cast<f32x4*>(row + c) =
+            f32x4{x[f][4 * j] * by, x[f][4 * j + 1] * by, x[f][4 * j + 2] * by, x[f][4 * j + 3] * by};
+    }
+}
+
+// A sequence's numbers of queries and keys that count
+struct Lengths {
+  int q, kv;
+  __device__ __forceinline__ Lengths(const AttnArgs& a, int b) {
+    q = a.q_lengths != nullptr ? min(max(a.q_lengths[b], 0), a.q_len) : a.q_len;
+    kv = a.kv_lengths != nullptr ? min(max(a.kv_lengths[b], 0), a.kv_len) : a.kv_len;
+  }
+  // keys that query r sees
+  __device__ __forceinline__ int keys(const AttnArgs& a, int r) const {
+    return a.causal ? min(max(r + (kv - q) + 1, 0), kv) : kv;
+  }
+};
+
+// a block's place: which sequence and head of k and v, which range (split), which tile
+struct AttnGrid {
+  int32_t tiles, splits, per_split;  // of columns, or of keys; per_split: rows of a range of the other, a multiple of kTile
+  FastDiv div_tiles, div_splits, div_heads;
+  uint32_t blocks;
+};
+struct AttnPlace {
+  int b, h, split, tile;
+  __device__ __forceinline__ AttnPlace(const AttnArgs& a, const AttnGrid& g) {
+    // neighbouring blocks read the same k and v (or q and dy): a run of them to each XCD's L2
+    uint32_t t = xcd_remap(blockIdx.x, gridDim.x);
+    const uint32_t u = fdiv(t, g.div_tiles);
+    tile = t - u * g.tiles;
+    const uint32_t w = fdiv(u, g.div_splits);
+    split = u - w * g.splits;
+    b = fdiv(w, g.div_heads);
+    h = w - b * a.kv_heads;
+  }
+};
+
+// tiles * splits * sequences * heads; ranges where there would be fewer blocks than `want`, of `least` rows at least
+inline AttnGrid make_attn_grid(const AttnArgs& a, int64_t tiles, int64_t rows, int64_t want, int64_t least) {
+  AttnGrid g;
+  const int64_t base = std::max<int64_t>(1, (int64_t)a.batch * a.kv_heads * tiles);
+  const int64_t splits = std::clamp<int64_t>(want / base, 1, std::max<int64_t>(1, rows / least));
+  int64_t per = (rows + splits - 1) / splits;
+  per = std::max<int64_t>(kTile, (per + kTile - 1) / kTile * kTile);
+  g.per_split = (int32_t)std::min<int64_t>(per, 1 << 30);
+  g.splits = (int32_t)std::max<int64_t>(1, (rows + per - 1) / per);
+  g.tiles = (int32_t)tiles;
+  g.div_tiles = make_fastdiv((uint32_t)std::max<int64_t>(1, tiles));
+  g.div_splits = make_fastdiv((uint32_t)g.splits);
+  g.div_heads = make_fastdiv((uint32_t)a.kv_heads);
+  g.blocks = (uint32_t)std::min<int64_t>((int64_t)a.batch * a.kv_heads * tiles * g.splits, 0xffffffffll);
+  return g;
+}
+
+// f(DP) for the narrowest head that holds d features
+template <typename F>
+void with_head(int d, F&& f) {
+  if (d <= 32) f(std::integral_constant<int, 32>{});
+  else if (d <= 64) f(std::integral_constant<int, 64>{});
+  else if (d <= 96) f(std::integral_constant<int, 96>{});
+  else f(std::integral_constant<int, 128>{});
+}
+
+constexpr int64_t kMaxBlocks = (1ll << 32) / 256 - 1;  // of 256 threads in a launch
+
+}  // namespace
+
+}  // namespace numbat

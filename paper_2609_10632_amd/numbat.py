@@ -1,5 +1,5 @@
-"""Thin Python binding of the C ABI in ``include/numbat_conv.h`` and ``include/numbat_mlp.h``
-(argument marshalling only).
+"""Thin Python binding of the C ABI in ``include/numbat_conv.h``, ``include/numbat_mlp.h`` and
+``include/numbat_attention.h`` (argument marshalling only).
 
 Every function here has the name of the C entry point it calls and does nothing but
 turn Python arguments into C arguments: tensors become device pointers (their
@@ -22,10 +22,12 @@ NUMBAT_ABI_VERSION = 1
 OK, ERR_NULL, ERR_BAD_DESC, ERR_UNSUPPORTED, ERR_ALIGN, ERR_WORKSPACE, ERR_DEVICE, ERR_VERSION = range(8)
 (OP_CONV_FWD, OP_CONV_BWD_DATA, OP_CONV_BWD_WEIGHT, OP_BN_SILU_FWD, OP_BN_SILU_BWD, OP_CLIP_SGD_NESTEROV,
  OP_CONV_BWD_DATA_BN_SILU, OP_LINEAR_FWD, OP_LINEAR_BWD_DATA, OP_LINEAR_BWD_WEIGHT, OP_LAYER_NORM_BWD,
- OP_ADAMW) = range(12)
+ OP_ADAMW, OP_GROUP_NORM_FWD, OP_GROUP_NORM_BWD, OP_ATTENTION_FWD, OP_ATTENTION_BWD) = range(16)
 BF16, F32 = range(2)
 MLP_KERNEL_CLASSES = range(64, 64 + 9)
+ATTENTION_KERNEL_CLASSES = range(96, 96 + 10)
 ACT_NONE, ACT_RELU, ACT_GELU, ACT_GELU_TANH, ACT_SILU = range(5)
+ROTARY_HALVES, ROTARY_PAIRS = range(2)
 
 EXPORTED = (
     "numbat_abi_version", "numbat_last_error", "numbat_status_string", "numbat_conv_output_shape",
@@ -39,6 +41,9 @@ EXPORTED = (
 EXPORTED_MLP = (
     "numbat_linear_fwd", "numbat_linear_bwd_data", "numbat_linear_bwd_weight", "numbat_layer_norm_fwd",
     "numbat_layer_norm_bwd", "numbat_adamw_step", "numbat_adamw_state_values",
+)
+EXPORTED_ATTENTION = (
+    "numbat_group_norm_fwd", "numbat_group_norm_bwd", "numbat_rotary", "numbat_attention_fwd", "numbat_attention_bwd",
 )
 
 
@@ -92,6 +97,29 @@ class numbat_adamw_tensor(ctypes.Structure):
                 ("n", ctypes.c_int64), ("group", ctypes.c_int32), ("grad_type", ctypes.c_int32)]
 
 
+class numbat_group_norm_problem(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_uint32), ("n", ctypes.c_int32), ("m", ctypes.c_int64), ("c", ctypes.c_int32),
+                ("groups", ctypes.c_int32), ("act", ctypes.c_int32), ("eps", ctypes.c_float), ("x_type", ctypes.c_int32),
+                ("y_type", ctypes.c_int32), ("x_row_stride", ctypes.c_int64), ("y_row_stride", ctypes.c_int64),
+                ("dx_row_stride", ctypes.c_int64)]
+
+
+class numbat_rotary_problem(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_uint32), ("heads", ctypes.c_int32), ("d", ctypes.c_int32),
+                ("axes", ctypes.c_int32), ("m", ctypes.c_int64), ("pairs", ctypes.c_int32 * 4),
+                ("extents", ctypes.c_int32 * 4), ("layout", ctypes.c_int32), ("shared", ctypes.c_int32),
+                ("inverse", ctypes.c_int32), ("type", ctypes.c_int32), ("base", ctypes.c_double),
+                ("x_row_stride", ctypes.c_int64), ("y_row_stride", ctypes.c_int64)]
+
+
+class numbat_attention_problem(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_uint32), ("batch", ctypes.c_int32), ("q_len", ctypes.c_int32),
+                ("kv_len", ctypes.c_int32), ("q_heads", ctypes.c_int32), ("kv_heads", ctypes.c_int32),
+                ("d", ctypes.c_int32), ("causal", ctypes.c_int32), ("scale", ctypes.c_float),
+                ("reserved", ctypes.c_int32), ("q_row_stride", ctypes.c_int64), ("k_row_stride", ctypes.c_int64),
+                ("v_row_stride", ctypes.c_int64), ("y_row_stride", ctypes.c_int64)]
+
+
 class NumbatError(RuntimeError):
     def __init__(self, status: int, name: str, detail: str, call: str):
         super().__init__(f"{call}: {name}: {detail}")
@@ -114,6 +142,8 @@ def load() -> ctypes.CDLL:
         CP, BP = ctypes.POINTER(numbat_conv_problem), ctypes.POINTER(numbat_bn_problem)
         PP = ctypes.POINTER(numbat_pool_problem)
         LP, NP = ctypes.POINTER(numbat_linear_problem), ctypes.POINTER(numbat_layer_norm_problem)
+        GP, RP = ctypes.POINTER(numbat_group_norm_problem), ctypes.POINTER(numbat_rotary_problem)
+        AP = ctypes.POINTER(numbat_attention_problem)
         D = ctypes.c_double
         sig = {
             "numbat_abi_version": (ctypes.c_uint32, []),
@@ -148,6 +178,11 @@ def load() -> ctypes.CDLL:
             "numbat_adamw_step": (ctypes.c_int, [P, ctypes.c_int32, ctypes.POINTER(numbat_sgd_group), ctypes.c_int32,
                                                   ctypes.c_int32, D, D, D, ctypes.c_int64, D, P, P, S, P]),
             "numbat_adamw_state_values": (ctypes.c_int, [ctypes.c_int64, P, P, P, P, P, P, P]),
+            "numbat_group_norm_fwd": (ctypes.c_int, [GP, P, P, P, P, P, P, P, S, P]),
+            "numbat_group_norm_bwd": (ctypes.c_int, [GP, P, P, P, P, P, P, P, P, P, ctypes.c_int, P, S, P]),
+            "numbat_rotary": (ctypes.c_int, [RP, P, P, P, P]),
+            "numbat_attention_fwd": (ctypes.c_int, [AP, P, P, P, P, P, P, P, P, S, P]),
+            "numbat_attention_bwd": (ctypes.c_int, [AP, P, P, P, P, P, P, P, P, P, P, P, P, S, P]),
             "numbat_kernel_class_count": (ctypes.c_int, []),
             "numbat_kernel_class_name": (ctypes.c_char_p, [ctypes.c_int]),
             "numbat_timing_enable": (ctypes.c_int, [ctypes.c_int]),
@@ -443,6 +478,65 @@ def numbat_adamw_state_values(n, m, m_unit, v, v_unit, m_value, v_value, stream=
     _check(load().numbat_adamw_state_values(n, _ptr(m), _ptr(m_unit), _ptr(v), _ptr(v_unit), _ptr(m_value),
                                             _ptr(v_value), _stream(stream)),
            "numbat_adamw_state_values")
+
+
+def group_norm_problem(n, m, c, groups, act=ACT_NONE, eps=1e-5, x_type=BF16, y_type=BF16, x_row_stride=0, y_row_stride=0,
+                       dx_row_stride=0):
+    return numbat_group_norm_problem(ctypes.sizeof(numbat_group_norm_problem), n, m, c, groups, act, eps, x_type, y_type,
+                                     x_row_stride, y_row_stride, dx_row_stride)
+
+
+def numbat_group_norm_fwd(p, x, gamma, beta, y, mean=None, rstd=None, ws=None, stream=None, ws_bytes=None):
+    _check(load().numbat_group_norm_fwd(ctypes.byref(p), _ptr(x), _ptr(gamma), _ptr(beta), _ptr(y), _ptr(mean),
+                                        _ptr(rstd), _ptr(ws), _nbytes(ws) if ws_bytes is None else ws_bytes,
+                                        _stream(stream)),
+           "numbat_group_norm_fwd")
+
+
+def numbat_group_norm_bwd(p, dy, x, mean, rstd, gamma, beta, dx, dgamma, dbeta, accumulate=False, ws=None, stream=None,
+                          ws_bytes=None):
+    _check(load().numbat_group_norm_bwd(ctypes.byref(p), _ptr(dy), _ptr(x), _ptr(mean), _ptr(rstd), _ptr(gamma),
+                                        _ptr(beta), _ptr(dx), _ptr(dgamma), _ptr(dbeta), int(bool(accumulate)),
+                                        _ptr(ws), _nbytes(ws) if ws_bytes is None else ws_bytes, _stream(stream)),
+           "numbat_group_norm_bwd")
+
+
+def rotary_problem(m, heads, d, pairs, extents=None, base=10000.0, layout=ROTARY_HALVES, shared=False, inverse=False,
+                   type=BF16, x_row_stride=0, y_row_stride=0):
+    """pairs: the pairs that each axis turns (1 to 4 axes); extents: the grid that the rows lie on, one
+    number for each axis, where no positions are given."""
+    if not 1 <= len(pairs) <= 4 or (extents is not None and len(extents) != len(pairs)):
+        raise ValueError("rotary_problem: 1 to 4 axes, and an extent for each of them")
+    four = lambda v: (ctypes.c_int32 * 4)(*v)  # noqa: E731
+    return numbat_rotary_problem(ctypes.sizeof(numbat_rotary_problem), heads, d, len(pairs), m, four(pairs),
+                                 four(extents or ()), layout, int(bool(shared)), int(bool(inverse)), type, base,
+                                 x_row_stride, y_row_stride)
+
+
+def numbat_rotary(p, x, positions, y, stream=None):
+    _check(load().numbat_rotary(ctypes.byref(p), _ptr(x), _ptr(positions), _ptr(y), _stream(stream)), "numbat_rotary")
+
+
+def attention_problem(batch, q_len, kv_len, q_heads, kv_heads, d, causal=False, scale=None, q_row_stride=0,
+                      k_row_stride=0, v_row_stride=0, y_row_stride=0):
+    """scale: of the scores, d ** -0.5 unless given."""
+    return numbat_attention_problem(ctypes.sizeof(numbat_attention_problem), batch, q_len, kv_len, q_heads, kv_heads, d,
+                                    int(bool(causal)), max(d, 1) ** -0.5 if scale is None else scale, 0, q_row_stride,
+                                    k_row_stride, v_row_stride, y_row_stride)
+
+
+def numbat_attention_fwd(p, q, k, v, q_lengths, kv_lengths, y, lse=None, ws=None, stream=None, ws_bytes=None):
+    _check(load().numbat_attention_fwd(ctypes.byref(p), _ptr(q), _ptr(k), _ptr(v), _ptr(q_lengths), _ptr(kv_lengths),
+                                       _ptr(y), _ptr(lse), _ptr(ws), _nbytes(ws) if ws_bytes is None else ws_bytes,
+                                       _stream(stream)),
+           "numbat_attention_fwd")
+
+
+def numbat_attention_bwd(p, dy, q, k, v, y, lse, q_lengths, kv_lengths, dq, dk, dv, ws=None, stream=None, ws_bytes=None):
+    _check(load().numbat_attention_bwd(ctypes.byref(p), _ptr(dy), _ptr(q), _ptr(k), _ptr(v), _ptr(y), _ptr(lse),
+                                       _ptr(q_lengths), _ptr(kv_lengths), _ptr(dq), _ptr(dk), _ptr(dv), _ptr(ws),
+                                       _nbytes(ws) if ws_bytes is None else ws_bytes, _stream(stream)),
+           "numbat_attention_bwd")
 
 
 def numbat_kernel_class_count() -> int:
