@@ -40,6 +40,7 @@ typedef struct {
   int32_t y_type;        /* numbat_type of y and dy */
   int64_t x_row_stride;  /* x; at most 2^21, like the others */
   int64_t y_row_stride;  /* y and dy */
+  int64_t r_row_stride;  /* residual_grad */
   int64_t dx_row_stride; /* dx */
 } numbat_group_norm_problem;
 
@@ -97,16 +98,17 @@ numbat_status numbat_group_norm_fwd(const numbat_group_norm_problem* p, const vo
 
 /* Backward of group norm and activation, with xh = (x - mean) rstd, t = gamma xh + beta, dt = dy act'(t)
  * and h = gamma dt:
- *   dx = rstd (h - sum h / N - xh sum(h xh) / N)           (sums over the image's group)
- *   dgamma = sum_rows dt xh,  dbeta = sum_rows dt           (fp32 [c], over all images; accumulate: added)
- * gamma, beta NULL: 1 and 0.  Each of dx, dgamma, dbeta may be NULL where it is not wanted; the
- * workspace is required all the same.  dx may be the buffer of dy, or of x, if types and strides
- * agree (NUMBAT_ERR_BAD_DESC otherwise).
+ *   dx = rstd (h - sum h / N - xh sum(h xh) / N) + residual_grad   (sums over the image's group)
+ *   dgamma = sum_rows dt xh,  dbeta = sum_rows dt                   (fp32 [c], over all images; accumulate: added)
+ * gamma, beta NULL: 1 and 0.  residual_grad [n m][c] of x's type or NULL: the gradient that reaches x around the
+ * norm.  Each of dx, dgamma, dbeta may be NULL where it is not wanted; the workspace is required all the
+ * same.  dx may be the buffer of dy, of x or of residual_grad, if types and strides agree
+ * (NUMBAT_ERR_BAD_DESC otherwise).
  * ws: numbat_workspace_size(NUMBAT_OP_GROUP_NORM_BWD). */
 numbat_status numbat_group_norm_bwd(const numbat_group_norm_problem* p, const void* dy, const void* x,
                                     const float* mean, const float* rstd, const float* gamma, const float* beta,
-                                    void* dx, float* dgamma, float* dbeta, int accumulate, void* ws, size_t ws_bytes,
-                                    void* stream);
+                                    const void* residual_grad, void* dx, float* dgamma, float* dbeta, int accumulate,
+                                    void* ws, size_t ws_bytes, void* stream);
 
 /* Turns pair (a, b) number j of every head by the angle of its axis' position:
  *   y_a = a cos(t) - b sin(t),  y_b = b cos(t) + a sin(t),  t = position * base^-e   (inverse: -t)

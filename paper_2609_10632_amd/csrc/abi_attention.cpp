@@ -42,7 +42,7 @@ numbat_status check_gn(const numbat_group_norm_problem* p, GnArgs* a) {
   if (p->n > 65535 || p->c > 65536 || p->m > kMaxIndex)
     return fail(NUMBAT_ERR_UNSUPPORTED, "at most 65535 images, 65536 channels and 2^31-1 rows (n=%d c=%d m=%lld)", p->n,
                 p->c, (long long)p->m);
-  for (int64_t s : {p->x_row_stride, p->y_row_stride, p->dx_row_stride})
+  for (int64_t s : {p->x_row_stride, p->y_row_stride, p->r_row_stride, p->dx_row_stride})
     if (!stride_ok(s, p->c))
       return fail(NUMBAT_ERR_BAD_DESC, "row stride %lld is smaller than c = %d or above 2^21", (long long)s, p->c);
   std::memset(a, 0, sizeof *a);
@@ -56,6 +56,7 @@ numbat_status check_gn(const numbat_group_norm_problem* p, GnArgs* a) {
   a->y_f32 = p->y_type == NUMBAT_TYPE_F32;
   a->ldx = dense(p->x_row_stride, p->c);
   a->ldy = dense(p->y_row_stride, p->c);
+  a->ldr = dense(p->r_row_stride, p->c);
   a->lddx = dense(p->dx_row_stride, p->c);
   return NUMBAT_OK;
 }
@@ -216,8 +217,8 @@ numbat_status numbat_group_norm_fwd(const numbat_group_norm_problem* p, const vo
 
 numbat_status numbat_group_norm_bwd(const numbat_group_norm_problem* p, const void* dy, const void* x,
                                     const float* mean, const float* rstd, const float* gamma, const float* beta,
-                                    void* dx, float* dgamma, float* dbeta, int accumulate, void* ws, size_t ws_bytes,
-                                    void* stream) {
+                                    const void* residual_grad, void* dx, float* dgamma, float* dbeta, int accumulate,
+                                    void* ws, size_t ws_bytes, void* stream) {
   GnArgs a;
   numbat_status st = check_gn(p, &a);
   if (st != NUMBAT_OK) return st;
@@ -234,8 +235,12 @@ numbat_status numbat_group_norm_bwd(const numbat_group_norm_problem* p, const vo
     return fail(NUMBAT_ERR_NULL, "dy, x, mean and rstd are required");
   if (dx == nullptr && dgamma == nullptr && dbeta == nullptr)
     return fail(NUMBAT_ERR_NULL, "at least one of dx, dgamma and dbeta is required");
-  if (!aligned16(dy) || !aligned16(x) || !aligned16(dx))
-    return fail(NUMBAT_ERR_ALIGN, "dy, x and dx must be 16-byte aligned");
+  if (dx == nullptr && residual_grad != nullptr) return fail(NUMBAT_ERR_NULL, "residual_grad needs dx");
+  if (!aligned16(dy) || !aligned16(x) || !aligned16(residual_grad) || !aligned16(dx))
+    return fail(NUMBAT_ERR_ALIGN, "dy, x, residual_grad and dx must be 16-byte aligned");
+  if (dx != nullptr && dx == residual_grad && a.ldr != a.lddx)
+    return fail(NUMBAT_ERR_BAD_DESC, "dx in residual_grad's buffer needs its row stride (dx %lld, residual_grad %lld)",
+                (long long)a.lddx, (long long)a.ldr);
   if (dx == x && a.ldx != a.lddx)
     return fail(NUMBAT_ERR_BAD_DESC, "dx in x's buffer needs its row stride (dx %lld, x %lld)", (long long)a.lddx,
                 (long long)a.ldx);
@@ -244,7 +249,7 @@ numbat_status numbat_group_norm_bwd(const numbat_group_norm_problem* p, const vo
                 (long long)a.lddx, (long long)a.ldy);
   st = check_ws(ws, ws_bytes, with_header(gn_bwd_ws(a)));
   if (st != NUMBAT_OK) return st;
-  e = gn_bwd_launch(a, dy, x, mean, rstd, gamma, beta, dx, dgamma, dbeta, accumulate != 0, ws_body(ws), s);
+  e = gn_bwd_launch(a, dy, x, mean, rstd, gamma, beta, residual_grad, dx, dgamma, dbeta, accumulate != 0, ws_body(ws), s);
   return e == hipSuccess ? ok() : hip_fail(e, "group norm backward launch");
 }
 

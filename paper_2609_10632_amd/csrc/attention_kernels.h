@@ -29,15 +29,15 @@ struct GnArgs {
   int64_t m;
   float eps;
   int32_t x_f32, y_f32;  // type of x, dx / of y, dy
-  int64_t ldx, ldy, lddx;
+  int64_t ldx, ldy, ldr, lddx;
 };
 size_t gn_fwd_ws(const GnArgs& a);
 hipError_t gn_fwd_launch(const GnArgs& a, const void* x, const float* gamma, const float* beta, void* y, float* mean,
                          float* rstd, void* ws, hipStream_t s);
 size_t gn_bwd_ws(const GnArgs& a);
 hipError_t gn_bwd_launch(const GnArgs& a, const void* dy, const void* x, const float* mean, const float* rstd,
-                         const float* gamma, const float* beta, void* dx, float* dgamma, float* dbeta, int accumulate,
-                         void* ws, hipStream_t s);
+                         const float* gamma, const float* beta, const void* res, void* dx, float* dgamma, float* dbeta,
+                         int accumulate, void* ws, hipStream_t s);
 
 // ---------------------------------------------------------------------------
 // Rotary positions

@@ -4,11 +4,16 @@
 //             dgamma = sum dt xh,  dbeta = sum dt
 // the means over the rows and channels of an image's group.
 //
-// A thread owns eight neighbouring channels and walks down rows, so that a block reads whole rows of a
-// slab of channels.  Values are added after the mean of the thread's first rows is taken off them
-// (`shift`): a thread of n rows then loses at most a factor n / 4 + 1 of cancellation in its sum of squares,
-// whatever the mean.  Threads, blocks and channels are joined by their counts, means and centred
-// squares, in a fixed order.
+// A thread owns eight neighbouring channels and walks down rows, so that a block covers whole rows of a slab
+// of channels.  Two ways:
+//   held      a block's slab is whole groups of one image and its threads hold it in registers: every value
+//             is read once and written once, in one launch.
+//   passes    larger maps: a pass over ranges of rows leaves each group's sums of each range, and the pass
+//             that writes the result joins them first, every block for the groups of its slab; the second
+//             read of a map is mostly from the caches.
+// Squares are added after a value within the data's range is taken off (`shift`), so that a mean far from
+// zero costs nothing; threads, ranges and channels are joined by counts, means and centred squares.  All in
+// a fixed order.
 #include <algorithm>
 
 #include "act.h"
@@ -21,56 +26,10 @@ namespace numbat {
 namespace {
 
 constexpr int V = 8;            // channels of a thread
-constexpr int kThreads = 256;
-constexpr int kSlab = 2048;     // channels of a block at most
-constexpr int kAhead = 4;       // rows a thread loads before it works on them
-
-// how an image's values are dealt to blocks of one pass
-struct GnGrid {
-  int32_t slabs, slab;        // slabs of channels, and their channels (the last may have fewer), a multiple of V
-  int32_t cols, side;         // threads across a slab and down
-  int32_t chunks;             // ranges of rows
-  int64_t rows;               // of a range (the last may have fewer)
-  int32_t per_group;          // channels of a group
-};
-
-GnGrid make_grid(const GnArgs& a, int64_t blocks, int most) {
-  GnGrid g;
-  const int vecs = (a.c + V - 1) / V;
-  g.slabs = (a.c + kSlab - 1) / kSlab;
-  g.cols = (vecs + g.slabs - 1) / g.slabs;
-  g.slab = g.cols * V;
-  g.slabs = (a.c + g.slab - 1) / g.slab;
-  g.side = kThreads / g.cols;
-  const int64_t least = (int64_t)g.side * kAhead;
-  int64_t chunks = std::clamp<int64_t>(blocks / ((int64_t)a.n * g.slabs), 1, most);
-  chunks = std::min(chunks, (a.m + least - 1) / least);
-  g.rows = (a.m + chunks - 1) / chunks;
-  g.chunks = (int32_t)((a.m + g.rows - 1) / g.rows);
-  g.per_group = a.c / a.groups;
-  return g;
-}
-dim3 blocks_of(const GnArgs& a, const GnGrid& g) { return dim3((unsigned)g.chunks, (unsigned)g.slabs, (unsigned)a.n); }
-
-// A (slab, group) pair that overlaps is entry slab + group of a list: along the channels one of them
-// advances at every entry.
-__host__ __device__ __forceinline__ int entries(const GnArgs& a, const GnGrid& g) { return a.groups + g.slabs; }
-
-// this thread's part of the block's rows and channels
-struct Place {
-  int img, col, count;  // first channel and how many of its V lie inside
-  int64_t row, end;     // first row within the image, and the range's end
-  int lane_row;
-  __device__ __forceinline__ Place(const GnArgs& a, const GnGrid& g) {
-    img = blockIdx.z;
-    const int across = threadIdx.x % g.cols;
-    lane_row = threadIdx.x / g.cols;
-    col = blockIdx.y * g.slab + across * V;
-    count = lane_row < g.side ? min(V, a.c - col) : 0;
-    row = blockIdx.x * g.rows + lane_row;
-    end = min(a.m, (int64_t)(blockIdx.x + 1) * g.rows);
-  }
-};
+constexpr int kThreads = 256;   // of the passes
+constexpr int kSlab = 2048;     // channels of a block of the passes at most
+constexpr int kAhead = 8;       // rows a thread of the statistics pass loads before it works on them, and of the
+constexpr int kHalf = kAhead / 2;  // others, which hold two turns or two operands
 
 __device__ __forceinline__ void act8(float (&t)[V], int act) {
   auto each = [&](auto f) __attribute__((always_inline)) {
@@ -100,330 +59,788 @@ __device__ __forceinline__ void slope8(const float (&t)[V], float (&d)[V], int a
   }
 }
 
-// rows row, row + side, ... of a thread: f(row number, vectors of one or two operands), kAhead loaded at a time
+// The work on one row ends: left to itself the compiler unpacks every row that a thread holds at once
+__device__ __forceinline__ void row_done() { __builtin_amdgcn_sched_barrier(0); }
+
+// what a thread knows of its channels
+struct Gain {
+  float gamma[V], beta[V];
+  __device__ __forceinline__ Gain(const float* ga, const float* be, int col, int count) {
+    if (ga != nullptr) {
+      get_some<false>(ga + col, count, gamma);
+    } else {
+#pragma unroll
+      for (int e = 0; e < V; ++e) gamma[e] = 1.f;
+    }
+    if (be != nullptr) {
+      get_some<false>(be + col, count, beta);
+    } else {
+#pragma unroll
+      for (int e = 0; e < V; ++e) beta[e] = 0.f;
+    }
+  }
+};
+
+// f(e, group) of a vector's channels; behind the last that counts its group again
 template <typename F>
-__device__ __forceinline__ void walk(const Place& p, int side, F&& f) {
-  int64_t r = p.row;
-  for (; r + (kAhead - 1) * side < p.end; r += kAhead * side) f(r, std::integral_constant<int, kAhead>{});
-  for (; r < p.end; r += side) f(r, std::integral_constant<int, 1>{});
+__device__ __forceinline__ void each_channel(int col, int count, int per_group, F&& f) {
+  int grp = col / per_group, left = (grp + 1) * per_group - col;
+#pragma unroll
+  for (int e = 0; e < V; ++e) {
+    f(e, grp);
+    if (--left == 0 && e + 1 < count) {
+      left = per_group;
+      ++grp;
+    }
+  }
+}
+
+// xh, and dt in dy's place, of a vector
+__device__ __forceinline__ void grads8(float (&x)[V], float (&d)[V], const float (&mean)[V], const float (&rstd)[V],
+                                       const Gain& g, int act) {
+  float t[V];
+#pragma unroll
+  for (int e = 0; e < V; ++e) {
+    x[e] = (x[e] - mean[e]) * rstd[e];
+    t[e] = __builtin_fmaf(x[e], g.gamma[e], g.beta[e]);
+  }
+  slope8(t, d, act);
+}
+
+// Sums two values of every channel over the `side` threads down a slab of `width` channels: in a[c] and b[c] of
+// a[side][width], b[side][width] afterwards.  Called by all T threads, after a barrier.
+template <int T>
+__device__ __forceinline__ void slab_sums(float* a, float* b, int width, int side) {
+  const int parts = max(1, min(side, T / width));
+  float ta = 0.f, tb = 0.f;
+  const int c = threadIdx.x % width, part = threadIdx.x / width;
+  if (parts > 1) {
+    if (part < parts)
+      for (int i = part; i < side; i += parts) {
+        ta += a[i * width + c];
+        tb += b[i * width + c];
+      }
+    __syncthreads();
+    if (part < parts) {
+      a[part * width + c] = ta;
+      b[part * width + c] = tb;
+    }
+    __syncthreads();
+    side = parts;
+  }
+  for (int k = threadIdx.x; k < width; k += T) {  // (a column belongs to one thread)
+    ta = tb = 0.f;
+    for (int i = 0; i < side; ++i) {
+      ta += a[i * width + k];
+      tb += b[i * width + k];
+    }
+    a[k] = ta;
+    b[k] = tb;
+  }
+  __syncthreads();
+}
+
+// f(group number of the slab, its channels lo .. hi of the slab, lane, lanes) by a power of two of lanes for each
+// group that overlaps channels c0 .. c0 + width - 1; whole waves stay together, so f may exchange values among a
+// group's lanes.  Groups past the last have lo >= hi.
+template <int T, typename F>
+__device__ __forceinline__ void each_group(int c0, int width, int per_group, F&& f) {
+  int lanes = 1;
+  while (lanes < 64 && lanes < per_group) lanes *= 2;
+  const int g0 = c0 / per_group, g1 = (c0 + width - 1) / per_group;
+  for (int first = g0; first <= g1; first += T / lanes) {
+    const int grp = first + threadIdx.x / lanes;
+    const int lo = max(grp * per_group - c0, 0), hi = grp <= g1 ? min((grp + 1) * per_group - c0, width) : 0;
+    f(grp, lo, hi, (int)threadIdx.x % lanes, lanes);
+  }
+}
+__device__ __forceinline__ float lane_sum(float t, int lanes) {
+  for (int o = lanes / 2; o > 0; o /= 2) t += __shfl_xor(t, o);
+  return t;
+}
+
+// Mean and centred squares of a group's channels lo .. hi out of the channels' own (each of `rows` values)
+__device__ __forceinline__ float2 join_channels(const float* mean, const float* sq, float rows, int lo, int hi, int lane,
+                                                int lanes) {
+  float m = 0.f, s = 0.f;
+  for (int c = lo + lane; c < hi; c += lanes) m += mean[c];
+  m = lane_sum(m, lanes);
+  m = hi > lo ? m / (float)(hi - lo) : 0.f;
+  for (int c = lo + lane; c < hi; c += lanes) {
+    const float d = mean[c] - m;
+    s += __builtin_fmaf(rows * d, d, sq[c]);
+  }
+  return make_float2(m, lane_sum(s, lanes));
 }
 
 // ---------------------------------------------------------------------------
-// count, mean and centred squares of every entry of a block: part[img][chunk][entry]
-template <typename T, bool ALIGNED>
-__global__ __launch_bounds__(kThreads) void gn_stats_kernel(GnArgs a, GnGrid g, const T* x, float2* part) {
-  __shared__ float s_mean[kThreads * V], s_sq[kThreads * V];
-  const Place p(a, g);
-  const T* xp = x + (int64_t)p.img * a.m * a.ldx + p.col;
-  const int64_t rows = p.end - (int64_t)blockIdx.x * g.rows;
+// Held: a block of T threads for `width` channels of an image, whole groups, NV rows of each thread.
+
+struct GnHeld {
+  int32_t width, slabs, cols, side;  // channels of a block, blocks of an image, threads across and down
+  int32_t rows;                      // of a thread
+  int32_t per_group;
+};
+
+// A vector as it was loaded: bf16 stays packed until it is worked on
+template <typename T>
+struct Raw;
+template <>
+struct Raw<bf16_t> {
+  u32x4 u;
+  template <bool ALIGNED>
+  __device__ __forceinline__ void get(const bf16_t* p, int count) {
+    if (count >= V) {
+      const uint4 v = get16<ALIGNED>(p);
+      u = u32x4{v.x, v.y, v.z, v.w};
+    } else {
+      float f[V];
+      get_some<ALIGNED>(p, count, f);
+      const uint4 v = pack8(f);
+      u = u32x4{v.x, v.y, v.z, v.w};
+    }
+  }
+  __device__ __forceinline__ void zero() { u = u32x4{0, 0, 0, 0}; }
+  __device__ __forceinline__ void values(float (&f)[V]) const { unpack8(make_uint4(u.x, u.y, u.z, u.w), f); }
+  // (the compiler would otherwise keep what it has unpacked, twice the registers)
+  __device__ __forceinline__ void keep() { asm volatile("" : "+v"(u)); }
+};
+template <>
+struct Raw<float> {
+  float v[V];
+  template <bool ALIGNED>
+  __device__ __forceinline__ void get(const float* p, int count) {
+    get_some<ALIGNED>(p, count, v);
+  }
+  __device__ __forceinline__ void zero() {
+#pragma unroll
+    for (int e = 0; e < V; ++e) v[e] = 0.f;
+  }
+  __device__ __forceinline__ void values(float (&f)[V]) const {
+#pragma unroll
+    for (int e = 0; e < V; ++e) f[e] = v[e];
+  }
+  __device__ __forceinline__ void keep() {}
+};
+
+template <int T>
+struct HeldPlace {
+  int img, c0, at, col, count, lane_row;  // col: the thread's first channel; at: within the slab
+  __device__ __forceinline__ HeldPlace(const GnHeld& g) {
+    // an XCD's L2 sees neighbouring slabs of an image: their rows share cache lines
+    const uint32_t t = xcd_remap(blockIdx.x, gridDim.x);
+    img = t / g.slabs;
+    c0 = (t - img * g.slabs) * g.width;
+    lane_row = threadIdx.x / g.cols;
+    at = (threadIdx.x - lane_row * g.cols) * V;
+    col = c0 + at;
+    count = lane_row < g.side ? min(V, g.width - at) : 0;
+  }
+};
+
+template <typename TX, typename TY, bool ALIGNED, int NV, int T>
+__global__ __launch_bounds__(T) void gn_fwd_held_kernel(GnArgs a, GnHeld g, const TX* x, const float* gamma,
+                                                        const float* beta, TY* y, float* mean, float* rstd) {
+  extern __shared__ float lds[];
+  float *s_a = lds, *s_b = s_a + g.side * g.width, *s_shift = s_b + g.side * g.width, *s_mean = s_shift + g.width,
+        *s_rstd = s_mean + g.width;
+  const HeldPlace<T> p(g);
+  const int m = (int)a.m;
+  Raw<TX> v[NV];
+  const TX* xp = x + (int64_t)p.img * a.m * a.ldx + p.col;
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    v[i].zero();
+    if (p.count > 0 && p.lane_row + i * g.side < m) v[i].template get<ALIGNED>(xp + (int64_t)(p.lane_row + i * g.side) * a.ldx, p.count);
+  }
+  const Gain gain(gamma, beta, p.count > 0 ? p.col : 0, p.count);
+  // the first thread's mean of a channel is every thread's shift
+  if (p.lane_row == 0) {
+    float t[V] = {};
+    int rows = 0;
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+      if (i * g.side < m) {
+        float f[V];
+        v[i].values(f);
+        ++rows;
+#pragma unroll
+        for (int e = 0; e < V; ++e) t[e] += f[e];
+      }
+#pragma unroll
+    for (int e = 0; e < V; ++e)
+      if (e < p.count) s_shift[p.at + e] = t[e] / (float)rows;
+  }
+#pragma unroll
+  for (int i = 0; i < NV; ++i) v[i].keep();
+  __syncthreads();
   if (p.count > 0) {
     float shift[V], s1[V], s2[V];
 #pragma unroll
-    for (int e = 0; e < V; ++e) shift[e] = s1[e] = s2[e] = 0.f;
-    bool first = true;
-    walk(p, g.side, [&](int64_t r, auto nc) __attribute__((always_inline)) {
-      constexpr int N = decltype(nc)::value;
-      float f[N][V];
+    for (int e = 0; e < V; ++e) {
+      shift[e] = e < p.count ? s_shift[p.at + e] : 0.f;
+      s1[e] = s2[e] = 0.f;
+    }
 #pragma unroll
-      for (int i = 0; i < N; ++i) get_some<ALIGNED>(xp + (r + (int64_t)i * g.side) * a.ldx, p.count, f[i]);
-      if (first) {
-        first = false;
-#pragma unroll
-        for (int e = 0; e < V; ++e) {
-          float t = 0.f;
-#pragma unroll
-          for (int i = 0; i < N; ++i) t += f[i][e];
-          shift[e] = t * (1.0f / N);
-        }
-      }
-#pragma unroll
-      for (int i = 0; i < N; ++i)
+    for (int i = 0; i < NV; ++i)
+      if (p.lane_row + i * g.side < m) {
+        float f[V];
+        v[i].values(f);
 #pragma unroll
         for (int e = 0; e < V; ++e) {
-          const float d = f[i][e] - shift[e];
+          const float d = f[e] - shift[e];
           s1[e] += d;
           s2[e] = __builtin_fmaf(d, d, s2[e]);
         }
-    });
-    const int64_t mine = p.row < p.end ? (p.end - p.row + g.side - 1) / g.side : 0;
-    const float inv = mine > 0 ? 1.0f / (float)mine : 0.f;
-    const int at = p.lane_row * g.slab + (p.col - (int)blockIdx.y * g.slab);
+        row_done();
+      }
 #pragma unroll
-    for (int e = 0; e < V; ++e) {
-      const float d = s1[e] * inv;
-      s_mean[at + e] = shift[e] + d;
-      s_sq[at + e] = fmaxf(__builtin_fmaf(-s1[e], d, s2[e]), 0.f);
-    }
+    for (int e = 0; e < V; ++e)
+      if (e < p.count) {
+        s_a[p.lane_row * g.width + p.at + e] = s1[e];
+        s_b[p.lane_row * g.width + p.at + e] = s2[e];
+      }
+  }
+#pragma unroll
+  for (int i = 0; i < NV; ++i) v[i].keep();
+  __syncthreads();
+  slab_sums<T>(s_a, s_b, g.width, g.side);
+  const float rows = (float)m;
+  for (int c = threadIdx.x; c < g.width; c += T) {  // each channel's mean and centred squares
+    const float d = s_a[c] / rows;
+    s_b[c] = fmaxf(__builtin_fmaf(-s_a[c], d, s_b[c]), 0.f);
+    s_a[c] = s_shift[c] + d;
   }
   __syncthreads();
-  // each channel's over the threads of its column
-  const int c0 = blockIdx.y * g.slab, width = min(g.slab, a.c - c0);
-  const int side = (int)min<int64_t>(g.side, rows);  // (threads further down had no row)
-  const float inv_rows = 1.0f / (float)rows;
-  for (int c = threadIdx.x; c < width; c += kThreads) {
-    float mean = 0.f, sq = 0.f;
-    for (int i = 0; i < side; ++i) mean = __builtin_fmaf((float)((rows - i + g.side - 1) / g.side), s_mean[i * g.slab + c], mean);
-    mean *= inv_rows;
-    for (int i = 0; i < side; ++i) {
-      const float d = s_mean[i * g.slab + c] - mean;
-      sq += __builtin_fmaf((float)((rows - i + g.side - 1) / g.side) * d, d, s_sq[i * g.slab + c]);
-    }
-    s_mean[c] = mean;
-    s_sq[c] = sq;
-  }
-  __syncthreads();
-  // each group's over its channels of the slab, by a power of two of lanes
-  int lanes = 1;
-  while (lanes < 64 && lanes < g.per_group) lanes *= 2;
-  const int lane = threadIdx.x % lanes;
-  const int g0 = c0 / g.per_group, g1 = (c0 + width - 1) / g.per_group;
-  float2* out = part + ((int64_t)p.img * g.chunks + blockIdx.x) * entries(a, g) + blockIdx.y;
-  for (int first = g0; first <= g1; first += kThreads / lanes) {  // (whole waves stay together)
-    const int grp = first + threadIdx.x / lanes;
-    const int lo = max(grp * g.per_group - c0, 0), hi = min((grp + 1) * g.per_group - c0, width);
-    float mean = 0.f, sq = 0.f;
-    for (int c = lo + lane; c < hi; c += lanes) mean += s_mean[c];
-    for (int o = lanes / 2; o > 0; o /= 2) mean += __shfl_xor(mean, o);
-    mean = hi > lo ? mean / (float)(hi - lo) : 0.f;
+  each_group<T>(p.c0, g.width, g.per_group, [&](int grp, int lo, int hi, int lane, int lanes) __attribute__((always_inline)) {
+    const float2 t = join_channels(s_a, s_b, rows, lo, hi, lane, lanes);
+    const float r = 1.0f / sqrtf(t.y / (rows * (float)g.per_group) + a.eps);
     for (int c = lo + lane; c < hi; c += lanes) {
-      const float d = s_mean[c] - mean;
-      sq += __builtin_fmaf((float)rows * d, d, s_sq[c]);
+      s_mean[c] = t.x;
+      s_rstd[c] = r;
     }
-    for (int o = lanes / 2; o > 0; o /= 2) sq += __shfl_xor(sq, o);
-    if (lane == 0 && grp <= g1) out[grp] = make_float2(mean, sq);
-  }
-}
-
-// the entries of an image's group, joined by one wave
-__device__ __forceinline__ float2 join_group(const GnArgs& a, const GnGrid& g, const float2* part, int img, int grp,
-                                             int lane) {
-  const int s0 = grp * g.per_group / g.slab, s1 = ((grp + 1) * g.per_group - 1) / g.slab, parts = s1 - s0 + 1;
-  const float2* at = part + (int64_t)img * g.chunks * entries(a, g) + grp + s0;
-  // values of entry i: its rows times its channels of the group
-  auto count = [&](int i) __attribute__((always_inline)) {
-    const int chunk = i / parts, slab = s0 + i % parts;
-    const int64_t rows = min(a.m, (int64_t)(chunk + 1) * g.rows) - chunk * g.rows;
-    const int lo = max(grp * g.per_group, slab * g.slab), hi = min((grp + 1) * g.per_group, (slab + 1) * g.slab);
-    return (float)rows * (float)(hi - lo);
-  };
-  auto entry = [&](int i) __attribute__((always_inline)) { return at[(int64_t)(i / parts) * entries(a, g) + i % parts]; };
-  const int total = g.chunks * parts;
-  const float inv = 1.0f / ((float)a.m * (float)g.per_group);
-  float mean = 0.f, sq = 0.f;
-  for (int i = lane; i < total; i += 64) mean = __builtin_fmaf(count(i), entry(i).x, mean);
-  for (int o = 32; o > 0; o /= 2) mean += __shfl_xor(mean, o);
-  mean *= inv;
-  for (int i = lane; i < total; i += 64) {
-    const float2 v = entry(i);
-    const float d = v.x - mean;
-    sq += __builtin_fmaf(count(i) * d, d, v.y);
-  }
-  for (int o = 32; o > 0; o /= 2) sq += __shfl_xor(sq, o);
-  return make_float2(mean, 1.0f / sqrtf(sq * inv + a.eps));
-}
-
-__global__ __launch_bounds__(kThreads) void gn_join_kernel(GnArgs a, GnGrid g, const float2* part, float2* stats,
-                                                           float* mean, float* rstd) {
-  const int64_t i = (int64_t)blockIdx.x * (kThreads / 64) + threadIdx.x / 64;
-  if (i >= (int64_t)a.n * a.groups) return;
-  const float2 t = join_group(a, g, part, (int)(i / a.groups), (int)(i % a.groups), threadIdx.x % 64);
-  if (threadIdx.x % 64 != 0) return;
-  stats[i] = t;
-  if (mean != nullptr) mean[i] = t.x;
-  if (rstd != nullptr) rstd[i] = t.y;
-}
-
-template <typename TX, typename TY, bool ALIGNED>
-__global__ __launch_bounds__(kThreads) void gn_fwd_kernel(GnArgs a, GnGrid g, const TX* x, const float* gamma,
-                                                          const float* beta, const float2* stats, TY* y) {
-  const Place p(a, g);
-  if (p.count <= 0) return;
-  float mean[V], scale[V], shift[V];
-#pragma unroll
-  for (int e = 0; e < V; ++e) {
-    const int c = p.col + (e < p.count ? e : 0);
-    const float2 t = stats[(int64_t)p.img * a.groups + c / g.per_group];
-    mean[e] = t.x;
-    scale[e] = t.y * (gamma != nullptr ? gamma[c] : 1.f);
-    shift[e] = beta != nullptr ? beta[c] : 0.f;
-  }
-  const TX* xp = x + (int64_t)p.img * a.m * a.ldx + p.col;
-  TY* yp = y + (int64_t)p.img * a.m * a.ldy + p.col;
-  walk(p, g.side, [&](int64_t r, auto nc) __attribute__((always_inline)) {
-    constexpr int N = decltype(nc)::value;
-    float f[N][V];
-#pragma unroll
-    for (int i = 0; i < N; ++i) get_some<ALIGNED>(xp + (r + (int64_t)i * g.side) * a.ldx, p.count, f[i]);
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-#pragma unroll
-      for (int e = 0; e < V; ++e) f[i][e] = __builtin_fmaf(f[i][e] - mean[e], scale[e], shift[e]);
-      act8(f[i], a.act);
-      put_some<ALIGNED>(yp + (r + (int64_t)i * g.side) * a.ldy, p.count, f[i]);
+    if (lane == 0 && hi > lo) {
+      if (mean != nullptr) mean[(int64_t)p.img * a.groups + grp] = t.x;
+      if (rstd != nullptr) rstd[(int64_t)p.img * a.groups + grp] = r;
     }
   });
+  __syncthreads();
+  if (p.count <= 0) return;
+  float mu[V], scale[V];
+#pragma unroll
+  for (int e = 0; e < V; ++e) {
+    mu[e] = e < p.count ? s_mean[p.at + e] : 0.f;
+    scale[e] = e < p.count ? s_rstd[p.at + e] * gain.gamma[e] : 0.f;
+  }
+  TY* yp = y + (int64_t)p.img * a.m * a.ldy + p.col;
+#pragma unroll
+  for (int i = 0; i < NV; ++i)
+    if (p.lane_row + i * g.side < m) {
+      float f[V];
+      v[i].values(f);
+#pragma unroll
+      for (int e = 0; e < V; ++e) f[e] = __builtin_fmaf(f[e] - mu[e], scale[e], gain.beta[e]);
+      act8(f, a.act);
+      put_some<ALIGNED>(yp + (int64_t)(p.lane_row + i * g.side) * a.ldy, p.count, f);
+      row_done();
+    }
+}
+
+// sums: each image's sums of dt and dt xh, [img][2][c], or nullptr
+template <typename TX, typename TY, bool ALIGNED, int NV, int T>
+__global__ __launch_bounds__(T) void gn_bwd_held_kernel(GnArgs a, GnHeld g, const TY* dy, const TX* x, const float* mean,
+                                                        const float* rstd, const float* gamma, const float* beta,
+                                                        const TX* res, TX* dx, float* sums) {
+  extern __shared__ float lds[];
+  float *s_a = lds, *s_b = s_a + g.side * g.width, *s_h1 = s_b + g.side * g.width, *s_h2 = s_h1 + g.width;
+  const HeldPlace<T> p(g);
+  const int m = (int)a.m;
+  Raw<TX> v[NV];
+  Raw<TY> d[NV];
+  const TX* xp = x + (int64_t)p.img * a.m * a.ldx + p.col;
+  const TY* dp = dy + (int64_t)p.img * a.m * a.ldy + p.col;
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    v[i].zero();
+    d[i].zero();
+    const int64_t r = p.lane_row + i * g.side;
+    if (p.count > 0 && r < m) {
+      v[i].template get<ALIGNED>(xp + r * a.ldx, p.count);
+      d[i].template get<ALIGNED>(dp + r * a.ldy, p.count);
+    }
+  }
+  const Gain gain(gamma, beta, p.count > 0 ? p.col : 0, p.count);
+  float mu[V], rs[V];
+  each_channel(p.count > 0 ? p.col : 0, p.count, g.per_group, [&](int e, int grp) __attribute__((always_inline)) {
+    mu[e] = mean[(int64_t)p.img * a.groups + grp];
+    rs[e] = rstd[(int64_t)p.img * a.groups + grp];
+  });
+  float dt[NV][V];
+  if (p.count > 0) {
+    float s1[V] = {}, s2[V] = {};
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+      if (p.lane_row + i * g.side < m) {
+        float f[V];
+        v[i].values(f);
+        d[i].values(dt[i]);
+        grads8(f, dt[i], mu, rs, gain, a.act);
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          s1[e] += dt[i][e];
+          s2[e] = __builtin_fmaf(dt[i][e], f[e], s2[e]);
+        }
+        row_done();
+      }
+#pragma unroll
+    for (int e = 0; e < V; ++e)
+      if (e < p.count) {
+        s_a[p.lane_row * g.width + p.at + e] = s1[e];
+        s_b[p.lane_row * g.width + p.at + e] = s2[e];
+      }
+  }
+#pragma unroll
+  for (int i = 0; i < NV; ++i) v[i].keep();
+  __syncthreads();
+  slab_sums<T>(s_a, s_b, g.width, g.side);
+  if (sums != nullptr)
+    for (int c = threadIdx.x; c < g.width; c += T) {
+      sums[(int64_t)p.img * 2 * a.c + p.c0 + c] = s_a[c];
+      sums[(int64_t)p.img * 2 * a.c + a.c + p.c0 + c] = s_b[c];
+    }
+  if (dx == nullptr) return;
+  const float inv = 1.0f / ((float)m * (float)g.per_group);
+  each_group<T>(p.c0, g.width, g.per_group, [&](int, int lo, int hi, int lane, int lanes) __attribute__((always_inline)) {
+    float h1 = 0.f, h2 = 0.f;
+    for (int c = lo + lane; c < hi; c += lanes) {
+      const float ga = gamma != nullptr ? gamma[p.c0 + c] : 1.f;
+      h1 = __builtin_fmaf(ga, s_a[c], h1);
+      h2 = __builtin_fmaf(ga, s_b[c], h2);
+    }
+    h1 = lane_sum(h1, lanes) * inv;
+    h2 = lane_sum(h2, lanes) * inv;
+    for (int c = lo + lane; c < hi; c += lanes) {
+      s_h1[c] = h1;
+      s_h2[c] = h2;
+    }
+  });
+  __syncthreads();
+  if (p.count <= 0) return;
+  float h1[V], h2[V];
+#pragma unroll
+  for (int e = 0; e < V; ++e) {
+    h1[e] = e < p.count ? s_h1[p.at + e] : 0.f;
+    h2[e] = e < p.count ? s_h2[p.at + e] : 0.f;
+  }
+  TX* op = dx + (int64_t)p.img * a.m * a.lddx + p.col;
+  const TX* rp = res != nullptr ? res + (int64_t)p.img * a.m * a.ldr + p.col : nullptr;
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int64_t r = p.lane_row + i * g.side;
+    if (r < m) {
+      float f[V], q[V] = {};
+      if (rp != nullptr) get_some<ALIGNED>(rp + r * a.ldr, p.count, q);
+      v[i].values(f);
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        const float xh = (f[e] - mu[e]) * rs[e];
+        f[e] = __builtin_fmaf(rs[e], __builtin_fmaf(dt[i][e], gain.gamma[e], -h1[e]) - xh * h2[e], q[e]);
+      }
+      put_some<ALIGNED>(op + r * a.lddx, p.count, f);
+      row_done();
+    }
+  }
 }
 
 // ---------------------------------------------------------------------------
-// sums over a block's rows: part[img][chunk][2][c] of dt and of dt xh
-template <typename TX, typename TY, bool ALIGNED>
-__global__ __launch_bounds__(kThreads) void gn_bwd_sums_kernel(GnArgs a, GnGrid g, const TY* dy, const TX* x,
-                                                               const float* mean, const float* rstd,
-                                                               const float* gamma, const float* beta, float* part) {
-  __shared__ float s_sum[2][kThreads * V];
+// Passes over ranges of rows
+
+// how an image's values are dealt to blocks of one pass
+struct GnGrid {
+  int32_t slabs, slab;        // slabs of channels, and their channels (the last may have fewer), a multiple of V
+  int32_t cols, side;         // threads across a slab and down
+  int32_t chunks;             // ranges of rows
+  int64_t rows;               // of a range (the last may have fewer)
+  int32_t per_group;          // channels of a group
+};
+
+// ranges of rows, the same number for each thread, that make up to `blocks` blocks
+GnGrid make_grid(const GnArgs& a, int64_t blocks, int64_t most) {
+  GnGrid g;
+  const int vecs = (a.c + V - 1) / V;
+  g.slabs = (a.c + kSlab - 1) / kSlab;
+  g.cols = (vecs + g.slabs - 1) / g.slabs;
+  g.slab = g.cols * V;
+  g.slabs = (a.c + g.slab - 1) / g.slab;
+  g.side = kThreads / g.cols;
+  const int64_t least = (int64_t)g.side * kHalf;
+  const int64_t chunks = std::clamp<int64_t>(blocks / ((int64_t)a.n * g.slabs), 1, most);
+  g.rows = std::max(least, (a.m + g.side * chunks - 1) / (g.side * chunks) * g.side);
+  g.chunks = (int32_t)((a.m + g.rows - 1) / g.rows);
+  g.per_group = a.c / a.groups;
+  return g;
+}
+dim3 blocks_of(const GnArgs& a, const GnGrid& g) { return dim3((unsigned)g.chunks, (unsigned)g.slabs, (unsigned)a.n); }
+
+// A (slab, group) pair that overlaps is entry slab + group of a list: along the channels one of them
+// advances at every entry.
+__host__ __device__ __forceinline__ int entries(const GnArgs& a, const GnGrid& g) { return a.groups + g.slabs; }
+
+// this thread's part of the block's rows and channels
+struct Place {
+  int img, c0, width, at, col, count;  // the slab's first channel and channels; the thread's, and how many lie inside
+  int64_t row, end;                    // first row within the image, and the range's end
+  int lane_row;
+  __device__ __forceinline__ Place(const GnArgs& a, const GnGrid& g) {
+    img = blockIdx.z;
+    c0 = blockIdx.y * g.slab;
+    width = min(g.slab, a.c - c0);
+    lane_row = threadIdx.x / g.cols;
+    at = (threadIdx.x - lane_row * g.cols) * V;
+    col = c0 + at;
+    count = lane_row < g.side ? min(V, a.c - col) : 0;
+    row = blockIdx.x * g.rows + lane_row;
+    end = min(a.m, (int64_t)(blockIdx.x + 1) * g.rows);
+  }
+};
+
+// N rows of a thread, row, row + side, ..., those inside the range
+template <bool ALIGNED, int N, typename T>
+__device__ __forceinline__ void get_rows(const T* base, int64_t ld, int64_t row, int64_t end, int side, int count,
+                                         Raw<T> (&v)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int64_t r = row + i * side;
+    if (r < end) v[i].template get<ALIGNED>(base + r * ld, count);
+    else v[i].zero();
+  }
+}
+
+// mean and centred squares of every entry of a block: part[img][chunk][entry]
+template <typename T, bool ALIGNED>
+__global__ __launch_bounds__(kThreads) void gn_stats_kernel(GnArgs a, GnGrid g, const T* x, float2* part) {
+  __shared__ float s_a[kThreads * V], s_b[kThreads * V], s_shift[kSlab];
   const Place p(a, g);
+  const T* xp = x + (int64_t)p.img * a.m * a.ldx + p.col;
+  const int64_t first = (int64_t)blockIdx.x * g.rows;
+  float shift[V], s1[V] = {}, s2[V] = {};
+  Raw<T> v[kAhead];
+  if (p.count > 0) get_rows<ALIGNED>(xp, a.ldx, p.row, p.end, g.side, p.count, v);
+  // the first thread's mean of a channel is every thread's shift
+  if (p.lane_row == 0) {
+    float t[V] = {};
+    int rows = 0;
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i)
+      if (p.row + i * g.side < p.end) {
+        float f[V];
+        v[i].values(f);
+        ++rows;
+#pragma unroll
+        for (int e = 0; e < V; ++e) t[e] += f[e];
+      }
+#pragma unroll
+    for (int e = 0; e < V; ++e)
+      if (e < p.count) s_shift[p.at + e] = t[e] / (float)rows;
+  }
+  __syncthreads();
   if (p.count > 0) {
-    float mu[V], rs[V], ga[V], be[V], s1[V], s2[V];
 #pragma unroll
-    for (int e = 0; e < V; ++e) {
-      const int c = p.col + (e < p.count ? e : 0);
-      const int64_t at = (int64_t)p.img * a.groups + c / g.per_group;
-      mu[e] = mean[at];
-      rs[e] = rstd[at];
-      ga[e] = gamma != nullptr ? gamma[c] : 1.f;
-      be[e] = beta != nullptr ? beta[c] : 0.f;
-      s1[e] = s2[e] = 0.f;
-    }
-    const TX* xp = x + (int64_t)p.img * a.m * a.ldx + p.col;
-    const TY* dp = dy + (int64_t)p.img * a.m * a.ldy + p.col;
-    walk(p, g.side, [&](int64_t r, auto nc) __attribute__((always_inline)) {
-      constexpr int N = decltype(nc)::value;
-      float f[N][V], d[N][V];
+    for (int e = 0; e < V; ++e) shift[e] = e < p.count ? s_shift[p.at + e] : 0.f;
+    for (int64_t r = p.row; r < p.end; r += (int64_t)kAhead * g.side) {
 #pragma unroll
-      for (int i = 0; i < N; ++i) {
-        get_some<ALIGNED>(xp + (r + (int64_t)i * g.side) * a.ldx, p.count, f[i]);
-        get_some<ALIGNED>(dp + (r + (int64_t)i * g.side) * a.ldy, p.count, d[i]);
-      }
+      for (int i = 0; i < kAhead; ++i)
+        if (r + i * g.side < p.end) {
+          float f[V];
+          v[i].values(f);
 #pragma unroll
-      for (int i = 0; i < N; ++i) {
-        float t[V];
-#pragma unroll
-        for (int e = 0; e < V; ++e) {
-          f[i][e] = (f[i][e] - mu[e]) * rs[e];
-          t[e] = __builtin_fmaf(f[i][e], ga[e], be[e]);
+          for (int e = 0; e < V; ++e) {
+            const float d = f[e] - shift[e];
+            s1[e] += d;
+            s2[e] = __builtin_fmaf(d, d, s2[e]);
+          }
+          row_done();
         }
-        slope8(t, d[i], a.act);
-#pragma unroll
-        for (int e = 0; e < V; ++e) {
-          s1[e] += d[i][e];
-          s2[e] = __builtin_fmaf(d[i][e], f[i][e], s2[e]);
-        }
-      }
-    });
-    const int at = p.lane_row * g.slab + (p.col - (int)blockIdx.y * g.slab);
-#pragma unroll
-    for (int e = 0; e < V; ++e) {
-      s_sum[0][at + e] = s1[e];
-      s_sum[1][at + e] = s2[e];
+      get_rows<ALIGNED>(xp, a.ldx, r + (int64_t)kAhead * g.side, p.end, g.side, p.count, v);
     }
+#pragma unroll
+    for (int e = 0; e < V; ++e)
+      if (e < p.count) {
+        s_a[p.lane_row * p.width + p.at + e] = s1[e];
+        s_b[p.lane_row * p.width + p.at + e] = s2[e];
+      }
   }
   __syncthreads();
-  const int c0 = blockIdx.y * g.slab, width = min(g.slab, a.c - c0);
-  float* out = part + ((int64_t)p.img * g.chunks + blockIdx.x) * 2 * a.c + c0;
-  for (int i = threadIdx.x; i < 2 * width; i += kThreads) {
-    const int k = i >= width, c = i - k * width;
-    float t = 0.f;
-    for (int j = 0; j < g.side; ++j) t += s_sum[k][j * g.slab + c];
-    out[(int64_t)k * a.c + c] = t;
+  slab_sums<kThreads>(s_a, s_b, p.width, g.side);
+  const float rows = (float)(p.end - first);
+  for (int c = threadIdx.x; c < p.width; c += kThreads) {
+    const float d = s_a[c] / rows;
+    s_b[c] = fmaxf(__builtin_fmaf(-s_a[c], d, s_b[c]), 0.f);
+    s_a[c] = s_shift[c] + d;
   }
-}
-
-// a block for each image's group: the chunks' sums added for each channel (sums[img][2][c]) and the
-// group's means of h and h xh (means[img][group])
-__global__ __launch_bounds__(kThreads) void gn_bwd_join_kernel(GnArgs a, GnGrid g, const float* part,
-                                                               const float* gamma, float* sums, float2* means) {
-  __shared__ float2 s_sum[kThreads];
-  const int img = blockIdx.y, grp = blockIdx.x, tid = threadIdx.x;
-  int lanes = 1;
-  while (lanes < kThreads && lanes < g.per_group) lanes *= 2;
-  const int lane = tid % lanes, side = kThreads / lanes;
-  float h1 = 0.f, h2 = 0.f;
-  for (int first = 0; first < g.per_group; first += lanes) {
-    const int c = first + lane;
-    float2 t = make_float2(0.f, 0.f);
-    if (c < g.per_group) {
-      const float* at = part + (int64_t)img * g.chunks * 2 * a.c + grp * g.per_group + c;
-      for (int j = tid / lanes; j < g.chunks; j += side) {
-        t.x += at[(int64_t)j * 2 * a.c];
-        t.y += at[(int64_t)j * 2 * a.c + a.c];
-      }
-    }
-    s_sum[tid] = t;
-    __syncthreads();
-    if (tid < lanes && c < g.per_group) {
-      for (int j = 1; j < side; ++j) {
-        t.x += s_sum[j * lanes + lane].x;
-        t.y += s_sum[j * lanes + lane].y;
-      }
-      const int ch = grp * g.per_group + c;
-      sums[(int64_t)img * 2 * a.c + ch] = t.x;
-      sums[(int64_t)img * 2 * a.c + a.c + ch] = t.y;
-      const float ga = gamma != nullptr ? gamma[ch] : 1.f;
-      h1 = __builtin_fmaf(ga, t.x, h1);
-      h2 = __builtin_fmaf(ga, t.y, h2);
-    }
-    __syncthreads();
-  }
-  s_sum[tid] = make_float2(h1, h2);
   __syncthreads();
-  for (int o = lanes / 2; o > 0; o /= 2) {
-    if (tid < o) {
-      s_sum[tid].x += s_sum[tid + o].x;
-      s_sum[tid].y += s_sum[tid + o].y;
-    }
-    __syncthreads();
-  }
-  if (tid == 0) {
-    const float inv = 1.0f / ((float)a.m * (float)g.per_group);
-    means[(int64_t)img * a.groups + grp] = make_float2(s_sum[0].x * inv, s_sum[0].y * inv);
-  }
-}
-
-template <typename TX, typename TY, bool ALIGNED>
-__global__ __launch_bounds__(kThreads) void gn_bwd_kernel(GnArgs a, GnGrid g, const TY* dy, const TX* x,
-                                                          const float* mean, const float* rstd, const float* gamma,
-                                                          const float* beta, const float2* means, TX* dx) {
-  const Place p(a, g);
-  if (p.count <= 0) return;
-  float mu[V], rs[V], ga[V], be[V], h1[V], h2[V];
-#pragma unroll
-  for (int e = 0; e < V; ++e) {
-    const int c = p.col + (e < p.count ? e : 0);
-    const int64_t at = (int64_t)p.img * a.groups + c / g.per_group;
-    mu[e] = mean[at];
-    rs[e] = rstd[at];
-    ga[e] = gamma != nullptr ? gamma[c] : 1.f;
-    be[e] = beta != nullptr ? beta[c] : 0.f;
-    h1[e] = means[at].x;
-    h2[e] = means[at].y;
-  }
-  const TX* xp = x + (int64_t)p.img * a.m * a.ldx + p.col;
-  const TY* dp = dy + (int64_t)p.img * a.m * a.ldy + p.col;
-  TX* op = dx + (int64_t)p.img * a.m * a.lddx + p.col;
-  walk(p, g.side, [&](int64_t r, auto nc) __attribute__((always_inline)) {
-    constexpr int N = decltype(nc)::value;
-    float f[N][V], d[N][V];
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      get_some<ALIGNED>(xp + (r + (int64_t)i * g.side) * a.ldx, p.count, f[i]);
-      get_some<ALIGNED>(dp + (r + (int64_t)i * g.side) * a.ldy, p.count, d[i]);
-    }
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      float t[V];
-#pragma unroll
-      for (int e = 0; e < V; ++e) {
-        f[i][e] = (f[i][e] - mu[e]) * rs[e];
-        t[e] = __builtin_fmaf(f[i][e], ga[e], be[e]);
-      }
-      slope8(t, d[i], a.act);
-#pragma unroll
-      for (int e = 0; e < V; ++e) t[e] = rs[e] * (__builtin_fmaf(d[i][e], ga[e], -h1[e]) - f[i][e] * h2[e]);
-      put_some<ALIGNED>(op + (r + (int64_t)i * g.side) * a.lddx, p.count, t);
-    }
+  float2* out = part + ((int64_t)p.img * g.chunks + blockIdx.x) * entries(a, g) + blockIdx.y;
+  each_group<kThreads>(p.c0, p.width, g.per_group, [&](int grp, int lo, int hi, int lane, int lanes) __attribute__((always_inline)) {
+    const float2 t = join_channels(s_a, s_b, rows, lo, hi, lane, lanes);
+    if (lane == 0 && hi > lo) out[grp] = t;
   });
 }
 
+// f(range, its entry) of every lane's share of the ranges, eight loads in flight
+template <typename F>
+__device__ __forceinline__ void each_chunk(const float2* at, int step, int chunks, int lane, int lanes, F&& f) {
+  for (int i = lane; i < chunks; i += 8 * lanes) {
+    float2 v[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = at[(int64_t)min(i + k * lanes, chunks - 1) * step];
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      if (i + k * lanes < chunks) f(i + k * lanes, v[k]);
+  }
+}
+
+// The entries of an image's group, joined by a power of two of lanes: mean and centred squares.  The first
+// entry's mean is the shift of the others' (of E ranges at most 1 + E of cancellation).
+__device__ __forceinline__ float2 join_stats(const GnArgs& a, const GnGrid& g, const float2* part, int img, int grp,
+                                             int lane, int lanes) {
+  const int s0 = grp * g.per_group / g.slab, s1 = ((grp + 1) * g.per_group - 1) / g.slab;
+  const float2* at = part + (int64_t)img * g.chunks * entries(a, g) + grp;
+  const float shift = at[s0].x;
+  float t1 = 0.f, t2 = 0.f;
+  for (int s = s0; s <= s1; ++s) {
+    const int wide = min((grp + 1) * g.per_group, (s + 1) * g.slab) - max(grp * g.per_group, s * g.slab);
+    each_chunk(at + s, entries(a, g), g.chunks, lane, lanes, [&](int i, float2 v) __attribute__((always_inline)) {
+      const float count = (float)(min(a.m, (int64_t)(i + 1) * g.rows) - i * g.rows) * (float)wide, d = v.x - shift;
+      t1 = __builtin_fmaf(count, d, t1);
+      t2 += __builtin_fmaf(count * d, d, v.y);
+    });
+  }
+  t1 = lane_sum(t1, lanes);
+  t2 = lane_sum(t2, lanes);
+  const float inv = 1.0f / ((float)a.m * (float)g.per_group), d = t1 * inv;
+  return make_float2(shift + d, 1.0f / sqrtf(fmaxf(__builtin_fmaf(-t1, d, t2), 0.f) * inv + a.eps));
+}
+// the entries' sums, times what makes them means
+__device__ __forceinline__ float2 join_sums(const GnArgs& a, const GnGrid& g, const float2* part, int img, int grp,
+                                            int lane, int lanes) {
+  const int s0 = grp * g.per_group / g.slab, s1 = ((grp + 1) * g.per_group - 1) / g.slab;
+  const float2* at = part + (int64_t)img * g.chunks * entries(a, g) + grp;
+  float t1 = 0.f, t2 = 0.f;
+  for (int s = s0; s <= s1; ++s)
+    each_chunk(at + s, entries(a, g), g.chunks, lane, lanes, [&](int, float2 v) __attribute__((always_inline)) {
+      t1 += v.x;
+      t2 += v.y;
+    });
+  const float inv = 1.0f / ((float)a.m * (float)g.per_group);
+  return make_float2(lane_sum(t1, lanes) * inv, lane_sum(t2, lanes) * inv);
+}
+
+// A block of the writing pass joins the groups of its slab, or, where they have too many entries for that, a
+// kernel of its own has joined every group: which of the two, and the lanes of a group
+constexpr int kJoinInBlock = 4096;
+bool joins_in_block(const GnArgs& a, const GnGrid& g) {
+  const int64_t groups = std::min<int64_t>(a.groups, g.slab / g.per_group + 2);
+  return groups * g.chunks <= kJoinInBlock && groups <= kThreads;
+}
+
+// both joins of a group that its lanes have at hand: f(entry's result) for every channel
+template <bool STATS>
+__global__ __launch_bounds__(kThreads) void gn_join_kernel(GnArgs a, GnGrid g, const float2* part, float2* joined) {
+  const int64_t i = (int64_t)blockIdx.x * (kThreads / 64) + threadIdx.x / 64;
+  if (i >= (int64_t)a.n * a.groups) return;
+  const int img = (int)(i / a.groups), grp = (int)(i - (int64_t)img * a.groups), lane = threadIdx.x % 64;
+  const float2 t = STATS ? join_stats(a, g, part, img, grp, lane, 64) : join_sums(a, g, part, img, grp, lane, 64);
+  if (lane == 0) joined[i] = t;
+}
+
+// s_join[group of the slab]: from the entries (joined == nullptr), or from what was joined before
+template <bool STATS>
+__device__ __forceinline__ void block_join(const GnArgs& a, const GnGrid& src, const Place& p, const float2* part,
+                                           const float2* joined, float2* s_join) {
+  const int g0 = p.c0 / src.per_group, count = (p.c0 + p.width - 1) / src.per_group - g0 + 1;
+  int lanes = 1;
+  while (lanes < 64 && lanes * 2 * count <= kThreads) lanes *= 2;
+  const int i = threadIdx.x / lanes, lane = threadIdx.x % lanes, grp = g0 + min(i, count - 1);
+  const float2 t = STATS ? join_stats(a, src, part, p.img, grp, lane, lanes) : join_sums(a, src, part, p.img, grp, lane, lanes);
+  if (lane == 0 && i < count) s_join[i] = t;
+  __syncthreads();
+}
+
+template <typename TX, typename TY, bool ALIGNED>
+__global__ __launch_bounds__(kThreads, 4) void gn_fwd_kernel(GnArgs a, GnGrid g, GnGrid src, const TX* x, const float* gamma,
+                                                          const float* beta, const float2* part, const float2* joined,
+                                                          TY* y, float* mean, float* rstd) {
+  __shared__ float2 s_join[kThreads];
+  const Place p(a, g);
+  const TX* xp = x + (int64_t)p.img * a.m * a.ldx + p.col;
+  TY* yp = y + (int64_t)p.img * a.m * a.ldy + p.col;
+  Raw<TX> v[kHalf], w[kHalf];
+  const int64_t turn = (int64_t)kHalf * g.side;
+  if (p.count > 0) {
+    get_rows<ALIGNED>(xp, a.ldx, p.row, p.end, g.side, p.count, v);
+    get_rows<ALIGNED>(xp, a.ldx, p.row + turn, p.end, g.side, p.count, w);
+  }
+  const Gain gain(gamma, beta, p.count > 0 ? p.col : 0, p.count);
+  if (joined == nullptr) block_join<true>(a, src, p, part, joined, s_join);
+  const int g0 = p.c0 / g.per_group;
+  // the first range's blocks write the statistics of the groups that start in their slab
+  if (blockIdx.x == 0)
+    for (int grp = (p.c0 + g.per_group - 1) / g.per_group + threadIdx.x; grp * g.per_group < p.c0 + p.width; grp += kThreads) {
+      const int64_t i = (int64_t)p.img * a.groups + grp;
+      const float2 t = joined == nullptr ? s_join[grp - g0] : joined[i];
+      if (mean != nullptr) mean[i] = t.x;
+      if (rstd != nullptr) rstd[i] = t.y;
+    }
+  if (p.count <= 0) return;
+  float mu[V], scale[V];
+  each_channel(p.col, p.count, g.per_group, [&](int e, int grp) __attribute__((always_inline)) {
+    const float2 t = joined == nullptr ? s_join[grp - g0] : joined[(int64_t)p.img * a.groups + grp];
+    mu[e] = t.x;
+    scale[e] = t.y * gain.gamma[e];
+  });
+  auto write = [&](int64_t r, const Raw<TX>(&u)[kHalf]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < kHalf; ++i)
+      if (r + i * g.side < p.end) {
+        float f[V];
+        u[i].values(f);
+#pragma unroll
+        for (int e = 0; e < V; ++e) f[e] = __builtin_fmaf(f[e] - mu[e], scale[e], gain.beta[e]);
+        act8(f, a.act);
+        put_some<ALIGNED>(yp + (r + i * g.side) * a.ldy, p.count, f);
+        row_done();
+      }
+  };
+  for (int64_t r = p.row; r < p.end; r += 2 * turn) {
+    write(r, v);
+    get_rows<ALIGNED>(xp, a.ldx, r + 2 * turn, p.end, g.side, p.count, v);
+    write(r + turn, w);
+    get_rows<ALIGNED>(xp, a.ldx, r + 3 * turn, p.end, g.side, p.count, w);
+  }
+}
+
+// Sums over a block's rows: of dt and of dt xh for each channel, sums[img][chunk][2][c], and of h and h xh for
+// each entry, part[img][chunk][entry]
+template <typename TX, typename TY, bool ALIGNED>
+__global__ __launch_bounds__(kThreads) void gn_bwd_sums_kernel(GnArgs a, GnGrid g, const TY* dy, const TX* x,
+                                                               const float* mean, const float* rstd, const float* gamma,
+                                                               const float* beta, float* sums, float2* part) {
+  __shared__ float s_a[kThreads * V], s_b[kThreads * V];
+  const Place p(a, g);
+  if (p.count > 0) {
+    constexpr int N = kHalf;
+    const TX* xp = x + (int64_t)p.img * a.m * a.ldx + p.col;
+    const TY* dp = dy + (int64_t)p.img * a.m * a.ldy + p.col;
+    Raw<TX> v[N];
+    Raw<TY> d[N];
+    get_rows<ALIGNED>(xp, a.ldx, p.row, p.end, g.side, p.count, v);
+    get_rows<ALIGNED>(dp, a.ldy, p.row, p.end, g.side, p.count, d);
+    const Gain gain(gamma, beta, p.col, p.count);
+    float mu[V], rs[V], s1[V] = {}, s2[V] = {};
+    each_channel(p.col, p.count, g.per_group, [&](int e, int grp) __attribute__((always_inline)) {
+      mu[e] = mean[(int64_t)p.img * a.groups + grp];
+      rs[e] = rstd[(int64_t)p.img * a.groups + grp];
+    });
+    for (int64_t r = p.row; r < p.end; r += (int64_t)N * g.side) {
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        if (r + i * g.side < p.end) {
+          float f[V], t[V];
+          v[i].values(f);
+          d[i].values(t);
+          grads8(f, t, mu, rs, gain, a.act);
+#pragma unroll
+          for (int e = 0; e < V; ++e) {
+            s1[e] += t[e];
+            s2[e] = __builtin_fmaf(t[e], f[e], s2[e]);
+          }
+          row_done();
+        }
+      get_rows<ALIGNED>(xp, a.ldx, r + (int64_t)N * g.side, p.end, g.side, p.count, v);
+      get_rows<ALIGNED>(dp, a.ldy, r + (int64_t)N * g.side, p.end, g.side, p.count, d);
+    }
+#pragma unroll
+    for (int e = 0; e < V; ++e)
+      if (e < p.count) {
+        s_a[p.lane_row * p.width + p.at + e] = s1[e];
+        s_b[p.lane_row * p.width + p.at + e] = s2[e];
+      }
+  }
+  __syncthreads();
+  slab_sums<kThreads>(s_a, s_b, p.width, g.side);
+  float* out = sums + ((int64_t)p.img * g.chunks + blockIdx.x) * 2 * a.c + p.c0;
+  for (int c = threadIdx.x; c < p.width; c += kThreads) {
+    out[c] = s_a[c];
+    out[a.c + c] = s_b[c];
+  }
+  float2* pt = part + ((int64_t)p.img * g.chunks + blockIdx.x) * entries(a, g) + blockIdx.y;
+  each_group<kThreads>(p.c0, p.width, g.per_group, [&](int grp, int lo, int hi, int lane, int lanes) __attribute__((always_inline)) {
+    float h1 = 0.f, h2 = 0.f;
+    for (int c = lo + lane; c < hi; c += lanes) {
+      const float ga = gamma != nullptr ? gamma[p.c0 + c] : 1.f;
+      h1 = __builtin_fmaf(ga, s_a[c], h1);
+      h2 = __builtin_fmaf(ga, s_b[c], h2);
+    }
+    h1 = lane_sum(h1, lanes);
+    h2 = lane_sum(h2, lanes);
+    if (lane == 0 && hi > lo) pt[grp] = make_float2(h1, h2);
+  });
+}
+
+template <typename TX, typename TY, bool ALIGNED>
+__global__ __launch_bounds__(kThreads, 3) void gn_bwd_kernel(GnArgs a, GnGrid g, GnGrid src, const TY* dy, const TX* x,
+                                                          const float* mean, const float* rstd, const float* gamma,
+                                                          const float* beta, const TX* res, const float2* part,
+                                                          const float2* joined, TX* dx) {
+  __shared__ float2 s_join[kThreads];
+  constexpr int N = kHalf;
+  const Place p(a, g);
+  const TX* xp = x + (int64_t)p.img * a.m * a.ldx + p.col;
+  const TY* dp = dy + (int64_t)p.img * a.m * a.ldy + p.col;
+  const TX* rp = res != nullptr ? res + (int64_t)p.img * a.m * a.ldr + p.col : nullptr;
+  TX* op = dx + (int64_t)p.img * a.m * a.lddx + p.col;
+  Raw<TX> v[N];
+  Raw<TY> d[N];
+  if (p.count > 0) {
+    get_rows<ALIGNED>(xp, a.ldx, p.row, p.end, g.side, p.count, v);
+    get_rows<ALIGNED>(dp, a.ldy, p.row, p.end, g.side, p.count, d);
+  }
+  const Gain gain(gamma, beta, p.count > 0 ? p.col : 0, p.count);
+  if (joined == nullptr) block_join<false>(a, src, p, part, joined, s_join);
+  if (p.count <= 0) return;
+  const int g0 = p.c0 / g.per_group;
+  float mu[V], rs[V], h1[V], h2[V];
+  each_channel(p.col, p.count, g.per_group, [&](int e, int grp) __attribute__((always_inline)) {
+    const int64_t at = (int64_t)p.img * a.groups + grp;
+    mu[e] = mean[at];
+    rs[e] = rstd[at];
+    const float2 t = joined == nullptr ? s_join[grp - g0] : joined[at];
+    h1[e] = t.x;
+    h2[e] = t.y;
+  });
+  for (int64_t r = p.row; r < p.end; r += (int64_t)N * g.side) {
+    if (r != p.row) {
+      get_rows<ALIGNED>(xp, a.ldx, r, p.end, g.side, p.count, v);
+      get_rows<ALIGNED>(dp, a.ldy, r, p.end, g.side, p.count, d);
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (r + i * g.side < p.end) {
+        float f[V], t[V], q[V] = {};
+        if (rp != nullptr) get_some<ALIGNED>(rp + (r + i * g.side) * a.ldr, p.count, q);
+        v[i].values(f);
+        d[i].values(t);
+        grads8(f, t, mu, rs, gain, a.act);
+#pragma unroll
+        for (int e = 0; e < V; ++e)
+          t[e] = __builtin_fmaf(rs[e], __builtin_fmaf(t[e], gain.gamma[e], -h1[e]) - f[e] * h2[e], q[e]);
+        put_some<ALIGNED>(op + (r + i * g.side) * a.lddx, p.count, t);
+        row_done();
+      }
+  }
+}
+
+// ---------------------------------------------------------------------------
 // f(TX, TY, ALIGNED)
 template <typename F>
 void with_types(const GnArgs& a, bool aligned, F&& f) {
@@ -437,76 +854,168 @@ void with_types(const GnArgs& a, bool aligned, F&& f) {
   else typed(bf16_t{}, bf16_t{});
 }
 
-// blocks of the passes: what they read is bound for HBM
-GnGrid sums_grid(const GnArgs& a) { return make_grid(a, 2048, 256); }
-GnGrid apply_grid(const GnArgs& a) { return make_grid(a, 4096, 1 << 20); }
+constexpr int kHeldThreads = 512;
 
-bool rows_aligned(const GnArgs& a) { return a.ldx % V == 0 && a.ldy % V == 0; }
+// Whether an image's groups are held, and by which blocks: the fewest whole groups that are whole vectors, more of
+// them while rows of a slab are short of a cache line and there are blocks enough.  held_rows: rows that a thread's
+// registers hold.
+bool make_held(const GnArgs& a, int held_rows, GnHeld* g) {
+  const int per = a.c / a.groups;
+  int width = per;
+  while (width % V != 0 && width < a.c) width += per;
+  if (width % V != 0 || a.c % width != 0) width = per;  // (the last vector of a slab is then a part of one)
+  auto rows = [&](int w) {
+    const int cols = (w + V - 1) / V;
+    return cols > kHeldThreads / 2 ? INT64_MAX : (a.m + kHeldThreads / cols - 1) / (kHeldThreads / cols);
+  };
+  const int bytes = a.x_f32 ? 4 : 2;
+  if (rows(width) > held_rows) return false;
+  while (width * bytes < 128 && a.c % (2 * width) == 0 && rows(2 * width) <= held_rows &&
+         (int64_t)a.n * a.c / (2 * width) >= 512)
+    width *= 2;
+  if ((int64_t)a.n * (a.c / width) > ((1ll << 32) - 1) / kHeldThreads) return false;  // (threads of a launch)
+  g->width = width;
+  g->slabs = a.c / width;
+  g->cols = (width + V - 1) / V;
+  g->side = (int)std::min<int64_t>(kHeldThreads / g->cols, a.m);
+  g->rows = (int)((a.m + g->side - 1) / g->side);
+  g->per_group = per;
+  return true;
+}
+size_t held_lds(const GnHeld& g, int arrays) { return (size_t)(2 * g.side + arrays) * g.width * sizeof(float); }
+
+// Rows that a thread of the held kernels holds at most: a row takes 4 registers of bf16 and 8 of fp32, the
+// backward two of them
+int held_fwd_rows(const GnArgs& a) { return a.x_f32 ? 8 : 16; }
+int held_bwd_rows(const GnArgs& a) { return a.x_f32 || a.y_f32 ? 6 : 10; }
+// f(rows) for the fewest of ROWS... that are enough
+template <int FIRST, int... REST, typename F>
+void with_rows(int rows, F&& f) {
+  if constexpr (sizeof...(REST) == 0) f(std::integral_constant<int, FIRST>{});
+  else if (rows <= FIRST) f(std::integral_constant<int, FIRST>{});
+  else with_rows<REST...>(rows, f);
+}
+
+// Blocks of the passes: as many as run at a time (four to a CU of the forward's, three of the backward's), so that
+// no part of a round is left for the end
+GnGrid stats_grid(const GnArgs& a) { return make_grid(a, 1024, 256); }
+GnGrid fwd_grid(const GnArgs& a) { return make_grid(a, 1024, 1 << 20); }
+GnGrid sums_grid(const GnArgs& a) { return make_grid(a, 768, 256); }
+GnGrid bwd_grid(const GnArgs& a) { return make_grid(a, 768, 1 << 20); }
 
 }  // namespace
 
 size_t gn_fwd_ws(const GnArgs& a) {
-  const GnGrid g = sums_grid(a);
+  GnHeld h;
+  if (make_held(a, held_fwd_rows(a), &h)) return 0;
+  const GnGrid g = stats_grid(a);
   return ((size_t)a.n * a.groups + (size_t)a.n * g.chunks * entries(a, g)) * sizeof(float2);
 }
 
 hipError_t gn_fwd_launch(const GnArgs& a, const void* x, const float* gamma, const float* beta, void* y, float* mean,
                          float* rstd, void* ws, hipStream_t s) {
-  const GnGrid g = sums_grid(a), ga = apply_grid(a);
-  float2* stats = static_cast<float2*>(ws);
-  float2* part = stats + (size_t)a.n * a.groups;
-  with_types(a, rows_aligned(a), [&](auto tx, auto ty, auto al) {
+  GnHeld h;
+  const bool held = make_held(a, held_fwd_rows(a), &h);
+  const bool aligned = a.ldx % V == 0 && a.ldy % V == 0 && (!held || h.width % V == 0 || h.slabs == 1);
+  with_types(a, aligned, [&](auto tx, auto ty, auto al) {
     using TX = decltype(tx);
     using TY = decltype(ty);
     constexpr bool AL = decltype(al)::value;
+    const TX* xp = static_cast<const TX*>(x);
+    TY* yp = static_cast<TY*>(y);
+    if (held) {
+      trace_begin(KC_GN_FWD);
+      auto go = [&](auto nv) {
+        NUMBAT_LAUNCH((gn_fwd_held_kernel<TX, TY, AL, decltype(nv)::value, kHeldThreads>), dim3((unsigned)(a.n * h.slabs)),
+                      dim3(kHeldThreads), held_lds(h, 3), s, a, h, xp, gamma, beta, yp, mean, rstd);
+      };
+      if constexpr (sizeof(TX) == 4) with_rows<2, 8>(h.rows, go);
+      else with_rows<2, 8, 16>(h.rows, go);
+      trace_end(KC_GN_FWD);
+      return;
+    }
+    const GnGrid g = stats_grid(a), ga = fwd_grid(a);
+    float2* joined = static_cast<float2*>(ws);
+    float2* part = joined + (size_t)a.n * a.groups;
     trace_begin(KC_GN_STATS);
-    NUMBAT_LAUNCH((gn_stats_kernel<TX, AL>), blocks_of(a, g), dim3(kThreads), 0, s, a, g, static_cast<const TX*>(x), part);
-    const unsigned joins = (unsigned)(((int64_t)a.n * a.groups + kThreads / 64 - 1) / (kThreads / 64));
-    NUMBAT_LAUNCH(gn_join_kernel, dim3(joins), dim3(kThreads), 0, s, a, g, part, stats, mean, rstd);
+    NUMBAT_LAUNCH((gn_stats_kernel<TX, AL>), blocks_of(a, g), dim3(kThreads), 0, s, a, g, xp, part);
+    if (joins_in_block(a, g)) {
+      joined = nullptr;
+    } else {
+      const unsigned joins = (unsigned)(((int64_t)a.n * a.groups + kThreads / 64 - 1) / (kThreads / 64));
+      NUMBAT_LAUNCH((gn_join_kernel<true>), dim3(joins), dim3(kThreads), 0, s, a, g, part, joined);
+    }
     trace_end(KC_GN_STATS);
     trace_begin(KC_GN_FWD);
-    NUMBAT_LAUNCH((gn_fwd_kernel<TX, TY, AL>), blocks_of(a, ga), dim3(kThreads), 0, s, a, ga, static_cast<const TX*>(x),
-                  gamma, beta, stats, static_cast<TY*>(y));
+    NUMBAT_LAUNCH((gn_fwd_kernel<TX, TY, AL>), blocks_of(a, ga), dim3(kThreads), 0, s, a, ga, g, xp, gamma, beta, part,
+                  joined, yp, mean, rstd);
     trace_end(KC_GN_FWD);
   });
   return hipGetLastError();
 }
 
 size_t gn_bwd_ws(const GnArgs& a) {
+  GnHeld h;
+  if (make_held(a, held_bwd_rows(a), &h)) return (size_t)a.n * 2 * a.c * sizeof(float);
   const GnGrid g = sums_grid(a);
-  return (size_t)a.n * a.groups * sizeof(float2) + (size_t)a.n * (g.chunks + 1) * 2 * a.c * sizeof(float);
+  return (size_t)a.n * (a.groups + (size_t)g.chunks * entries(a, g)) * sizeof(float2) +
+         (size_t)a.n * g.chunks * 2 * a.c * sizeof(float);
 }
 
 hipError_t gn_bwd_launch(const GnArgs& a, const void* dy, const void* x, const float* mean, const float* rstd,
-                         const float* gamma, const float* beta, void* dx, float* dgamma, float* dbeta, int accumulate,
-                         void* ws, hipStream_t s) {
-  const GnGrid g = sums_grid(a), ga = apply_grid(a);
-  float2* means = static_cast<float2*>(ws);
-  float* sums = reinterpret_cast<float*>(means + (size_t)a.n * a.groups);
-  float* part = sums + (size_t)a.n * 2 * a.c;
-  with_types(a, rows_aligned(a) && a.lddx % V == 0, [&](auto tx, auto ty, auto al) {
+                         const float* gamma, const float* beta, const void* res, void* dx, float* dgamma, float* dbeta,
+                         int accumulate, void* ws, hipStream_t s) {
+  GnHeld h;
+  const bool held = make_held(a, held_bwd_rows(a), &h);
+  const bool aligned = a.ldx % V == 0 && a.ldy % V == 0 && (dx == nullptr || a.lddx % V == 0) &&
+                       (res == nullptr || a.ldr % V == 0) && (!held || h.width % V == 0 || h.slabs == 1);
+  const bool vectors = dgamma != nullptr || dbeta != nullptr;
+  float* sums = static_cast<float*>(ws);
+  int ranges = a.n;  // rows of sums
+  with_types(a, aligned, [&](auto tx, auto ty, auto al) {
     using TX = decltype(tx);
     using TY = decltype(ty);
     constexpr bool AL = decltype(al)::value;
-    const TX* xp = static_cast<const TX*>(x);
+    const TX *xp = static_cast<const TX*>(x), *rp = static_cast<const TX*>(res);
     const TY* dp = static_cast<const TY*>(dy);
+    TX* op = static_cast<TX*>(dx);
+    if (held) {
+      trace_begin(KC_GN_BWD);
+      auto go = [&](auto nv) {
+        NUMBAT_LAUNCH((gn_bwd_held_kernel<TX, TY, AL, decltype(nv)::value, kHeldThreads>), dim3((unsigned)(a.n * h.slabs)),
+                      dim3(kHeldThreads), held_lds(h, 2), s, a, h, dp, xp, mean, rstd, gamma, beta, rp, op,
+                      vectors ? sums : nullptr);
+      };
+      if constexpr (sizeof(TX) == 4 || sizeof(TY) == 4) with_rows<2, 6>(h.rows, go);
+      else with_rows<2, 6, 10>(h.rows, go);
+      trace_end(KC_GN_BWD);
+      return;
+    }
+    const GnGrid g = sums_grid(a), ga = bwd_grid(a);
+    ranges = a.n * g.chunks;
+    float2* joined = reinterpret_cast<float2*>(sums + (size_t)ranges * 2 * a.c);
+    float2* part = joined + (size_t)a.n * a.groups;
     trace_begin(KC_GN_BWD_SUMS);
     NUMBAT_LAUNCH((gn_bwd_sums_kernel<TX, TY, AL>), blocks_of(a, g), dim3(kThreads), 0, s, a, g, dp, xp, mean, rstd, gamma,
-                  beta, part);
-    NUMBAT_LAUNCH(gn_bwd_join_kernel, dim3((unsigned)a.groups, (unsigned)a.n), dim3(kThreads), 0, s, a, g, part, gamma,
-                  sums, means);
+                  beta, sums, part);
+    if (joins_in_block(a, g)) {
+      joined = nullptr;
+    } else if (dx != nullptr) {
+      const unsigned joins = (unsigned)(((int64_t)a.n * a.groups + kThreads / 64 - 1) / (kThreads / 64));
+      NUMBAT_LAUNCH((gn_join_kernel<false>), dim3(joins), dim3(kThreads), 0, s, a, g, part, joined);
+    }
     trace_end(KC_GN_BWD_SUMS);
     if (dx != nullptr) {
       trace_begin(KC_GN_BWD);
-      NUMBAT_LAUNCH((gn_bwd_kernel<TX, TY, AL>), blocks_of(a, ga), dim3(kThreads), 0, s, a, ga, dp, xp, mean, rstd, gamma,
-                    beta, means, static_cast<TX*>(dx));
+      NUMBAT_LAUNCH((gn_bwd_kernel<TX, TY, AL>), blocks_of(a, ga), dim3(kThreads), 0, s, a, ga, g, dp, xp, mean, rstd, gamma,
+                    beta, rp, part, joined, op);
       trace_end(KC_GN_BWD);
     }
   });
   const hipError_t e = hipGetLastError();
-  if (e != hipSuccess || (dgamma == nullptr && dbeta == nullptr)) return e;
+  if (e != hipSuccess || !vectors) return e;
   trace_begin(KC_GN_BWD_FINISH);
-  column_sum_launch(sums, a.n, 2 * (int64_t)a.c, 2 * a.c, a.c, dbeta, dgamma, accumulate, s);
+  column_sum_launch(sums, ranges, 2 * (int64_t)a.c, 2 * a.c, a.c, dbeta, dgamma, accumulate, s);
   trace_end(KC_GN_BWD_FINISH);
   return hipGetLastError();
 }

@@ -101,7 +101,7 @@ class numbat_group_norm_problem(ctypes.Structure):
     _fields_ = [("struct_size", ctypes.c_uint32), ("n", ctypes.c_int32), ("m", ctypes.c_int64), ("c", ctypes.c_int32),
                 ("groups", ctypes.c_int32), ("act", ctypes.c_int32), ("eps", ctypes.c_float), ("x_type", ctypes.c_int32),
                 ("y_type", ctypes.c_int32), ("x_row_stride", ctypes.c_int64), ("y_row_stride", ctypes.c_int64),
-                ("dx_row_stride", ctypes.c_int64)]
+                ("r_row_stride", ctypes.c_int64), ("dx_row_stride", ctypes.c_int64)]
 
 
 class numbat_rotary_problem(ctypes.Structure):
@@ -179,7 +179,7 @@ def load() -> ctypes.CDLL:
                                                   ctypes.c_int32, D, D, D, ctypes.c_int64, D, P, P, S, P]),
             "numbat_adamw_state_values": (ctypes.c_int, [ctypes.c_int64, P, P, P, P, P, P, P]),
             "numbat_group_norm_fwd": (ctypes.c_int, [GP, P, P, P, P, P, P, P, S, P]),
-            "numbat_group_norm_bwd": (ctypes.c_int, [GP, P, P, P, P, P, P, P, P, P, ctypes.c_int, P, S, P]),
+            "numbat_group_norm_bwd": (ctypes.c_int, [GP, P, P, P, P, P, P, P, P, P, P, ctypes.c_int, P, S, P]),
             "numbat_rotary": (ctypes.c_int, [RP, P, P, P, P]),
             "numbat_attention_fwd": (ctypes.c_int, [AP, P, P, P, P, P, P, P, P, S, P]),
             "numbat_attention_bwd": (ctypes.c_int, [AP, P, P, P, P, P, P, P, P, P, P, P, P, S, P]),
@@ -481,9 +481,9 @@ def numbat_adamw_state_values(n, m, m_unit, v, v_unit, m_value, v_value, stream=
 
 
 def group_norm_problem(n, m, c, groups, act=ACT_NONE, eps=1e-5, x_type=BF16, y_type=BF16, x_row_stride=0, y_row_stride=0,
-                       dx_row_stride=0):
+                       r_row_stride=0, dx_row_stride=0):
     return numbat_group_norm_problem(ctypes.sizeof(numbat_group_norm_problem), n, m, c, groups, act, eps, x_type, y_type,
-                                     x_row_stride, y_row_stride, dx_row_stride)
+                                     x_row_stride, y_row_stride, r_row_stride, dx_row_stride)
 
 
 def numbat_group_norm_fwd(p, x, gamma, beta, y, mean=None, rstd=None, ws=None, stream=None, ws_bytes=None):
@@ -493,11 +493,12 @@ def numbat_group_norm_fwd(p, x, gamma, beta, y, mean=None, rstd=None, ws=None, s
            "numbat_group_norm_fwd")
 
 
-def numbat_group_norm_bwd(p, dy, x, mean, rstd, gamma, beta, dx, dgamma, dbeta, accumulate=False, ws=None, stream=None,
-                          ws_bytes=None):
+def numbat_group_norm_bwd(p, dy, x, mean, rstd, gamma, beta, dx, dgamma, dbeta, accumulate=False, ws=None,
+                          residual_grad=None, stream=None, ws_bytes=None):
     _check(load().numbat_group_norm_bwd(ctypes.byref(p), _ptr(dy), _ptr(x), _ptr(mean), _ptr(rstd), _ptr(gamma),
-                                        _ptr(beta), _ptr(dx), _ptr(dgamma), _ptr(dbeta), int(bool(accumulate)),
-                                        _ptr(ws), _nbytes(ws) if ws_bytes is None else ws_bytes, _stream(stream)),
+                                        _ptr(beta), _ptr(residual_grad), _ptr(dx), _ptr(dgamma), _ptr(dbeta),
+                                        int(bool(accumulate)), _ptr(ws), _nbytes(ws) if ws_bytes is None else ws_bytes,
+                                        _stream(stream)),
            "numbat_group_norm_bwd")
 
 

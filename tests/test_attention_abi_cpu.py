@@ -30,8 +30,8 @@ def test_header_binding_and_library_agree():
     assert names == set(nb.EXPORTED_ATTENTION)
     for n in names:
         assert getattr(nb.load(), n) is not None and callable(getattr(nb, n))
-    # uint32, int32, int64, 3 int32, float, 2 int32, 3 int64
-    assert ctypes.sizeof(nb.numbat_group_norm_problem) == 64
+    # uint32, int32, int64, 3 int32, float, 2 int32, 4 int64
+    assert ctypes.sizeof(nb.numbat_group_norm_problem) == 72
     # uint32, 3 int32, int64, 8 int32, 4 int32, double, 2 int64
     assert ctypes.sizeof(nb.numbat_rotary_problem) == 96
     # uint32, 7 int32, float, int32, 4 int64
@@ -52,19 +52,19 @@ def gn_fwd(p, x=P, y=P + 64, gamma=None, beta=None, mean=None, rstd=None, ws=P, 
     nb.numbat_group_norm_fwd(p, x, gamma, beta, y, mean, rstd, ws, ws_bytes=b)
 
 
-def gn_bwd(p, dy=P, x=P, mean=P, rstd=P, gamma=None, beta=None, dx=P + 64, dg=P, db=None, ws=P, b=1 << 40):
-    nb.numbat_group_norm_bwd(p, dy, x, mean, rstd, gamma, beta, dx, dg, db, False, ws, ws_bytes=b)
+def gn_bwd(p, dy=P, x=P, mean=P, rstd=P, gamma=None, beta=None, res=None, dx=P + 64, dg=P, db=None, ws=P, b=1 << 40):
+    nb.numbat_group_norm_bwd(p, dy, x, mean, rstd, gamma, beta, dx, dg, db, False, ws, residual_grad=res, ws_bytes=b)
 
 
 @pytest.mark.parametrize("call,op", [(gn_fwd, nb.OP_GROUP_NORM_FWD), (gn_bwd, nb.OP_GROUP_NORM_BWD)])
 def test_group_norm_refusals(call, op):
-    make = lambda **kw: nb.group_norm_problem(**{"n": 2, "m": 5000, "c": 24, "groups": 3, **kw})  # noqa: E731
+    make = lambda **kw: nb.group_norm_problem(**{"n": 2, "m": 50000, "c": 24, "groups": 3, **kw})  # noqa: E731
     bad = make()
     bad.struct_size += 8
     assert status_of(call, bad) == nb.ERR_VERSION
     for kw in ({"n": -1}, {"m": -1}, {"c": 0}, {"groups": 0}, {"groups": 5}, {"groups": 25}, {"act": 5}, {"act": -1},
                {"eps": -1.0}, {"eps": float("nan")}, {"eps": float("inf")}, {"x_type": 2}, {"y_type": -1},
-               {"x_row_stride": 23}, {"y_row_stride": -24}, {"dx_row_stride": (1 << 21) + 8}):
+               {"x_row_stride": 23}, {"y_row_stride": -24}, {"r_row_stride": 8}, {"dx_row_stride": (1 << 21) + 8}):
         assert status_of(call, make(**kw)) == nb.ERR_BAD_DESC, kw
         assert status_of(nb.numbat_workspace_size, op, make(**kw)) == nb.ERR_BAD_DESC, kw
     for kw in ({"n": 65536}, {"c": 65544, "groups": 3}, {"m": 1 << 31}):
@@ -74,7 +74,7 @@ def test_group_norm_refusals(call, op):
         if call is gn_bwd and arg == "y":
             continue
         assert status_of(call, p, **{arg: None}) == nb.ERR_NULL, arg
-    for arg in ("x", "dy", "dx") if call is gn_bwd else ("x", "y"):
+    for arg in ("x", "dy", "dx", "res") if call is gn_bwd else ("x", "y"):
         assert status_of(call, p, **{arg: P + 8}) == nb.ERR_ALIGN, arg
     for arg in ("gamma", "beta", "mean", "rstd"):
         assert status_of(call, p, **{arg: P + 2}) == nb.ERR_ALIGN, arg
@@ -95,7 +95,9 @@ def test_group_norm_in_place():
     assert status_of(gn_bwd, make(dx_row_stride=32), dx=P, dy=P + 64) == nb.ERR_BAD_DESC
     assert status_of(gn_bwd, make(y_row_stride=32), dx=P, x=P + 64) == nb.ERR_BAD_DESC
     assert status_of(gn_bwd, make(y_type=nb.F32), dx=P, x=P + 64) == nb.ERR_BAD_DESC
+    assert status_of(gn_bwd, make(r_row_stride=32), dx=P, res=P, x=P + 64, dy=P + 64) == nb.ERR_BAD_DESC
     assert status_of(gn_bwd, make(), dx=None, dg=None) == nb.ERR_NULL
+    assert status_of(gn_bwd, make(), dx=None, res=P) == nb.ERR_NULL
 
 
 def test_rotary_refusals():

@@ -3,7 +3,7 @@ side, odd channels, rows and strides, groups of one channel and of all, one row,
 zero, in place.
 
 Bounds.  A thread adds at most 64 rows after a shift that lies within their spread (twice the centred squares
-at most), 128 threads' sums are joined one after another, then lanes, channels and ranges: sums are at
+at most), at most 128 sums are joined one after another, then lanes, channels and ranges: sums are at
 most 256 additions deep, so a mean is off by 256 2^-24 of the values' size and a variance by 512 2^-24 of
 itself.  Activations: 2^-20 of their argument, slopes 2^-20 (1 + |t|), and a change of t enters by a
 slope of at most 1.13 (a second derivative of at most 1.2)."""
@@ -23,7 +23,13 @@ DEEP = 256 * U
 # images, rows, channels, groups
 SIZES = [(1, 1, 8, 1), (1, 1, 6, 2), (2, 3, 7, 7), (1, 400, 576, 32), (2, 1600, 96, 32), (3, 77, 327, 3), (2, 6400, 48, 8),
          (1, 130, 2056, 257), (1, 9, 4104, 1), (2, 50, 24, 24), (1, 5000, 9, 1), (5, 31, 40, 5), (1, 25600, 16, 2),
-         (70, 2, 64, 4), (1, 33, 5000, 4), (1, 1601, 384, 32), (3, 6500, 192, 32)]
+         (70, 2, 64, 4), (1, 33, 5000, 4), (1, 1601, 384, 32), (3, 6500, 192, 32),
+         # held: one row of threads' registers after another full, slabs of several groups, groups that are no whole
+         # vectors, and the sizes past which the passes take over
+         (1, 170, 24, 2), (1, 171, 24, 2), (1, 2040, 24, 2), (1, 2050, 24, 2), (1, 2720, 24, 2), (1, 2721, 24, 2),
+         (40, 200, 96, 24), (2, 500, 54, 3), (2, 700, 15, 1), (33, 16, 2048, 1), (3, 10, 2056, 1),
+         # passes: groups over several slabs, groups too many to join in every block, many images
+         (2, 3000, 4100, 2), (1, 6000, 2048, 2048), (65, 1300, 40, 1)]
 
 
 def matrix(rows, c, seed, dtype, pitch=0, scale=1.0, mean=1.0, ends=float("nan")):
@@ -47,7 +53,7 @@ def problem(n, m, c, groups, name, xt, yt, pitch, eps):
     code = {"bf16": nb.BF16, "f32": nb.F32}
     return nb.group_norm_problem(n, m, c, groups, act=getattr(nb, "ACT_" + name.upper()), eps=eps, x_type=code[xt],
                                  y_type=code[yt], x_row_stride=c + pitch, y_row_stride=c + pitch,
-                                 dx_row_stride=c + pitch)
+                                 r_row_stride=c + pitch, dx_row_stride=c + pitch)
 
 
 def space(op, p):
@@ -182,6 +188,13 @@ def backward(n, m, c, groups, name="silu", xt="bf16", yt="bf16", pitch=0, affine
         once = dx.clone(), dg.clone(), db.clone()
         nb.numbat_group_norm_bwd(p, dy, x, mu, rs, gamma, beta, *args, True, ws)
         assert torch.equal(dx, once[0]) and torch.equal(dg, 2 * once[1]) and torch.equal(db, 2 * once[2])
+        res = matrix(n * m, c, seed + 9, TYPES[xt], pitch)
+        nb.numbat_group_norm_bwd(p, dy, x, mu, rs, gamma, beta, dx[:, :c], None, None, False, ws, residual_grad=res)
+        both = dx_ref + d(res)  # the sum is rounded once
+        close(dx[:, :c], both, rstd * off + 2 * U * (dx_ref.abs() + d(res).abs()) + (B if xt == "bf16" else U) * both.abs(), "dx + residual")
+        mine = torch.empty_strided(res.shape, (c + pitch, 1), dtype=res.dtype, device="cuda").copy_(res)
+        nb.numbat_group_norm_bwd(p, dy, x, mu, rs, gamma, beta, mine, None, None, False, ws, residual_grad=mine)
+        assert torch.equal(mine, dx[:, :c])
         for buf in ((x,) if xt != yt else (x, dy)):  # in the buffer of either operand
             mine = torch.empty_strided(buf.shape, (c + pitch, 1), dtype=buf.dtype, device="cuda").copy_(buf)
             nb.numbat_group_norm_bwd(p, mine if buf is dy else dy, mine if buf is x else x, mu, rs, gamma, beta, mine, None,
