@@ -74,11 +74,13 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_fwd_kernel(AttnArgs a, AttnGr
   float most = -INFINITY, sum = 0.f;  // log2 of the weights' unit; this half's sum of weights
 
   auto tile = [&](const unsigned char* st, int key) __attribute__((always_inline)) {
-    f32x16 s[2] = {zeros16(), zeros16()};
+    f32x16 s[2];
+    u32x4 vf[2][FB];  // v's operands of two slices of 16 keys
+    auto read_v = [&](int u) __attribute__((always_inline)) {
 #pragma unroll
-    for (int k = 0; k < KS; ++k)
-#pragma unroll
-      for (int i = 0; i < 2; ++i) s[i] = mfma32x32x16(along.read(st, i, k), qf[k], s[i]);
+      for (int f = 0; f < FB; ++f) vf[u & 1][f] = across.read(st + H::TILE, f, u);
+    };
+    along_pair<DP>(along, st, 0, st, 1, qf, qf, s[0], s[1], [&] { read_v(0); });
     if (key + kTile > wave_all) {
 #pragma unroll
       for (int i = 0; i < 2; ++i)
@@ -110,13 +112,14 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_fwd_kernel(AttnArgs a, AttnGr
         sum += s[i][r];
       }
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int u = 0; u < 4; ++u) {
+      if (u < 3) read_v(u + 1);
+      const u32x4 w = operand(s[u / 2], u % 2);
+      pin();
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const u32x4 w = operand(s[i], u);
-#pragma unroll
-        for (int f = 0; f < FB; ++f) o[f] = mfma32x32x16(across.read(st + H::TILE, f, 2 * i + u), w, o[f]);
-      }
+      for (int f = 0; f < FB; ++f) o[f] = mfma32x32x16(vf[u & 1][f], w, o[f]);
+      pin();
+    }
   };
   auto step = [&](unsigned char* st, unsigned char* next, int key) __attribute__((always_inline)) {
     stage_ready();  // this stage has landed, and every wave is done with the other

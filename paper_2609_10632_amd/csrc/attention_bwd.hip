@@ -12,6 +12,7 @@
 //         product, so their gradients are added in its sums.
 // Few columns, or few keys, are split into ranges of the other, whose sums a third kernel adds in order.
 #include <algorithm>
+#include <type_traits>
 
 #include "attention_tile.h"
 
@@ -105,12 +106,13 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_dq_kernel(AttnArgs a, AttnGri
   auto tile = [&](const unsigned char* st, int key) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      f32x16 s = zeros16(), dp = zeros16();
+      f32x16 s, dp;
+      u32x4 kf[2][FB];  // k's operands of two slices of 16 keys
+      auto read_k = [&](int u) __attribute__((always_inline)) {
 #pragma unroll
-      for (int k = 0; k < KS; ++k) {
-        s = mfma32x32x16(along.read(st, i, k), qf[k], s);
-        dp = mfma32x32x16(along.read(st + H::TILE, i, k), df[k], dp);
-      }
+        for (int f = 0; f < FB; ++f) kf[u][f] = across.read(st, f, 2 * i + u);
+      };
+      along_pair<DP>(along, st, i, st + H::TILE, i, qf, df, s, dp, [&] { read_k(0); });
 #pragma unroll
       for (int r = 0; r < 16; ++r)
         s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], a.scale_log2, -stat.x)) * (dp[r] - stat.y);
@@ -121,9 +123,12 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_dq_kernel(AttnArgs a, AttnGri
       }
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
+        if (u == 0) read_k(1);
         const u32x4 w = operand(s, u);
+        pin();
 #pragma unroll
-        for (int f = 0; f < FB; ++f) dq[f] = mfma32x32x16(across.read(st, f, 2 * i + u), w, dq[f]);
+        for (int f = 0; f < FB; ++f) dq[f] = mfma32x32x16(kf[u][f], w, dq[f]);
+        pin();
       }
     }
   };
@@ -210,6 +215,7 @@ __global__ __launch_bounds__(NW * 64, DP <= 64 ? 2 : 1) void attn_dkv_kernel(Att
       s_keys[u][tid] = n.keys(a, (int)fdiv((uint32_t)(c + tid), a.div_group));
     }
   };
+  constexpr int AHEAD = 2;  // slices of operands read ahead
   Along<DP> along;
   Across<DP> across;
   along.init(lane);
@@ -218,15 +224,13 @@ __global__ __launch_bounds__(NW * 64, DP <= 64 ? 2 : 1) void attn_dkv_kernel(Att
 #pragma unroll
   for (int f = 0; f < FB; ++f) dk[f] = dv[f] = zeros16();
 
-  auto tile = [&](const unsigned char* st, int u, bool masked) __attribute__((always_inline)) {
+  auto tile = [&](const unsigned char* st, int u, auto maskedc) __attribute__((always_inline)) {
+    constexpr bool masked = decltype(maskedc)::value;
+    const unsigned char *tq = st, *td = st + H::TILE;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      f32x16 s = zeros16(), dp = zeros16();
-#pragma unroll
-      for (int k = 0; k < KS; ++k) {
-        s = mfma32x32x16(along.read(st, i, k), kf[k], s);
-        dp = mfma32x32x16(along.read(st + H::TILE, i, k), vf[k], dp);
-      }
+      f32x16 s, dp;
+      along_pair<DP, AHEAD>(along, tq, i, td, i, kf, vf, s, dp, [] {});
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const int at = 32 * i + 8 * j + 4 * half;
@@ -236,48 +240,64 @@ __global__ __launch_bounds__(NW * 64, DP <= 64 ? 2 : 1) void attn_dkv_kernel(Att
         for (int e = 0; e < 4; ++e) {
           const int r = 4 * j + e;
           s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], a.scale_log2, -lse[e]));
-          dp[r] -= delta[e];
         }
-        if (masked) {
+        if constexpr (masked) {
           const int4 last = *reinterpret_cast<const int4*>(&s_keys[u][at]);
           const int l[4] = {last.x, last.y, last.z, last.w};
 #pragma unroll
           for (int e = 0; e < 4; ++e)
             if (key >= l[e]) s[4 * j + e] = 0.f;
         }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) dp[4 * j + e] = (dp[4 * j + e] - delta[e]) * s[4 * j + e];
       }
+      // operands read one product ahead
+      u32x4 x[2], y[2], pw, dw;
+      x[0] = across.read(td, 0, 2 * i);
+      y[0] = across.read(tq, 0, 2 * i);
 #pragma unroll
-      for (int r = 0; r < 16; ++r) dp[r] *= s[r];
-#pragma unroll
-      for (int w = 0; w < 2; ++w) {
-        const u32x4 pw = operand(s, w), dw = operand(dp, w);
-#pragma unroll
-        for (int f = 0; f < FB; ++f) {
-          dv[f] = mfma32x32x16(across.read(st + H::TILE, f, 2 * i + w), pw, dv[f]);
-          dk[f] = mfma32x32x16(across.read(st, f, 2 * i + w), dw, dk[f]);
+      for (int t = 0; t < 2 * FB; ++t) {
+        if (t % FB == 0) {
+          pw = operand(s, t / FB);
+          dw = operand(dp, t / FB);
         }
+        if (t + 1 < 2 * FB) {
+          x[(t + 1) & 1] = across.read(td, (t + 1) % FB, 2 * i + (t + 1) / FB);
+          y[(t + 1) & 1] = across.read(tq, (t + 1) % FB, 2 * i + (t + 1) / FB);
+        }
+        pin();
+        dv[t % FB] = mfma32x32x16(x[t & 1], pw, dv[t % FB]);
+        dk[t % FB] = mfma32x32x16(y[t & 1], dw, dk[t % FB]);
+        pin();
       }
     }
   };
-  auto step = [&](unsigned char* st, unsigned char* next, int u, int c) __attribute__((always_inline)) {
+  auto step = [&](unsigned char* st, unsigned char* next, int u, int c, auto maskedc) __attribute__((always_inline)) {
     stage_ready();  // this stage has landed, and every wave is done with the other
     float2 v = make_float2(INFINITY, 0.f);
     if (c + kTile < end) {
       load(next, c + kTile);
       v = stat_of(c + kTile);
     }
-    // (every column of the tile sees every key of the block from a certain row on)
-    tile(st, u, a.causal && n.keys(a, (int)fdiv((uint32_t)c, a.div_group)) < k0 + NW * 32);
+    tile(st, u, maskedc);
     if (c + kTile < end) put_stats(u ^ 1, c + kTile, v);
   };
   if (begin < end) {
     load(st0, begin);
     put_stats(0, begin, stat_of(begin));
   }
-  for (int c = begin; c < end; c += 2 * kTile) {
-    step(st0, st1, 0, c);
-    if (c + kTile < end) step(st1, st0, 1, c + kTile);
-  }
+  // Pairs of tiles, first those with a column that does not see every key of the block.  (Loops of their own: one
+  // with both kinds in it would move its accumulators from register to register.)
+  auto pairs = [&](int c, int to, auto maskedc) __attribute__((always_inline)) {
+    for (; c < to; c += 2 * kTile) {
+      step(st0, st1, 0, c, maskedc);
+      if (c + kTile < end) step(st1, st0, 1, c + kTile, maskedc);
+    }
+    return c;
+  };
+  const int64_t all = a.causal ? (int64_t)max(k0 + NW * 32 - 1 - (n.kv - n.q), 0) * a.group : 0;  // the first that sees all
+  const int from = pairs(begin, (int)min(all, (int64_t)end), std::true_type{});
+  pairs(from, end, std::false_type{});
 
   if (!valid)  // (rows behind the sequence's end)
 #pragma unroll

@@ -83,18 +83,18 @@ __device__ __forceinline__ void stage_ready() {
   asm volatile("" ::: "memory");
 }
 
-// operand rows of 32 along the features
+// Operand rows of 32 along the features.  (Where a lane's chunks lie differs by exclusive-ors of constants: one
+// address serves all.)
 template <int DP>
 struct Along {
   using H = Head<DP>;
-  uint32_t at[H::KS];
+  uint32_t at;
   __device__ __forceinline__ void init(int lane) {
     const int r = lane & 31;
-#pragma unroll
-    for (int k = 0; k < H::KS; ++k) at[k] = r * H::ROW + ((2 * k + (lane >> 5)) ^ H::swizzle(r)) * 16;
+    at = r * H::ROW + ((lane >> 5) ^ H::swizzle(r)) * 16;
   }
   __device__ __forceinline__ u32x4 read(const unsigned char* tile, int block, int k) const {
-    return *reinterpret_cast<const u32x4*>(tile + at[k] + block * 32 * H::ROW);
+    return *reinterpret_cast<const u32x4*>(tile + (at ^ (uint32_t)(32 * k)) + block * 32 * H::ROW);
   }
 };
 
@@ -102,38 +102,82 @@ struct Along {
 template <int DP>
 struct Across {
   using H = Head<DP>;
-  uint32_t at[H::FB][2];
+  uint32_t at;
   __device__ __forceinline__ void init(int lane) {
     // lanes of 16 read 4 rows x 16 features: lane 4 e + q of them 4 features of row e
     const int g = lane >> 4, e = lane >> 2 & 3, q = lane & 3;
-#pragma unroll
-    for (int f = 0; f < H::FB; ++f)
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const int r = 8 * u + 4 * (g >> 1) + e, c = 4 * f + 2 * (g & 1) + (q >> 1);
-        at[f][u] = r * H::ROW + (c ^ H::swizzle(r)) * 16 + (q & 1) * 8;
-      }
+    const int r = 4 * (g >> 1) + e, c = 2 * (g & 1) + (q >> 1);
+    at = r * H::ROW + (c ^ H::swizzle(r)) * 16 + (q & 1) * 8;
   }
+  // (8 rows further down the swizzle differs in bit 1)
   __device__ __forceinline__ u32x4 read(const unsigned char* tile, int f, int slice) const {
+    const unsigned char* p = tile + slice * 16 * H::ROW;
     const v2u_t lo = __builtin_bit_cast(
-        v2u_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s_t*)(tile + at[f][0] + slice * 16 * H::ROW)));
+        v2u_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s_t*)(p + (at ^ (uint32_t)(64 * f)))));
     const v2u_t hi = __builtin_bit_cast(
-        v2u_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s_t*)(tile + at[f][1] + slice * 16 * H::ROW)));
+        v2u_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s_t*)(p + (at ^ (uint32_t)(64 * f + 32)) + 8 * H::ROW)));
     return u32x4{lo.x, lo.y, hi.x, hi.y};
   }
 };
-
-// slice s (16 rows) of a 32 x 32 product's accumulators as an operand
-__device__ __forceinline__ u32x4 operand(const f32x16& x, int s) {
-  return u32x4{pack2(x[8 * s], x[8 * s + 1]), pack2(x[8 * s + 2], x[8 * s + 3]), pack2(x[8 * s + 4], x[8 * s + 5]),
-               pack2(x[8 * s + 6], x[8 * s + 7])};
-}
 
 __device__ __forceinline__ f32x16 zeros16() {
   f32x16 x;
 #pragma unroll
   for (int i = 0; i < 16; ++i) x[i] = 0.f;
   return x;
+}
+
+// Keeps what is written before it before, and what is written behind it behind.  The products' operands are
+// read from LDS some instructions ahead of their use; left to itself the compiler moves each read to its
+// use, where a wave waits out the LDS's latency.
+__device__ __forceinline__ void pin() { __builtin_amdgcn_sched_barrier(0); }
+
+// s[j] = sum over features of rows `block[j]` of tile[j] and the columns in f[j]: two products side by side, their
+// operands read two slices ahead.  behind(): reads for what follows, issued with the last slices.
+template <int DP, int AHEAD = 2, typename F>
+__device__ __forceinline__ void along_pair(const Along<DP>& along, const unsigned char* t0, int b0, const unsigned char* t1,
+                                           int b1, const u32x4 (&f0)[DP / 16], const u32x4 (&f1)[DP / 16], f32x16& s0,
+                                           f32x16& s1, F&& behind) {
+  constexpr int KS = DP / 16;
+  u32x4 x[AHEAD + 1], y[AHEAD + 1];
+#pragma unroll
+  for (int k = 0; k < AHEAD; ++k) {
+    x[k] = along.read(t0, b0, k);
+    y[k] = along.read(t1, b1, k);
+  }
+  s0 = zeros16();
+  s1 = zeros16();
+#pragma unroll
+  for (int k = 0; k < KS; ++k) {
+    if (k + AHEAD < KS) {
+      x[(k + AHEAD) % (AHEAD + 1)] = along.read(t0, b0, k + AHEAD);
+      y[(k + AHEAD) % (AHEAD + 1)] = along.read(t1, b1, k + AHEAD);
+    } else if (k + AHEAD == KS) {
+      behind();
+    }
+    pin();
+    s0 = mfma32x32x16(x[k % (AHEAD + 1)], f0[k], s0);
+    s1 = mfma32x32x16(y[k % (AHEAD + 1)], f1[k], s1);
+    pin();
+  }
+}
+
+// The order of the instructions up to the next pin(): N times a product, READS reads of LDS and OTHER vector
+// instructions, which run while the matrix unit is busy with the product.
+template <int N, int READS, int OTHER>
+__device__ __forceinline__ void interleave() {
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);      // matrix
+    __builtin_amdgcn_sched_group_barrier(0x100, READS, 0);  // LDS reads
+    __builtin_amdgcn_sched_group_barrier(0x002, OTHER, 0);  // vector
+  }
+}
+
+// slice s (16 rows) of a 32 x 32 product's accumulators as an operand
+__device__ __forceinline__ u32x4 operand(const f32x16& x, int s) {
+  return u32x4{pack2(x[8 * s], x[8 * s + 1]), pack2(x[8 * s + 2], x[8 * s + 3]), pack2(x[8 * s + 4], x[8 * s + 5]),
+               pack2(x[8 * s + 6], x[8 * s + 7])};
 }
 
 // a lane's 16 bytes of a row of d features in memory: features 16 k + 8 h .. + 7
@@ -204,15 +248,24 @@ struct Lengths {
 struct AttnGrid {
   int32_t tiles, splits, per_split;  // of columns, or of keys; per_split: rows of a range of the other, a multiple of kTile
   FastDiv div_tiles, div_splits, div_heads;
-  uint32_t blocks;
+  uint32_t units, blocks;  // sequences, heads and ranges; times tiles
 };
 struct AttnPlace {
   int b, h, split, tile;
   __device__ __forceinline__ AttnPlace(const AttnArgs& a, const AttnGrid& g) {
-    // neighbouring blocks read the same k and v (or q and dy): a run of them to each XCD's L2
-    uint32_t t = xcd_remap(blockIdx.x, gridDim.x);
-    const uint32_t u = fdiv(t, g.div_tiles);
-    tile = t - u * g.tiles;
+    // The tiles of one head and range read the same k and v (or q and dy), so they share an XCD's L2.  Heads are
+    // dealt to the XCDs in turn: sequences of different lengths then weigh on all of them alike.  (Those left
+    // over are dealt by tiles.)
+    const uint32_t x = blockIdx.x % kXcds, i = blockIdx.x / kXcds, dealt = g.units / kXcds * kXcds;
+    uint32_t u = fdiv(i, g.div_tiles);
+    tile = i - u * g.tiles;
+    u = u * kXcds + x;
+    if (u >= dealt) {
+      const uint32_t left = blockIdx.x - dealt * g.tiles;
+      u = fdiv(left, g.div_tiles);
+      tile = left - u * g.tiles;
+      u += dealt;
+    }
     const uint32_t w = fdiv(u, g.div_splits);
     split = u - w * g.splits;
     b = fdiv(w, g.div_heads);
@@ -233,6 +286,7 @@ inline AttnGrid make_attn_grid(const AttnArgs& a, int64_t tiles, int64_t rows, i
   g.div_tiles = make_fastdiv((uint32_t)std::max<int64_t>(1, tiles));
   g.div_splits = make_fastdiv((uint32_t)g.splits);
   g.div_heads = make_fastdiv((uint32_t)a.kv_heads);
+  g.units = (uint32_t)std::min<int64_t>((int64_t)a.batch * a.kv_heads * g.splits, 0xffffffffll);
   g.blocks = (uint32_t)std::min<int64_t>((int64_t)a.batch * a.kv_heads * tiles * g.splits, 0xffffffffll);
   return g;
 }

@@ -667,7 +667,7 @@ __device__ __forceinline__ void block_join(const GnArgs& a, const GnGrid& src, c
 }
 
 template <typename TX, typename TY, bool ALIGNED>
-__global__ __launch_bounds__(kThreads, 4) void gn_fwd_kernel(GnArgs a, GnGrid g, GnGrid src, const TX* x, const float* gamma,
+__global__ __launch_bounds__(kThreads, sizeof(TX) == 4 ? 3 : 4) void gn_fwd_kernel(GnArgs a, GnGrid g, GnGrid src, const TX* x, const float* gamma,
                                                           const float* beta, const float2* part, const float2* joined,
                                                           TY* y, float* mean, float* rstd) {
   __shared__ float2 s_join[kThreads];
@@ -788,7 +788,7 @@ __global__ __launch_bounds__(kThreads) void gn_bwd_sums_kernel(GnArgs a, GnGrid 
 }
 
 template <typename TX, typename TY, bool ALIGNED>
-__global__ __launch_bounds__(kThreads, 3) void gn_bwd_kernel(GnArgs a, GnGrid g, GnGrid src, const TY* dy, const TX* x,
+__global__ __launch_bounds__(kThreads, sizeof(TX) < sizeof(TY) ? 2 : 3) void gn_bwd_kernel(GnArgs a, GnGrid g, GnGrid src, const TY* dy, const TX* x,
                                                           const float* mean, const float* rstd, const float* gamma,
                                                           const float* beta, const TX* res, const float2* part,
                                                           const float2* joined, TX* dx) {
