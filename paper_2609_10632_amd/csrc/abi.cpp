@@ -58,7 +58,7 @@ const char* const kMlpClassNames[KC_MLP_END - KC_MLP_FIRST] = {
     "layer_norm_bwd_finish", "adamw_norm", "adamw"};
 const char* const kAttentionClassNames[KC_ATTENTION_END - KC_ATTENTION_FIRST] = {
     "group_norm_stats", "group_norm_fwd", "group_norm_bwd_sums", "group_norm_bwd", "group_norm_bwd_finish", "rotary",
-    "attention_fwd", "attention_join", "attention_bwd_rows", "attention_bwd"};
+    "attention_fwd", "attention_join", "attention_dq", "attention_dkv"};
 
 const char* class_name(int c) {
   if (c >= 0 && c < KC_COUNT) return kClassNames[c];

@@ -151,22 +151,40 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_fwd_kernel(AttnArgs a, AttnGr
 }
 
 // the ranges' results weighted by their sums: a thread for 4 features of a column
-__global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a, int splits, const float* part, const float* part_lse) {
+__global__ __launch_bounds__(64) void attn_join_kernel(AttnArgs a, int splits, const float* part, const float* part_lse) {
   const int per = a.d / 4, cols = a.q_len * a.group;
   const int64_t total = (int64_t)a.batch * a.kv_heads * cols;
-  for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < total * per; i += gridDim.x * 256ll) {
+  for (int64_t i = blockIdx.x * 64ll + threadIdx.x; i < total * per; i += gridDim.x * 64ll) {
     const int64_t c = i / per;
     const int f = (int)(i - c * per) * 4;
-    float top = -INFINITY;
-    for (int s = 0; s < splits; ++s) top = fmaxf(top, part_lse[s * total + c]);
-    const float unit = top == -INFINITY ? 0.f : top;
-    float sum = 0.f;
+    // (eight ranges' loads in flight)
+    constexpr int N = 8;
+    float top = -INFINITY, sum = 0.f;
     f32x4 y = {0.f, 0.f, 0.f, 0.f};
-    for (int s = 0; s < splits; ++s) {
-      const float w = __builtin_amdgcn_exp2f(part_lse[s * total + c] - unit);
-      const f32x4 v = *reinterpret_cast<const f32x4*>(part + (s * total + c) * a.d + f);
-      sum += w;
-      y += v * w;
+    for (int s = 0; s < splits; s += N) {
+      float lse[N];
+#pragma unroll
+      for (int e = 0; e < N; ++e) lse[e] = part_lse[min(s + e, splits - 1) * total + c];
+#pragma unroll
+      for (int e = 0; e < N; ++e) top = fmaxf(top, lse[e]);
+    }
+    const float unit = top == -INFINITY ? 0.f : top;
+    for (int s = 0; s < splits; s += N) {
+      float lse[N];
+      f32x4 v[N];
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        const int64_t at = min(s + e, splits - 1) * total + c;
+        lse[e] = part_lse[at];
+        v[e] = *reinterpret_cast<const f32x4*>(part + at * a.d + f);
+      }
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        const float w = s + e < splits ? __builtin_amdgcn_exp2f(lse[e] - unit) : 0.f;
+        sum += w;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[i] = __builtin_fmaf(w, v[e][i], y[i]);
+      }
     }
     const float inv = sum == 0.f ? 0.f : 1.0f / sum;
     const int64_t bh = c / cols;
@@ -182,11 +200,26 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a, int splits, 
   }
 }
 
-int fwd_waves(const AttnArgs& a) { return (int64_t)a.q_len * a.group <= 32 ? 1 : 4; }
+// Waves of a block: four share a tile's loads, but a grid of few blocks, or blocks of few columns, leave less of the
+// card idle with two or one.  What counts is the waves' work on the fullest CU.  (16 x 9 heads of 400 columns: 576
+// blocks of four put 12 waves on some CUs, 1008 of two 8.)
+int fwd_waves(const AttnArgs& a) {
+  const int64_t columns = (int64_t)a.q_len * a.group, heads = (int64_t)a.batch * a.kv_heads;
+  int best = 4;
+  int64_t least = INT64_MAX;
+  for (int nw : {4, 2, 1}) {
+    const int64_t blocks = heads * ((columns + nw * 32 - 1) / (nw * 32)), waves = (blocks + kCus - 1) / kCus * nw;
+    if (waves < least) {
+      least = waves;
+      best = nw;
+    }
+  }
+  return best;
+}
 
 AttnGrid fwd_grid(const AttnArgs& a) {
   const int64_t columns = fwd_waves(a) * 32, tiles = ((int64_t)a.q_len * a.group + columns - 1) / columns;
-  return make_attn_grid(a, tiles, a.kv_len, 512, 256);
+  return make_attn_grid(a, tiles, a.kv_len, fwd_waves(a) == 1 ? 1024 : 512, 256);
 }
 
 size_t columns_of(const AttnArgs& a) { return (size_t)a.batch * a.kv_heads * a.q_len * a.group; }
@@ -211,7 +244,9 @@ hipError_t attn_fwd_launch(const AttnArgs& a, void* ws, hipStream_t s) {
   trace_begin(KC_ATTN_FWD);
   with_head(a.d, [&](auto dc) {
     constexpr int DP = decltype(dc)::value;
-    if (fwd_waves(a) == 1) NUMBAT_LAUNCH((attn_fwd_kernel<DP, 1>), dim3(g.blocks), dim3(64), 0, s, a, g, part, part_lse);
+    const int nw = fwd_waves(a);
+    if (nw == 1) NUMBAT_LAUNCH((attn_fwd_kernel<DP, 1>), dim3(g.blocks), dim3(64), 0, s, a, g, part, part_lse);
+    else if (nw == 2) NUMBAT_LAUNCH((attn_fwd_kernel<DP, 2>), dim3(g.blocks), dim3(128), 0, s, a, g, part, part_lse);
     else NUMBAT_LAUNCH((attn_fwd_kernel<DP, 4>), dim3(g.blocks), dim3(256), 0, s, a, g, part, part_lse);
   });
   trace_end(KC_ATTN_FWD);
@@ -219,7 +254,7 @@ hipError_t attn_fwd_launch(const AttnArgs& a, void* ws, hipStream_t s) {
   if (e != hipSuccess || g.splits == 1) return e;
   trace_begin(KC_ATTN_JOIN);
   const int64_t threads = (int64_t)columns_of(a) * (a.d / 4);
-  NUMBAT_LAUNCH(attn_join_kernel, dim3((unsigned)std::min<int64_t>((threads + 255) / 256, 1 << 16)), dim3(256), 0, s, a,
+  NUMBAT_LAUNCH(attn_join_kernel, dim3((unsigned)std::min<int64_t>((threads + 63) / 64, 1 << 18)), dim3(64), 0, s, a,
                 g.splits, part, part_lse);
   trace_end(KC_ATTN_JOIN);
   return hipGetLastError();

@@ -3,9 +3,7 @@
 // as two kernels that each form P and ds anew, since a single one would have to add dq over blocks of
 // keys in an order that changes from run to run (or keep a copy of dq for each): seven products
 // where five would do.
-//   rows  delta = sum dy y of each column, beside lse in base 2; a column that counts for nothing gets an
-//         lse of plus infinity, hence weights of zero
-//   dq    a wave owns 32 columns and walks the keys, as in the forward: s^T = k q^T, dp^T = v dy^T,
+//   dq    first delta = sum dy y of each column, which it leaves for the other; a wave owns 32 columns and walks the keys, as in the forward: s^T = k q^T, dp^T = v dy^T,
 //         dq^T += k^T ds^T; k and v in LDS, q and dy in registers
 //   dkv   a wave owns 32 keys and walks the columns: s = q k^T, dp = dy v^T, dv^T += dy^T P, dk^T += q^T ds;
 //         q and dy in LDS, k and v in registers.  The heads that share a head of k and v are columns of one
@@ -20,37 +18,8 @@ namespace numbat {
 
 namespace {
 
-// a group of G lanes for each row's head: G = d / 8 rounded up to a power of two
-__global__ __launch_bounds__(256) void attn_rows_kernel(AttnArgs a, int lanes, float2* rows) {
-  const int heads = a.kv_heads * a.group, cols = a.q_len * a.group;
-  const int64_t total = (int64_t)a.batch * a.q_len * heads;
-  const int f = threadIdx.x % lanes * 8;
-  // (whole waves stay in the loop together for the exchange)
-  for (int64_t first = blockIdx.x * (256ll / lanes); first < total; first += gridDim.x * (256ll / lanes)) {
-    const int64_t i = first + threadIdx.x / lanes;
-    const int64_t br = i / heads;
-    const int head = (int)(i - br * heads), b = (int)(br / a.q_len), r = (int)(br - (int64_t)b * a.q_len);
-    const bool counts = i < total && r < (a.q_lengths != nullptr ? a.q_lengths[b] : a.q_len);
-    float t = 0.f;
-    if (counts && f < a.d) {
-      const int64_t at = br * a.ldy + head * a.d + f;
-      float y[8], g[8];
-      unpack8(*reinterpret_cast<const uint4*>(a.y + at), y);
-      unpack8(*reinterpret_cast<const uint4*>(a.dy + at), g);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) t = __builtin_fmaf(y[e], g[e], t);
-    }
-    for (int o = lanes / 2; o > 0; o /= 2) t += __shfl_xor(t, o);
-    if (i < total && f == 0) {
-      const float lse = counts ? a.lse[((int64_t)b * heads + head) * a.q_len + r] : -INFINITY;
-      const int kv = head / a.group, c = r * a.group + head - kv * a.group;
-      rows[((int64_t)b * a.kv_heads + kv) * cols + c] = make_float2(lse == -INFINITY ? INFINITY : lse * kLog2e, t);
-    }
-  }
-}
-
 template <int DP, int NW>
-__global__ __launch_bounds__(NW * 64, 2) void attn_dq_kernel(AttnArgs a, AttnGrid g, const float2* rows, float* part) {
+__global__ __launch_bounds__(NW * 64, 2) void attn_dq_kernel(AttnArgs a, AttnGrid g, float2* rows, float* part) {
   using H = Head<DP>;
   constexpr int KS = H::KS, FB = H::FB;
   __shared__ __attribute__((aligned(1024))) unsigned char st0[2 * H::TILE];
@@ -84,7 +53,28 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_dq_kernel(AttnArgs a, AttnGri
     qf[k] = row_chunk(qrow, valid, a.d, k, half);
     df[k] = row_chunk(drow, valid, a.d, k, half);
   }
-  const float2 stat = inside ? rows[((int64_t)p.b * a.kv_heads + p.h) * cols + col] : make_float2(INFINITY, 0.f);
+  // lse in base 2 and delta of the lane's column, which the other kernel reads too; a column that counts for
+  // nothing gets an lse of plus infinity, hence weights of zero
+  float2 stat = make_float2(INFINITY, 0.f);
+  {
+    const bf16_t* yrow = a.y + ((int64_t)p.b * a.q_len + row) * a.ldy + head * a.d;
+    float t = 0.f;
+#pragma unroll
+    for (int k = 0; k < KS; ++k) {
+      const u32x4 yf = row_chunk(yrow, valid, a.d, k, half);
+      float y[8], g8[8];
+      unpack8(make_uint4(yf.x, yf.y, yf.z, yf.w), y);
+      unpack8(make_uint4(df[k].x, df[k].y, df[k].z, df[k].w), g8);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) t = __builtin_fmaf(y[e], g8[e], t);
+    }
+    stat.y = half_sum(t);
+    if (valid) {
+      const float lse = a.lse[((int64_t)p.b * a.kv_heads * a.group + head) * a.q_len + row];
+      if (lse != -INFINITY) stat.x = lse * kLog2e;
+    }
+    if (inside && half == 0 && p.split == 0) rows[((int64_t)p.b * a.kv_heads + p.h) * cols + col] = stat;
+  }
 
   const bf16_t* kbase = a.k + (int64_t)p.b * a.kv_len * a.ldk + p.h * a.d;
   const bf16_t* vbase = a.v + (int64_t)p.b * a.kv_len * a.ldv + p.h * a.d;
@@ -369,14 +359,6 @@ hipError_t attn_bwd_launch(const AttnArgs& a, void* ws, hipStream_t s) {
   float2* rows = static_cast<float2*>(ws);
   float* part = reinterpret_cast<float*>(static_cast<char*>(ws) + rows_bytes(a));
   const AttnGrid gq = dq_grid(a), gk = dkv_grid(a);
-  if (a.q_len > 0) {
-    int lanes = 1;
-    while (lanes * 8 < a.d) lanes *= 2;
-    const int64_t blocks = ((int64_t)columns_of(a) * lanes + 255) / 256;
-    trace_begin(KC_ATTN_BWD_ROWS);
-    NUMBAT_LAUNCH(attn_rows_kernel, dim3((unsigned)std::min<int64_t>(blocks, 1 << 16)), dim3(256), 0, s, a, lanes, rows);
-    trace_end(KC_ATTN_BWD_ROWS);
-  }
   auto join = [&](auto kc, const AttnGrid& g, size_t vectors) {
     trace_begin(KC_ATTN_JOIN);
     const int64_t threads = (int64_t)vectors * (a.d / 4);
@@ -388,16 +370,16 @@ hipError_t attn_bwd_launch(const AttnArgs& a, void* ws, hipStream_t s) {
   with_head(a.d, [&](auto dc) {
     constexpr int DP = decltype(dc)::value;
     if (e == hipSuccess && a.q_len > 0) {
-      trace_begin(KC_ATTN_BWD);
+      trace_begin(KC_ATTN_DQ);
       NUMBAT_LAUNCH((attn_dq_kernel<DP, 4>), dim3(gq.blocks), dim3(256), 0, s, a, gq, rows, part);
-      trace_end(KC_ATTN_BWD);
+      trace_end(KC_ATTN_DQ);
       if (gq.splits > 1) join(std::false_type{}, gq, columns_of(a));
       e = hipGetLastError();
     }
     if (e == hipSuccess && a.kv_len > 0) {
-      trace_begin(KC_ATTN_BWD);
+      trace_begin(KC_ATTN_DKV);
       NUMBAT_LAUNCH((attn_dkv_kernel<DP, 4>), dim3(gk.blocks), dim3(256), 0, s, a, gk, rows, part);
-      trace_end(KC_ATTN_BWD);
+      trace_end(KC_ATTN_DKV);
       if (gk.splits > 1) join(std::true_type{}, gk, 2 * keys_of(a));
       e = hipGetLastError();
     }

@@ -17,8 +17,8 @@ enum AttentionKernelClass {
   KC_ROTARY,
   KC_ATTN_FWD,                       // attention forward
   KC_ATTN_JOIN,                      // results of ranges of keys or queries, joined
-  KC_ATTN_BWD_ROWS,                  // attention backward: each query's statistics
-  KC_ATTN_BWD,                       // attention backward: the products
+  KC_ATTN_DQ,                        // attention backward: gradient of q
+  KC_ATTN_DKV,                       // attention backward: gradients of k and v
   KC_ATTENTION_END
 };
 

@@ -300,6 +300,7 @@ void with_head(int d, F&& f) {
   else f(std::integral_constant<int, 128>{});
 }
 
+constexpr int kCus = 256;
 constexpr int64_t kMaxBlocks = (1ll << 32) / 256 - 1;  // of 256 threads in a launch
 
 }  // namespace
