@@ -20,7 +20,7 @@ namespace {
 constexpr float kRaise = 8.f;  // (log2)
 
 template <int DP, int NW>
-__global__ __launch_bounds__(NW * 64, 2) void attn_fwd_kernel(AttnArgs a, AttnGrid g, float* part, float* part_lse) {
+__global__ __launch_bounds__(NW * 64, DP <= 64 || NW == 4 ? 2 : 1) void attn_fwd_kernel(AttnArgs a, AttnGrid g, float* part, float* part_lse) {
   using H = Head<DP>;
   constexpr int KS = H::KS, FB = H::FB;
   // one object per stage: the compiler then knows that a stage's reads do not wait for the loads in
@@ -80,7 +80,9 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_fwd_kernel(AttnArgs a, AttnGr
 #pragma unroll
       for (int f = 0; f < FB; ++f) vf[u & 1][f] = across.read(st + H::TILE, f, u);
     };
+    __builtin_amdgcn_s_setprio(1);
     along_pair<DP>(along, st, 0, st, 1, qf, qf, s[0], s[1], [&] { read_v(0); });
+    __builtin_amdgcn_s_setprio(0);
     if (key + kTile > wave_all) {
 #pragma unroll
       for (int i = 0; i < 2; ++i)
@@ -111,6 +113,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_fwd_kernel(AttnArgs a, AttnGr
         s[i][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i][r], a.scale_log2, -unit));
         sum += s[i][r];
       }
+    __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
       if (u < 3) read_v(u + 1);
@@ -120,6 +123,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_fwd_kernel(AttnArgs a, AttnGr
       for (int f = 0; f < FB; ++f) o[f] = mfma32x32x16(vf[u & 1][f], w, o[f]);
       pin();
     }
+    __builtin_amdgcn_s_setprio(0);
   };
   auto step = [&](unsigned char* st, unsigned char* next, int key) __attribute__((always_inline)) {
     stage_ready();  // this stage has landed, and every wave is done with the other
@@ -200,22 +204,7 @@ __global__ __launch_bounds__(64) void attn_join_kernel(AttnArgs a, int splits, c
   }
 }
 
-// Waves of a block: four share a tile's loads, but a grid of few blocks, or blocks of few columns, leave less of the
-// card idle with two or one.  What counts is the waves' work on the fullest CU.  (16 x 9 heads of 400 columns: 576
-// blocks of four put 12 waves on some CUs, 1008 of two 8.)
-int fwd_waves(const AttnArgs& a) {
-  const int64_t columns = (int64_t)a.q_len * a.group, heads = (int64_t)a.batch * a.kv_heads;
-  int best = 4;
-  int64_t least = INT64_MAX;
-  for (int nw : {4, 2, 1}) {
-    const int64_t blocks = heads * ((columns + nw * 32 - 1) / (nw * 32)), waves = (blocks + kCus - 1) / kCus * nw;
-    if (waves < least) {
-      least = waves;
-      best = nw;
-    }
-  }
-  return best;
-}
+int fwd_waves(const AttnArgs& a) { return attn_waves(a, (int64_t)a.q_len * a.group, true); }
 
 AttnGrid fwd_grid(const AttnArgs& a) {
   const int64_t columns = fwd_waves(a) * 32, tiles = ((int64_t)a.q_len * a.group + columns - 1) / columns;

@@ -19,7 +19,7 @@ namespace numbat {
 namespace {
 
 template <int DP, int NW>
-__global__ __launch_bounds__(NW * 64, 2) void attn_dq_kernel(AttnArgs a, AttnGrid g, float2* rows, float* part) {
+__global__ __launch_bounds__(NW * 64, DP <= 64 || NW == 4 ? 2 : 1) void attn_dq_kernel(AttnArgs a, AttnGrid g, float2* rows, float* part) {
   using H = Head<DP>;
   constexpr int KS = H::KS, FB = H::FB;
   __shared__ __attribute__((aligned(1024))) unsigned char st0[2 * H::TILE];
@@ -144,7 +144,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_dq_kernel(AttnArgs a, AttnGri
 }
 
 template <int DP, int NW>
-__global__ __launch_bounds__(NW * 64, DP <= 64 ? 2 : 1) void attn_dkv_kernel(AttnArgs a, AttnGrid g, const float2* rows,
+__global__ __launch_bounds__(NW * 64, DP <= 64 || (NW == 4 && DP <= 96) ? 2 : 1) void attn_dkv_kernel(AttnArgs a, AttnGrid g, const float2* rows,
                                                                              float* part) {
   using H = Head<DP>;
   constexpr int KS = H::KS, FB = H::FB;
@@ -304,14 +304,22 @@ __global__ __launch_bounds__(NW * 64, DP <= 64 ? 2 : 1) void attn_dkv_kernel(Att
 
 // the ranges' sums added in order, a thread for 4 features: of columns (dq), or of keys (dk and dv beside it)
 template <bool KEYS>
-__global__ __launch_bounds__(256) void attn_bwd_join_kernel(AttnArgs a, int splits, const float* part) {
+__global__ __launch_bounds__(64) void attn_bwd_join_kernel(AttnArgs a, int splits, const float* part) {
   const int per = a.d / 4, len = KEYS ? 2 * a.kv_len : a.q_len * a.group;
   const int64_t total = (int64_t)a.batch * a.kv_heads * len;
-  for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < total * per; i += gridDim.x * 256ll) {
+  for (int64_t i = blockIdx.x * 64ll + threadIdx.x; i < total * per; i += gridDim.x * 64ll) {
     const int64_t c = i / per;
     const int f = (int)(i - c * per) * 4;
+    constexpr int N = 8;  // ranges' loads in flight
     f32x4 y = {0.f, 0.f, 0.f, 0.f};
-    for (int s = 0; s < splits; ++s) y += *reinterpret_cast<const f32x4*>(part + (s * total + c) * a.d + f);
+    for (int s = 0; s < splits; s += N) {
+      f32x4 v[N];
+#pragma unroll
+      for (int e = 0; e < N; ++e) v[e] = *reinterpret_cast<const f32x4*>(part + (min(s + e, splits - 1) * total + c) * a.d + f);
+#pragma unroll
+      for (int e = 0; e < N; ++e)
+        if (s + e < splits) y += v[e];
+    }
     const int64_t bh = c / len;
     const int at = (int)(c - bh * len), b = (int)(bh / a.kv_heads), h = (int)(bh - (int64_t)b * a.kv_heads);
     bf16_t* to;
@@ -330,16 +338,19 @@ __global__ __launch_bounds__(256) void attn_bwd_join_kernel(AttnArgs a, int spli
   }
 }
 
-constexpr int kColumnsOfBlock = 128, kKeysOfBlock = 128;
+int dq_waves(const AttnArgs& a) { return attn_waves(a, (int64_t)a.q_len * a.group, false); }
+int dkv_waves(const AttnArgs& a) { return attn_waves(a, a.kv_len, false); }
 
 size_t columns_of(const AttnArgs& a) { return (size_t)a.batch * a.kv_heads * a.q_len * a.group; }
 size_t keys_of(const AttnArgs& a) { return (size_t)a.batch * a.kv_heads * a.kv_len; }
 
 AttnGrid dq_grid(const AttnArgs& a) {
-  return make_attn_grid(a, ((int64_t)a.q_len * a.group + kColumnsOfBlock - 1) / kColumnsOfBlock, a.kv_len, 512, 256);
+  const int64_t side = dq_waves(a) * 32;
+  return make_attn_grid(a, ((int64_t)a.q_len * a.group + side - 1) / side, a.kv_len, 512, 256);
 }
 AttnGrid dkv_grid(const AttnArgs& a) {
-  return make_attn_grid(a, ((int64_t)a.kv_len + kKeysOfBlock - 1) / kKeysOfBlock, (int64_t)a.q_len * a.group, 512, 256);
+  const int64_t side = dkv_waves(a) * 32;
+  return make_attn_grid(a, ((int64_t)a.kv_len + side - 1) / side, (int64_t)a.q_len * a.group, 512, 256);
 }
 // dq and dkv run one after the other: their partials share their space
 size_t part_floats(const AttnArgs& a) {
@@ -362,8 +373,8 @@ hipError_t attn_bwd_launch(const AttnArgs& a, void* ws, hipStream_t s) {
   auto join = [&](auto kc, const AttnGrid& g, size_t vectors) {
     trace_begin(KC_ATTN_JOIN);
     const int64_t threads = (int64_t)vectors * (a.d / 4);
-    NUMBAT_LAUNCH((attn_bwd_join_kernel<decltype(kc)::value>), dim3((unsigned)std::min<int64_t>((threads + 255) / 256, 1 << 16)),
-                  dim3(256), 0, s, a, g.splits, part);
+    NUMBAT_LAUNCH((attn_bwd_join_kernel<decltype(kc)::value>), dim3((unsigned)std::min<int64_t>((threads + 63) / 64, 1 << 18)),
+                  dim3(64), 0, s, a, g.splits, part);
     trace_end(KC_ATTN_JOIN);
   };
   hipError_t e = hipGetLastError();
@@ -371,14 +382,16 @@ hipError_t attn_bwd_launch(const AttnArgs& a, void* ws, hipStream_t s) {
     constexpr int DP = decltype(dc)::value;
     if (e == hipSuccess && a.q_len > 0) {
       trace_begin(KC_ATTN_DQ);
-      NUMBAT_LAUNCH((attn_dq_kernel<DP, 4>), dim3(gq.blocks), dim3(256), 0, s, a, gq, rows, part);
+      if (dq_waves(a) == 4) NUMBAT_LAUNCH((attn_dq_kernel<DP, 4>), dim3(gq.blocks), dim3(256), 0, s, a, gq, rows, part);
+      else NUMBAT_LAUNCH((attn_dq_kernel<DP, 2>), dim3(gq.blocks), dim3(128), 0, s, a, gq, rows, part);
       trace_end(KC_ATTN_DQ);
       if (gq.splits > 1) join(std::false_type{}, gq, columns_of(a));
       e = hipGetLastError();
     }
     if (e == hipSuccess && a.kv_len > 0) {
       trace_begin(KC_ATTN_DKV);
-      NUMBAT_LAUNCH((attn_dkv_kernel<DP, 4>), dim3(gk.blocks), dim3(256), 0, s, a, gk, rows, part);
+      if (dkv_waves(a) == 4) NUMBAT_LAUNCH((attn_dkv_kernel<DP, 4>), dim3(gk.blocks), dim3(256), 0, s, a, gk, rows, part);
+      else NUMBAT_LAUNCH((attn_dkv_kernel<DP, 2>), dim3(gk.blocks), dim3(128), 0, s, a, gk, rows, part);
       trace_end(KC_ATTN_DKV);
       if (gk.splits > 1) join(std::true_type{}, gk, 2 * keys_of(a));
       e = hipGetLastError();

@@ -231,6 +231,9 @@ __device__ __forceinline__ void store_part(float* row, bool valid, int d, const 
     }
 }
 
+constexpr int kCus = 256;
+constexpr int64_t kMaxBlocks = (1ll << 32) / 256 - 1;  // of 256 threads in a launch
+
 // A sequence's numbers of queries and keys that count
 struct Lengths {
   int q, kv;
@@ -291,6 +294,25 @@ inline AttnGrid make_attn_grid(const AttnArgs& a, int64_t tiles, int64_t rows, i
   return g;
 }
 
+// Waves of a block: four share a tile's loads, but a grid of few blocks, or blocks of few columns, leave less of the
+// card idle with two or one.  What counts is the waves' work on the fullest CU, times what a wave's work costs
+// with fewer to share the loads (4 x 8 heads, 4096 x 4096, d = 64, dq: 1.2 to 1.4 times in twos; forward of 16 x 6
+// heads of 1600 columns: 149 us in ones, 80 in fours; of 16 x 9 heads of 400: 19 us in fours, 16 in twos).
+inline int attn_waves(const AttnArgs& a, int64_t columns, bool one) {
+  const int64_t heads = (int64_t)a.batch * a.kv_heads;
+  int best = 4;
+  double least = 1e300;
+  for (int nw = 4; nw >= (one ? 1 : 2); nw /= 2) {
+    const int64_t blocks = heads * ((columns + nw * 32 - 1) / (nw * 32));
+    const double work = (double)((blocks + kCus - 1) / kCus * nw) * (nw == 4 ? 1.0 : nw == 2 ? 1.3 : 1.9);
+    if (work < least) {
+      least = work;
+      best = nw;
+    }
+  }
+  return best;
+}
+
 // f(DP) for the narrowest head that holds d features
 template <typename F>
 void with_head(int d, F&& f) {
@@ -300,8 +322,6 @@ void with_head(int d, F&& f) {
   else f(std::integral_constant<int, 128>{});
 }
 
-constexpr int kCus = 256;
-constexpr int64_t kMaxBlocks = (1ll << 32) / 256 - 1;  // of 256 threads in a launch
 
 }  // namespace
 

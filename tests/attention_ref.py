@@ -3,7 +3,7 @@ import math
 
 import torch
 
-from mlp_ref import D
+from mlp_ref import B, D, U
 
 
 def group_norm(x, n, groups, gamma, beta, eps):
@@ -90,3 +90,31 @@ def fold(t, kv_heads):
     """The sums over the heads that share a head of k and v."""
     b, h, n, d = t.shape
     return t.reshape(b, kv_heads, h // kv_heads, n, d).sum(2)
+
+
+def weight_error(q, k, see, scale, lse):
+    """Of exp(s - lse), relative, before it is rounded to bf16: a score is off by (d + 8) 2^-24 of the sum of its
+    products' sizes, the exponential by 2^-20, its argument's two roundings by 2^-23 of their size."""
+    s_off = (q.shape[-1] + 8) * U * scale * (q.abs() @ k.abs().transpose(2, 3))
+    s = scale * q @ k.transpose(2, 3)
+    arg = 2 * U * (s.abs() + lse[..., None].abs().clamp(max=1e30)) + 2 * U * (s - lse[..., None].clamp(min=-1e30)).abs()
+    return torch.where(see, s_off + arg + 2 ** -20, torch.zeros((), dtype=D))
+
+
+def forward_bounds(q, k, v, p, lse, y, see, scale):
+    """How far y and lse may be off."""
+    n, off = k.shape[2], weight_error(q, k, see, scale, lse)
+    lse_off = (p * off).sum(-1) + (n + 8) * U + 4 * U * lse.abs()
+    off = off + (p * off).sum(-1, keepdim=True)  # (of the sum that divides it too)
+    return (p * (B + off + (n + 8) * 2 * U)) @ v.abs() + B * y.abs(), lse_off
+
+
+def grad_bounds(dy, q, k, v, y, p, ds, dq, dk, dv, lse, see, scale, kv_heads):
+    """How far dq, dk and dv may be off; dk and dv are the folded ones."""
+    d, n, cols = q.shape[-1], k.shape[2], q.shape[2] * (q.shape[1] // kv_heads)
+    off = weight_error(q, k, see, scale, lse)
+    dp_size = dy.abs() @ v.abs().transpose(2, 3) + (dy.abs() * y.abs()).sum(-1, keepdim=True)
+    ds_off = ds.abs() * (off + B + 4 * U) + p * (d + 16) * U * dp_size
+    return (scale * (ds_off + (n + 8) * 2 * U * ds.abs()) @ k.abs() + B * dq.abs(),
+            fold(scale * (ds_off + (cols + 8) * 2 * U * ds.abs()).transpose(2, 3) @ q.abs(), kv_heads) + B * dk.abs(),
+            fold((p * (B + off + (cols + 8) * 2 * U)).transpose(2, 3) @ dy.abs(), kv_heads) + B * dv.abs())

@@ -2,16 +2,15 @@
 lengths, features that are no power of two, shared heads, padded batches, causal sequences of unequal lengths,
 sequences without keys, q, k and v beside each other in one matrix, ranges of keys and queries.
 
-Bounds.  A score is a sum of d products: off by (d + 8) 2^-24 of the sum of their sizes, a weight
-relatively by that, 2^-20 for the exponential and its argument's rounding (|s - lse| 2^-23 each of them),
-and 2^-8 where it is rounded to bf16 for a product.  Sums of n products are off by (n + 8) 2^-24 of
-the sum of their sizes."""
+Bounds (attention_ref.py): of a score, (d + 8) 2^-24 of the sum of its products' sizes, of a weight, relatively,
+that and 2^-20 for the exponential with its argument's rounding, and 2^-8 where it is rounded to bf16 for a
+product; of a sum of n products, (n + 8) 2^-24 of the sum of their sizes."""
 import math
 
 import pytest
 
-from attention_ref import attention, attention_grads, fold, join, split, visible
-from mlp_ref import B, D, U, close
+from attention_ref import attention, attention_grads, fold, forward_bounds, grad_bounds, join, split, visible
+from mlp_ref import D, close
 
 pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
@@ -77,24 +76,12 @@ class Case:
         self.ry, self.rlse, self.rp = attention(self.rq, self.rk, self.rv, self.see, self.scale)
         self.empty = ~self.see.any(-1)[:, 0]  # [batch][q_len] or of one row for all sequences
 
-    def weight_error(self, lse):
-        """Of exp(s - lse), relative, before it is rounded."""
-        feat = self.size[5]
-        s_off = (feat + 8) * U * self.scale * (self.rq.abs() @ self.rk.abs().transpose(2, 3))
-        s = self.scale * self.rq @ self.rk.transpose(2, 3)
-        arg = 2 * U * (s.abs() + lse[..., None].abs().clamp(max=1e30)) + 2 * U * (s - lse[..., None].clamp(min=-1e30)).abs()
-        return torch.where(self.see, s_off + arg + 2 ** -20, torch.zeros((), dtype=D))
-
     def check_forward(self):
-        batch, q_len, kv_len, heads, kv_heads, feat = self.size
-        off = self.weight_error(self.rlse)
-        off = off + (self.rp * off).sum(-1, keepdim=True)  # (of the sum that divides it too)
-        bound = (self.rp * (B + off + (kv_len + 8) * 2 * U)) @ self.rv.abs()
-        close(self.y, join(self.ry), join(bound + B * self.ry.abs()), "y")
+        bound, lse_off = forward_bounds(self.rq, self.rk, self.rv, self.rp, self.rlse, self.ry, self.see, self.scale)
+        close(self.y, join(self.ry), join(bound), "y")
         lse = d(self.lse)
         empty = self.empty[:, None].expand(lse.shape)
         assert bool((lse[empty] == -math.inf).all()) and bool((lse[~empty] > -math.inf).all())
-        lse_off = (self.rp * self.weight_error(self.rlse)).sum(-1) + (kv_len + 8) * U + 4 * U * self.rlse.abs()
         close(lse[~empty], self.rlse[~empty], lse_off[~empty], "lse")
         again = torch.full_like(self.y, 7.0)
         nb.numbat_attention_fwd(self.p, self.q, self.k, self.v, self.ql, self.kl, again, None, self.ws)
@@ -118,14 +105,10 @@ class Case:
         lse = d(self.lse).masked_fill(self.empty[:, None].expand(self.lse.shape), 0.0)
         p = torch.exp(self.scale * self.rq @ self.rk.transpose(2, 3) - lse[..., None]).masked_fill(~self.see, 0.0)
         dq, dk, dv, ds = attention_grads(self.rdy, self.rq, self.rk, self.rv, y, p, self.scale)
-        off = self.weight_error(lse)
-        dp_size = self.rdy.abs() @ self.rv.abs().transpose(2, 3) + (self.rdy.abs() * y.abs()).sum(-1, keepdim=True)
-        ds_off = ds.abs() * (off + B + 4 * U) + p * (feat + 16) * U * dp_size
-        cols = q_len * (heads // kv_heads)
-        f = lambda t: join(fold(t, kv_heads))  # noqa: E731
-        close(self.dv, f(dv), f((p * (B + off + (cols + 8) * 2 * U)).transpose(2, 3) @ self.rdy.abs()) + B * f(dv).abs(), "dv")
-        close(self.dq, join(dq), join(self.scale * (ds_off + (kv_len + 8) * 2 * U * ds.abs()) @ self.rk.abs() + B * dq.abs()), "dq")
-        close(self.dk, f(dk), f(self.scale * (ds_off + (cols + 8) * 2 * U * ds.abs()).transpose(2, 3) @ self.rq.abs()) + B * f(dk).abs(), "dk")
+        dk, dv = fold(dk, kv_heads), fold(dv, kv_heads)
+        off = grad_bounds(self.rdy, self.rq, self.rk, self.rv, y, p, ds, dq, dk, dv, lse, self.see, self.scale, kv_heads)
+        for name, got, ref, bound in zip(("dq", "dk", "dv"), (self.dq, self.dk, self.dv), (dq, dk, dv), off):
+            close(got, join(ref), join(bound), name)
         once = [t.clone() for t in (self.dq, self.dk, self.dv)]
         call()
         assert all(torch.equal(a, b) for a, b in zip(once, (self.dq, self.dk, self.dv)))
