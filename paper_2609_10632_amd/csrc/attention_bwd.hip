@@ -102,7 +102,7 @@ __global__ __launch_bounds__(NW * 64, DP <= 64 || NW == 4 ? 2 : 1) void attn_dq_
 #pragma unroll
         for (int f = 0; f < FB; ++f) kf[u][f] = across.read(st, f, 2 * i + u);
       };
-      along_pair<DP>(along, st, i, st + H::TILE, i, qf, df, s, dp, [&] { read_k(0); });
+      along_pair<DP, 2>(along, st, i, st + H::TILE, i, qf, df, s, dp, [&] { read_k(0); });
 #pragma unroll
       for (int r = 0; r < 16; ++r)
         s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], a.scale_log2, -stat.x)) * (dp[r] - stat.y);

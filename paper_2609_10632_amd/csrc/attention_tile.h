@@ -132,45 +132,42 @@ __device__ __forceinline__ f32x16 zeros16() {
 // use, where a wave waits out the LDS's latency.
 __device__ __forceinline__ void pin() { __builtin_amdgcn_sched_barrier(0); }
 
-// s[j] = sum over features of rows `block[j]` of tile[j] and the columns in f[j]: two products side by side, their
-// operands read two slices ahead.  behind(): reads for what follows, issued with the last slices.
-template <int DP, int AHEAD = 2, typename F>
+// s[j] = sum over features of rows `block[j]` of tile[j] and the columns in f[j]: two products side by side.  AHEAD: their
+// operands are read that many slices ahead; 0 leaves the order to the compiler.  behind(): reads for what follows,
+// issued with the last slices.
+template <int DP, int AHEAD, typename F>
 __device__ __forceinline__ void along_pair(const Along<DP>& along, const unsigned char* t0, int b0, const unsigned char* t1,
                                            int b1, const u32x4 (&f0)[DP / 16], const u32x4 (&f1)[DP / 16], f32x16& s0,
                                            f32x16& s1, F&& behind) {
   constexpr int KS = DP / 16;
-  u32x4 x[AHEAD + 1], y[AHEAD + 1];
-#pragma unroll
-  for (int k = 0; k < AHEAD; ++k) {
-    x[k] = along.read(t0, b0, k);
-    y[k] = along.read(t1, b1, k);
-  }
   s0 = zeros16();
   s1 = zeros16();
+  if constexpr (AHEAD == 0) {
 #pragma unroll
-  for (int k = 0; k < KS; ++k) {
-    if (k + AHEAD < KS) {
-      x[(k + AHEAD) % (AHEAD + 1)] = along.read(t0, b0, k + AHEAD);
-      y[(k + AHEAD) % (AHEAD + 1)] = along.read(t1, b1, k + AHEAD);
-    } else if (k + AHEAD == KS) {
-      behind();
+    for (int k = 0; k < KS; ++k) {
+      s0 = mfma32x32x16(along.read(t0, b0, k), f0[k], s0);
+      s1 = mfma32x32x16(along.read(t1, b1, k), f1[k], s1);
     }
-    pin();
-    s0 = mfma32x32x16(x[k % (AHEAD + 1)], f0[k], s0);
-    s1 = mfma32x32x16(y[k % (AHEAD + 1)], f1[k], s1);
-    pin();
-  }
-}
-
-// The order of the instructions up to the next pin(): N times a product, READS reads of LDS and OTHER vector
-// instructions, which run while the matrix unit is busy with the product.
-template <int N, int READS, int OTHER>
-__device__ __forceinline__ void interleave() {
+  } else {
+    u32x4 x[AHEAD + 1], y[AHEAD + 1];
 #pragma unroll
-  for (int i = 0; i < N; ++i) {
-    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);      // matrix
-    __builtin_amdgcn_sched_group_barrier(0x100, READS, 0);  // LDS reads
-    __builtin_amdgcn_sched_group_barrier(0x002, OTHER, 0);  // vector
+    for (int k = 0; k < AHEAD; ++k) {
+      x[k] = along.read(t0, b0, k);
+      y[k] = along.read(t1, b1, k);
+    }
+#pragma unroll
+    for (int k = 0; k < KS; ++k) {
+      if (k + AHEAD < KS) {
+        x[(k + AHEAD) % (AHEAD + 1)] = along.read(t0, b0, k + AHEAD);
+        y[(k + AHEAD) % (AHEAD + 1)] = along.read(t1, b1, k + AHEAD);
+      } else if (k + AHEAD == KS) {
+        behind();
+      }
+      pin();
+      s0 = mfma32x32x16(x[k % (AHEAD + 1)], f0[k], s0);
+      s1 = mfma32x32x16(y[k % (AHEAD + 1)], f1[k], s1);
+      pin();
+    }
   }
 }
 
