@@ -62,6 +62,62 @@ __device__ __forceinline__ void slope8(const float (&t)[V], float (&d)[V], int a
 // The work on one row ends: left to itself the compiler unpacks every row that a thread holds at once
 __device__ __forceinline__ void row_done() { __builtin_amdgcn_sched_barrier(0); }
 
+// How vectors are loaded.  Whole ones stand in no branch: one that some lanes leave out makes the next wait for it.
+// (Moving vectors that a row ends in down from the row's last V channels, to load those without a branch too, costs
+// odd rows of fp32 more than the branch: 5 x 5141 x 327 with GELU 58 us against 32.)
+enum {
+  kWhole,    // whole vectors at 16-byte aligned addresses
+  kAnywhere  // at any address; a vector that the row ends in by elements
+};
+// A vector as it was loaded: bf16 stays packed until it is worked on.  Values behind `count` are not the thread's.
+template <typename T>
+struct Raw;
+template <>
+struct Raw<bf16_t> {
+  u32x4 u;
+  template <int HOW>
+  __device__ __forceinline__ void get(const bf16_t* p, int count) {
+    if constexpr (HOW == kWhole) {
+      u = *reinterpret_cast<const u32x4*>(p);
+    } else if (count >= V) {
+      const uint4 v = get16<false>(p);
+      u = u32x4{v.x, v.y, v.z, v.w};
+    } else {
+      float f[V];
+      get_some<false>(p, count, f);
+      const uint4 v = pack8(f);
+      u = u32x4{v.x, v.y, v.z, v.w};
+    }
+  }
+  __device__ __forceinline__ void values(float (&f)[V]) const { unpack8(make_uint4(u.x, u.y, u.z, u.w), f); }
+  __device__ __forceinline__ void zero() { u = u32x4{0, 0, 0, 0}; }
+  // (the compiler would otherwise keep what it has unpacked, twice the registers)
+  __device__ __forceinline__ void keep() { asm volatile("" : "+v"(u)); }
+};
+template <>
+struct Raw<float> {
+  float v[V];
+  template <int HOW>
+  __device__ __forceinline__ void get(const float* p, int count) {
+    if constexpr (HOW == kWhole) get_vec<true>(p, v);
+    else get_some<false>(p, count, v);
+  }
+  __device__ __forceinline__ void values(float (&f)[V]) const {
+#pragma unroll
+    for (int e = 0; e < V; ++e) f[e] = v[e];
+  }
+  __device__ __forceinline__ void zero() {
+#pragma unroll
+    for (int e = 0; e < V; ++e) v[e] = 0.f;
+  }
+  __device__ __forceinline__ void keep() {}
+};
+template <int HOW, typename T>
+__device__ __forceinline__ void put_row(T* p, int count, const float (&f)[V]) {
+  if constexpr (HOW == kWhole) put_vec<true>(p, f);
+  else put_some<false>(p, count, f);
+}
+
 // what a thread knows of its channels
 struct Gain {
   float gamma[V], beta[V];
@@ -107,8 +163,20 @@ __device__ __forceinline__ void grads8(float (&x)[V], float (&d)[V], const float
   slope8(t, d, act);
 }
 
-// Sums two values of every channel over the `side` threads down a slab of `width` channels: in a[c] and b[c] of
-// a[side][width], b[side][width] afterwards.  Called by all T threads, after a barrier.
+// A thread's values of its channels in LDS, 16 bytes at a time
+__device__ __forceinline__ void lds_put(float* p, const float (&f)[V]) {
+  *reinterpret_cast<float4*>(p) = make_float4(f[0], f[1], f[2], f[3]);
+  *reinterpret_cast<float4*>(p + 4) = make_float4(f[4], f[5], f[6], f[7]);
+}
+__device__ __forceinline__ void lds_get(const float* p, float (&f)[V]) {
+  const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
+  f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w;
+  f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
+}
+
+// Sums two values of every channel over the `side` threads down a slab of `width` channels (rounded up to whole
+// vectors): in a[c] and b[c] of a[side][width], b[side][width] afterwards.  Called by all T threads, after a
+// barrier.
 template <int T>
 __device__ __forceinline__ void slab_sums(float* a, float* b, int width, int side) {
   const int parts = max(1, min(side, T / width));
@@ -182,47 +250,6 @@ struct GnHeld {
   int32_t per_group;
 };
 
-// A vector as it was loaded: bf16 stays packed until it is worked on
-template <typename T>
-struct Raw;
-template <>
-struct Raw<bf16_t> {
-  u32x4 u;
-  template <bool ALIGNED>
-  __device__ __forceinline__ void get(const bf16_t* p, int count) {
-    if (count >= V) {
-      const uint4 v = get16<ALIGNED>(p);
-      u = u32x4{v.x, v.y, v.z, v.w};
-    } else {
-      float f[V];
-      get_some<ALIGNED>(p, count, f);
-      const uint4 v = pack8(f);
-      u = u32x4{v.x, v.y, v.z, v.w};
-    }
-  }
-  __device__ __forceinline__ void zero() { u = u32x4{0, 0, 0, 0}; }
-  __device__ __forceinline__ void values(float (&f)[V]) const { unpack8(make_uint4(u.x, u.y, u.z, u.w), f); }
-  // (the compiler would otherwise keep what it has unpacked, twice the registers)
-  __device__ __forceinline__ void keep() { asm volatile("" : "+v"(u)); }
-};
-template <>
-struct Raw<float> {
-  float v[V];
-  template <bool ALIGNED>
-  __device__ __forceinline__ void get(const float* p, int count) {
-    get_some<ALIGNED>(p, count, v);
-  }
-  __device__ __forceinline__ void zero() {
-#pragma unroll
-    for (int e = 0; e < V; ++e) v[e] = 0.f;
-  }
-  __device__ __forceinline__ void values(float (&f)[V]) const {
-#pragma unroll
-    for (int e = 0; e < V; ++e) f[e] = v[e];
-  }
-  __device__ __forceinline__ void keep() {}
-};
-
 template <int T>
 struct HeldPlace {
   int img, c0, at, col, count, lane_row;  // col: the thread's first channel; at: within the slab
@@ -233,17 +260,19 @@ struct HeldPlace {
     c0 = (t - img * g.slabs) * g.width;
     lane_row = threadIdx.x / g.cols;
     at = (threadIdx.x - lane_row * g.cols) * V;
+    if (lane_row >= g.side) at = lane_row = 0;  // (threads left over load what the first does, and are done)
     col = c0 + at;
-    count = lane_row < g.side ? min(V, g.width - at) : 0;
+    count = threadIdx.x < (unsigned)(g.side * g.cols) ? min(V, g.width - at) : 0;
   }
 };
 
-template <typename TX, typename TY, bool ALIGNED, int NV, int T>
+template <typename TX, typename TY, int HOW, int NV, int T>
 __global__ __launch_bounds__(T) void gn_fwd_held_kernel(GnArgs a, GnHeld g, const TX* x, const float* gamma,
                                                         const float* beta, TY* y, float* mean, float* rstd) {
-  extern __shared__ float lds[];
-  float *s_a = lds, *s_b = s_a + g.side * g.width, *s_shift = s_b + g.side * g.width, *s_mean = s_shift + g.width,
-        *s_rstd = s_mean + g.width;
+  extern __shared__ __attribute__((aligned(16))) float lds[];
+  const int span = g.cols * V;
+  float *s_a = lds, *s_b = s_a + g.side * span, *s_shift = s_b + g.side * span, *s_mean = s_shift + span,
+        *s_rstd = s_mean + span;
   const HeldPlace<T> p(g);
   const int m = (int)a.m;
   Raw<TX> v[NV];
@@ -251,11 +280,12 @@ __global__ __launch_bounds__(T) void gn_fwd_held_kernel(GnArgs a, GnHeld g, cons
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
     v[i].zero();
-    if (p.count > 0 && p.lane_row + i * g.side < m) v[i].template get<ALIGNED>(xp + (int64_t)(p.lane_row + i * g.side) * a.ldx, p.count);
+    // (rows past the last are the last again)
+    if (i < g.rows) v[i].template get<HOW>(xp + (int64_t)min(p.lane_row + i * g.side, m - 1) * a.ldx, p.count);
   }
   const Gain gain(gamma, beta, p.count > 0 ? p.col : 0, p.count);
   // the first thread's mean of a channel is every thread's shift
-  if (p.lane_row == 0) {
+  if (p.lane_row == 0 && p.count > 0) {
     float t[V] = {};
     int rows = 0;
 #pragma unroll
@@ -267,20 +297,17 @@ __global__ __launch_bounds__(T) void gn_fwd_held_kernel(GnArgs a, GnHeld g, cons
 #pragma unroll
         for (int e = 0; e < V; ++e) t[e] += f[e];
       }
+    const float inv = 1.0f / (float)rows;
 #pragma unroll
-    for (int e = 0; e < V; ++e)
-      if (e < p.count) s_shift[p.at + e] = t[e] / (float)rows;
+    for (int e = 0; e < V; ++e) t[e] *= inv;
+    lds_put(s_shift + p.at, t);
   }
 #pragma unroll
   for (int i = 0; i < NV; ++i) v[i].keep();
   __syncthreads();
   if (p.count > 0) {
-    float shift[V], s1[V], s2[V];
-#pragma unroll
-    for (int e = 0; e < V; ++e) {
-      shift[e] = e < p.count ? s_shift[p.at + e] : 0.f;
-      s1[e] = s2[e] = 0.f;
-    }
+    float shift[V], s1[V] = {}, s2[V] = {};
+    lds_get(s_shift + p.at, shift);
 #pragma unroll
     for (int i = 0; i < NV; ++i)
       if (p.lane_row + i * g.side < m) {
@@ -294,17 +321,13 @@ __global__ __launch_bounds__(T) void gn_fwd_held_kernel(GnArgs a, GnHeld g, cons
         }
         row_done();
       }
-#pragma unroll
-    for (int e = 0; e < V; ++e)
-      if (e < p.count) {
-        s_a[p.lane_row * g.width + p.at + e] = s1[e];
-        s_b[p.lane_row * g.width + p.at + e] = s2[e];
-      }
+    lds_put(s_a + p.lane_row * span + p.at, s1);
+    lds_put(s_b + p.lane_row * span + p.at, s2);
   }
 #pragma unroll
   for (int i = 0; i < NV; ++i) v[i].keep();
   __syncthreads();
-  slab_sums<T>(s_a, s_b, g.width, g.side);
+  slab_sums<T>(s_a, s_b, span, g.side);
   const float rows = (float)m;
   for (int c = threadIdx.x; c < g.width; c += T) {  // each channel's mean and centred squares
     const float d = s_a[c] / rows;
@@ -327,11 +350,10 @@ __global__ __launch_bounds__(T) void gn_fwd_held_kernel(GnArgs a, GnHeld g, cons
   __syncthreads();
   if (p.count <= 0) return;
   float mu[V], scale[V];
+  lds_get(s_mean + p.at, mu);
+  lds_get(s_rstd + p.at, scale);
 #pragma unroll
-  for (int e = 0; e < V; ++e) {
-    mu[e] = e < p.count ? s_mean[p.at + e] : 0.f;
-    scale[e] = e < p.count ? s_rstd[p.at + e] * gain.gamma[e] : 0.f;
-  }
+  for (int e = 0; e < V; ++e) scale[e] *= gain.gamma[e];
   TY* yp = y + (int64_t)p.img * a.m * a.ldy + p.col;
 #pragma unroll
   for (int i = 0; i < NV; ++i)
@@ -341,18 +363,19 @@ __global__ __launch_bounds__(T) void gn_fwd_held_kernel(GnArgs a, GnHeld g, cons
 #pragma unroll
       for (int e = 0; e < V; ++e) f[e] = __builtin_fmaf(f[e] - mu[e], scale[e], gain.beta[e]);
       act8(f, a.act);
-      put_some<ALIGNED>(yp + (int64_t)(p.lane_row + i * g.side) * a.ldy, p.count, f);
+      put_row<HOW>(yp + (int64_t)(p.lane_row + i * g.side) * a.ldy, p.count, f);
       row_done();
     }
 }
 
 // sums: each image's sums of dt and dt xh, [img][2][c], or nullptr
-template <typename TX, typename TY, bool ALIGNED, int NV, int T>
+template <typename TX, typename TY, int HOW, int NV, int T>
 __global__ __launch_bounds__(T) void gn_bwd_held_kernel(GnArgs a, GnHeld g, const TY* dy, const TX* x, const float* mean,
                                                         const float* rstd, const float* gamma, const float* beta,
                                                         const TX* res, TX* dx, float* sums) {
-  extern __shared__ float lds[];
-  float *s_a = lds, *s_b = s_a + g.side * g.width, *s_h1 = s_b + g.side * g.width, *s_h2 = s_h1 + g.width;
+  extern __shared__ __attribute__((aligned(16))) float lds[];
+  const int span = g.cols * V;
+  float *s_a = lds, *s_b = s_a + g.side * span, *s_h1 = s_b + g.side * span, *s_h2 = s_h1 + span;
   const HeldPlace<T> p(g);
   const int m = (int)a.m;
   Raw<TX> v[NV];
@@ -363,10 +386,10 @@ __global__ __launch_bounds__(T) void gn_bwd_held_kernel(GnArgs a, GnHeld g, cons
   for (int i = 0; i < NV; ++i) {
     v[i].zero();
     d[i].zero();
-    const int64_t r = p.lane_row + i * g.side;
-    if (p.count > 0 && r < m) {
-      v[i].template get<ALIGNED>(xp + r * a.ldx, p.count);
-      d[i].template get<ALIGNED>(dp + r * a.ldy, p.count);
+    if (i < g.rows) {  // (rows past the last are the last again)
+      const int64_t r = min(p.lane_row + i * g.side, m - 1);
+      v[i].template get<HOW>(xp + r * a.ldx, p.count);
+      d[i].template get<HOW>(dp + r * a.ldy, p.count);
     }
   }
   const Gain gain(gamma, beta, p.count > 0 ? p.col : 0, p.count);
@@ -392,17 +415,13 @@ __global__ __launch_bounds__(T) void gn_bwd_held_kernel(GnArgs a, GnHeld g, cons
         }
         row_done();
       }
-#pragma unroll
-    for (int e = 0; e < V; ++e)
-      if (e < p.count) {
-        s_a[p.lane_row * g.width + p.at + e] = s1[e];
-        s_b[p.lane_row * g.width + p.at + e] = s2[e];
-      }
+    lds_put(s_a + p.lane_row * span + p.at, s1);
+    lds_put(s_b + p.lane_row * span + p.at, s2);
   }
 #pragma unroll
   for (int i = 0; i < NV; ++i) v[i].keep();
   __syncthreads();
-  slab_sums<T>(s_a, s_b, g.width, g.side);
+  slab_sums<T>(s_a, s_b, span, g.side);
   if (sums != nullptr)
     for (int c = threadIdx.x; c < g.width; c += T) {
       sums[(int64_t)p.img * 2 * a.c + p.c0 + c] = s_a[c];
@@ -427,11 +446,8 @@ __global__ __launch_bounds__(T) void gn_bwd_held_kernel(GnArgs a, GnHeld g, cons
   __syncthreads();
   if (p.count <= 0) return;
   float h1[V], h2[V];
-#pragma unroll
-  for (int e = 0; e < V; ++e) {
-    h1[e] = e < p.count ? s_h1[p.at + e] : 0.f;
-    h2[e] = e < p.count ? s_h2[p.at + e] : 0.f;
-  }
+  lds_get(s_h1 + p.at, h1);
+  lds_get(s_h2 + p.at, h2);
   TX* op = dx + (int64_t)p.img * a.m * a.lddx + p.col;
   const TX* rp = res != nullptr ? res + (int64_t)p.img * a.m * a.ldr + p.col : nullptr;
 #pragma unroll
@@ -439,14 +455,18 @@ __global__ __launch_bounds__(T) void gn_bwd_held_kernel(GnArgs a, GnHeld g, cons
     const int64_t r = p.lane_row + i * g.side;
     if (r < m) {
       float f[V], q[V] = {};
-      if (rp != nullptr) get_some<ALIGNED>(rp + r * a.ldr, p.count, q);
+      if (rp != nullptr) {
+        Raw<TX> w;
+        w.template get<HOW>(rp + r * a.ldr, p.count);
+        w.values(q);
+      }
       v[i].values(f);
 #pragma unroll
       for (int e = 0; e < V; ++e) {
         const float xh = (f[e] - mu[e]) * rs[e];
         f[e] = __builtin_fmaf(rs[e], __builtin_fmaf(dt[i][e], gain.gamma[e], -h1[e]) - xh * h2[e], q[e]);
       }
-      put_some<ALIGNED>(op + r * a.lddx, p.count, f);
+      put_row<HOW>(op + r * a.lddx, p.count, f);
       row_done();
     }
   }
@@ -488,7 +508,7 @@ __host__ __device__ __forceinline__ int entries(const GnArgs& a, const GnGrid& g
 
 // this thread's part of the block's rows and channels
 struct Place {
-  int img, c0, width, at, col, count;  // the slab's first channel and channels; the thread's, and how many lie inside
+  int img, c0, width, at, col, count;  // the slab's first channel and channels; the thread's, how many lie inside
   int64_t row, end;                    // first row within the image, and the range's end
   int lane_row;
   __device__ __forceinline__ Place(const GnArgs& a, const GnGrid& g) {
@@ -504,30 +524,30 @@ struct Place {
   }
 };
 
-// N rows of a thread, row, row + side, ..., those inside the range
-template <bool ALIGNED, int N, typename T>
-__device__ __forceinline__ void get_rows(const T* base, int64_t ld, int64_t row, int64_t end, int side, int count,
-                                         Raw<T> (&v)[N]) {
+// N rows of a thread, row, row + side, ... (past the range's end the last one again, or none)
+template <int HOW, int N, typename T>
+__device__ __forceinline__ void get_rows(const T* base, int64_t ld, int64_t row, const Place& p, int side, Raw<T> (&v)[N]) {
+  if (row >= p.end) return;
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     const int64_t r = row + i * side;
-    if (r < end) v[i].template get<ALIGNED>(base + r * ld, count);
-    else v[i].zero();
+    if constexpr (HOW == kWhole) v[i].template get<HOW>(base + min(r, p.end - 1) * ld, p.count);
+    else if (r < p.end) v[i].template get<HOW>(base + r * ld, p.count);  // (there are branches anyhow)
   }
 }
 
 // mean and centred squares of every entry of a block: part[img][chunk][entry]
-template <typename T, bool ALIGNED>
+template <typename T, int HOW>
 __global__ __launch_bounds__(kThreads) void gn_stats_kernel(GnArgs a, GnGrid g, const T* x, float2* part) {
-  __shared__ float s_a[kThreads * V], s_b[kThreads * V], s_shift[kSlab];
+  __shared__ __attribute__((aligned(16))) float s_a[kThreads * V], s_b[kThreads * V], s_shift[kSlab];
   const Place p(a, g);
   const T* xp = x + (int64_t)p.img * a.m * a.ldx + p.col;
   const int64_t first = (int64_t)blockIdx.x * g.rows;
   float shift[V], s1[V] = {}, s2[V] = {};
   Raw<T> v[kAhead];
-  if (p.count > 0) get_rows<ALIGNED>(xp, a.ldx, p.row, p.end, g.side, p.count, v);
+  if (p.count > 0) get_rows<HOW>(xp, a.ldx, p.row, p, g.side, v);
   // the first thread's mean of a channel is every thread's shift
-  if (p.lane_row == 0) {
+  if (p.lane_row == 0 && p.count > 0) {
     float t[V] = {};
     int rows = 0;
 #pragma unroll
@@ -539,14 +559,14 @@ __global__ __launch_bounds__(kThreads) void gn_stats_kernel(GnArgs a, GnGrid g, 
 #pragma unroll
         for (int e = 0; e < V; ++e) t[e] += f[e];
       }
+    const float inv = 1.0f / (float)rows;
 #pragma unroll
-    for (int e = 0; e < V; ++e)
-      if (e < p.count) s_shift[p.at + e] = t[e] / (float)rows;
+    for (int e = 0; e < V; ++e) t[e] *= inv;
+    lds_put(s_shift + p.at, t);
   }
   __syncthreads();
   if (p.count > 0) {
-#pragma unroll
-    for (int e = 0; e < V; ++e) shift[e] = e < p.count ? s_shift[p.at + e] : 0.f;
+    lds_get(s_shift + p.at, shift);
     for (int64_t r = p.row; r < p.end; r += (int64_t)kAhead * g.side) {
 #pragma unroll
       for (int i = 0; i < kAhead; ++i)
@@ -561,17 +581,13 @@ __global__ __launch_bounds__(kThreads) void gn_stats_kernel(GnArgs a, GnGrid g, 
           }
           row_done();
         }
-      get_rows<ALIGNED>(xp, a.ldx, r + (int64_t)kAhead * g.side, p.end, g.side, p.count, v);
+      get_rows<HOW>(xp, a.ldx, r + (int64_t)kAhead * g.side, p, g.side, v);
     }
-#pragma unroll
-    for (int e = 0; e < V; ++e)
-      if (e < p.count) {
-        s_a[p.lane_row * p.width + p.at + e] = s1[e];
-        s_b[p.lane_row * p.width + p.at + e] = s2[e];
-      }
+    lds_put(s_a + p.lane_row * g.slab + p.at, s1);
+    lds_put(s_b + p.lane_row * g.slab + p.at, s2);
   }
   __syncthreads();
-  slab_sums<kThreads>(s_a, s_b, p.width, g.side);
+  slab_sums<kThreads>(s_a, s_b, g.slab, g.side);
   const float rows = (float)(p.end - first);
   for (int c = threadIdx.x; c < p.width; c += kThreads) {
     const float d = s_a[c] / rows;
@@ -666,8 +682,8 @@ __device__ __forceinline__ void block_join(const GnArgs& a, const GnGrid& src, c
   __syncthreads();
 }
 
-template <typename TX, typename TY, bool ALIGNED>
-__global__ __launch_bounds__(kThreads, sizeof(TX) == 4 ? 3 : 4) void gn_fwd_kernel(GnArgs a, GnGrid g, GnGrid src, const TX* x, const float* gamma,
+template <typename TX, typename TY, int HOW>
+__global__ __launch_bounds__(kThreads, sizeof(TX) == 2 ? 4 : 3) void gn_fwd_kernel(GnArgs a, GnGrid g, GnGrid src, const TX* x, const float* gamma,
                                                           const float* beta, const float2* part, const float2* joined,
                                                           TY* y, float* mean, float* rstd) {
   __shared__ float2 s_join[kThreads];
@@ -677,8 +693,8 @@ __global__ __launch_bounds__(kThreads, sizeof(TX) == 4 ? 3 : 4) void gn_fwd_kern
   Raw<TX> v[kHalf], w[kHalf];
   const int64_t turn = (int64_t)kHalf * g.side;
   if (p.count > 0) {
-    get_rows<ALIGNED>(xp, a.ldx, p.row, p.end, g.side, p.count, v);
-    get_rows<ALIGNED>(xp, a.ldx, p.row + turn, p.end, g.side, p.count, w);
+    get_rows<HOW>(xp, a.ldx, p.row, p, g.side, v);
+    get_rows<HOW>(xp, a.ldx, p.row + turn, p, g.side, w);
   }
   const Gain gain(gamma, beta, p.count > 0 ? p.col : 0, p.count);
   if (joined == nullptr) block_join<true>(a, src, p, part, joined, s_join);
@@ -707,25 +723,25 @@ __global__ __launch_bounds__(kThreads, sizeof(TX) == 4 ? 3 : 4) void gn_fwd_kern
 #pragma unroll
         for (int e = 0; e < V; ++e) f[e] = __builtin_fmaf(f[e] - mu[e], scale[e], gain.beta[e]);
         act8(f, a.act);
-        put_some<ALIGNED>(yp + (r + i * g.side) * a.ldy, p.count, f);
+        put_row<HOW>(yp + (r + i * g.side) * a.ldy, p.count, f);
         row_done();
       }
   };
   for (int64_t r = p.row; r < p.end; r += 2 * turn) {
     write(r, v);
-    get_rows<ALIGNED>(xp, a.ldx, r + 2 * turn, p.end, g.side, p.count, v);
+    get_rows<HOW>(xp, a.ldx, r + 2 * turn, p, g.side, v);
     write(r + turn, w);
-    get_rows<ALIGNED>(xp, a.ldx, r + 3 * turn, p.end, g.side, p.count, w);
+    get_rows<HOW>(xp, a.ldx, r + 3 * turn, p, g.side, w);
   }
 }
 
 // Sums over a block's rows: of dt and of dt xh for each channel, sums[img][chunk][2][c], and of h and h xh for
 // each entry, part[img][chunk][entry]
-template <typename TX, typename TY, bool ALIGNED>
+template <typename TX, typename TY, int HOW>
 __global__ __launch_bounds__(kThreads) void gn_bwd_sums_kernel(GnArgs a, GnGrid g, const TY* dy, const TX* x,
                                                                const float* mean, const float* rstd, const float* gamma,
                                                                const float* beta, float* sums, float2* part) {
-  __shared__ float s_a[kThreads * V], s_b[kThreads * V];
+  __shared__ __attribute__((aligned(16))) float s_a[kThreads * V], s_b[kThreads * V];
   const Place p(a, g);
   if (p.count > 0) {
     constexpr int N = kHalf;
@@ -733,8 +749,8 @@ __global__ __launch_bounds__(kThreads) void gn_bwd_sums_kernel(GnArgs a, GnGrid 
     const TY* dp = dy + (int64_t)p.img * a.m * a.ldy + p.col;
     Raw<TX> v[N];
     Raw<TY> d[N];
-    get_rows<ALIGNED>(xp, a.ldx, p.row, p.end, g.side, p.count, v);
-    get_rows<ALIGNED>(dp, a.ldy, p.row, p.end, g.side, p.count, d);
+    get_rows<HOW>(xp, a.ldx, p.row, p, g.side, v);
+    get_rows<HOW>(dp, a.ldy, p.row, p, g.side, d);
     const Gain gain(gamma, beta, p.col, p.count);
     float mu[V], rs[V], s1[V] = {}, s2[V] = {};
     each_channel(p.col, p.count, g.per_group, [&](int e, int grp) __attribute__((always_inline)) {
@@ -756,18 +772,14 @@ __global__ __launch_bounds__(kThreads) void gn_bwd_sums_kernel(GnArgs a, GnGrid 
           }
           row_done();
         }
-      get_rows<ALIGNED>(xp, a.ldx, r + (int64_t)N * g.side, p.end, g.side, p.count, v);
-      get_rows<ALIGNED>(dp, a.ldy, r + (int64_t)N * g.side, p.end, g.side, p.count, d);
+      get_rows<HOW>(xp, a.ldx, r + (int64_t)N * g.side, p, g.side, v);
+      get_rows<HOW>(dp, a.ldy, r + (int64_t)N * g.side, p, g.side, d);
     }
-#pragma unroll
-    for (int e = 0; e < V; ++e)
-      if (e < p.count) {
-        s_a[p.lane_row * p.width + p.at + e] = s1[e];
-        s_b[p.lane_row * p.width + p.at + e] = s2[e];
-      }
+    lds_put(s_a + p.lane_row * g.slab + p.at, s1);
+    lds_put(s_b + p.lane_row * g.slab + p.at, s2);
   }
   __syncthreads();
-  slab_sums<kThreads>(s_a, s_b, p.width, g.side);
+  slab_sums<kThreads>(s_a, s_b, g.slab, g.side);
   float* out = sums + ((int64_t)p.img * g.chunks + blockIdx.x) * 2 * a.c + p.c0;
   for (int c = threadIdx.x; c < p.width; c += kThreads) {
     out[c] = s_a[c];
@@ -787,8 +799,8 @@ __global__ __launch_bounds__(kThreads) void gn_bwd_sums_kernel(GnArgs a, GnGrid 
   });
 }
 
-template <typename TX, typename TY, bool ALIGNED>
-__global__ __launch_bounds__(kThreads, sizeof(TX) < sizeof(TY) ? 2 : 3) void gn_bwd_kernel(GnArgs a, GnGrid g, GnGrid src, const TY* dy, const TX* x,
+template <typename TX, typename TY, int HOW>
+__global__ __launch_bounds__(kThreads, sizeof(TX) < sizeof(TY) || (sizeof(TX) == 4 && HOW == kWhole) ? 2 : 3) void gn_bwd_kernel(GnArgs a, GnGrid g, GnGrid src, const TY* dy, const TX* x,
                                                           const float* mean, const float* rstd, const float* gamma,
                                                           const float* beta, const TX* res, const float2* part,
                                                           const float2* joined, TX* dx) {
@@ -802,8 +814,8 @@ __global__ __launch_bounds__(kThreads, sizeof(TX) < sizeof(TY) ? 2 : 3) void gn_
   Raw<TX> v[N];
   Raw<TY> d[N];
   if (p.count > 0) {
-    get_rows<ALIGNED>(xp, a.ldx, p.row, p.end, g.side, p.count, v);
-    get_rows<ALIGNED>(dp, a.ldy, p.row, p.end, g.side, p.count, d);
+    get_rows<HOW>(xp, a.ldx, p.row, p, g.side, v);
+    get_rows<HOW>(dp, a.ldy, p.row, p, g.side, d);
   }
   const Gain gain(gamma, beta, p.count > 0 ? p.col : 0, p.count);
   if (joined == nullptr) block_join<false>(a, src, p, part, joined, s_join);
@@ -820,33 +832,37 @@ __global__ __launch_bounds__(kThreads, sizeof(TX) < sizeof(TY) ? 2 : 3) void gn_
   });
   for (int64_t r = p.row; r < p.end; r += (int64_t)N * g.side) {
     if (r != p.row) {
-      get_rows<ALIGNED>(xp, a.ldx, r, p.end, g.side, p.count, v);
-      get_rows<ALIGNED>(dp, a.ldy, r, p.end, g.side, p.count, d);
+      get_rows<HOW>(xp, a.ldx, r, p, g.side, v);
+      get_rows<HOW>(dp, a.ldy, r, p, g.side, d);
     }
 #pragma unroll
     for (int i = 0; i < N; ++i)
       if (r + i * g.side < p.end) {
         float f[V], t[V], q[V] = {};
-        if (rp != nullptr) get_some<ALIGNED>(rp + (r + i * g.side) * a.ldr, p.count, q);
+        if (rp != nullptr) {
+          Raw<TX> w;
+          w.template get<HOW>(rp + (r + i * g.side) * a.ldr, p.count);
+          w.values(q);
+        }
         v[i].values(f);
         d[i].values(t);
         grads8(f, t, mu, rs, gain, a.act);
 #pragma unroll
         for (int e = 0; e < V; ++e)
           t[e] = __builtin_fmaf(rs[e], __builtin_fmaf(t[e], gain.gamma[e], -h1[e]) - f[e] * h2[e], q[e]);
-        put_some<ALIGNED>(op + (r + i * g.side) * a.lddx, p.count, t);
+        put_row<HOW>(op + (r + i * g.side) * a.lddx, p.count, t);
         row_done();
       }
   }
 }
 
 // ---------------------------------------------------------------------------
-// f(TX, TY, ALIGNED)
+// f(TX, TY, how vectors are loaded)
 template <typename F>
-void with_types(const GnArgs& a, bool aligned, F&& f) {
+void with_types(const GnArgs& a, bool whole, F&& f) {
   auto typed = [&](auto x, auto y) {
-    if (aligned) f(x, y, std::true_type{});
-    else f(x, y, std::false_type{});
+    if (whole) f(x, y, std::integral_constant<int, kWhole>{});
+    else f(x, y, std::integral_constant<int, kAnywhere>{});
   };
   if (a.x_f32 && a.y_f32) typed(0.f, 0.f);
   else if (a.x_f32) typed(0.f, bf16_t{});
@@ -882,7 +898,7 @@ bool make_held(const GnArgs& a, int held_rows, GnHeld* g) {
   g->per_group = per;
   return true;
 }
-size_t held_lds(const GnHeld& g, int arrays) { return (size_t)(2 * g.side + arrays) * g.width * sizeof(float); }
+size_t held_lds(const GnHeld& g, int arrays) { return (size_t)(2 * g.side + arrays) * g.cols * V * sizeof(float); }
 
 // Rows that a thread of the held kernels holds at most: a row takes 4 registers of bf16 and 8 of fp32, the
 // backward two of them
@@ -916,17 +932,17 @@ hipError_t gn_fwd_launch(const GnArgs& a, const void* x, const float* gamma, con
                          float* rstd, void* ws, hipStream_t s) {
   GnHeld h;
   const bool held = make_held(a, held_fwd_rows(a), &h);
-  const bool aligned = a.ldx % V == 0 && a.ldy % V == 0 && (!held || h.width % V == 0 || h.slabs == 1);
-  with_types(a, aligned, [&](auto tx, auto ty, auto al) {
+  const bool whole = a.c % V == 0 && a.ldx % V == 0 && a.ldy % V == 0 && (!held || h.width % V == 0);
+  with_types(a, whole, [&](auto tx, auto ty, auto how) {
     using TX = decltype(tx);
     using TY = decltype(ty);
-    constexpr bool AL = decltype(al)::value;
+    constexpr int HOW = decltype(how)::value;
     const TX* xp = static_cast<const TX*>(x);
     TY* yp = static_cast<TY*>(y);
     if (held) {
       trace_begin(KC_GN_FWD);
       auto go = [&](auto nv) {
-        NUMBAT_LAUNCH((gn_fwd_held_kernel<TX, TY, AL, decltype(nv)::value, kHeldThreads>), dim3((unsigned)(a.n * h.slabs)),
+        NUMBAT_LAUNCH((gn_fwd_held_kernel<TX, TY, HOW, decltype(nv)::value, kHeldThreads>), dim3((unsigned)(a.n * h.slabs)),
                       dim3(kHeldThreads), held_lds(h, 3), s, a, h, xp, gamma, beta, yp, mean, rstd);
       };
       if constexpr (sizeof(TX) == 4) with_rows<2, 8>(h.rows, go);
@@ -938,7 +954,7 @@ hipError_t gn_fwd_launch(const GnArgs& a, const void* x, const float* gamma, con
     float2* joined = static_cast<float2*>(ws);
     float2* part = joined + (size_t)a.n * a.groups;
     trace_begin(KC_GN_STATS);
-    NUMBAT_LAUNCH((gn_stats_kernel<TX, AL>), blocks_of(a, g), dim3(kThreads), 0, s, a, g, xp, part);
+    NUMBAT_LAUNCH((gn_stats_kernel<TX, HOW>), blocks_of(a, g), dim3(kThreads), 0, s, a, g, xp, part);
     if (joins_in_block(a, g)) {
       joined = nullptr;
     } else {
@@ -947,7 +963,7 @@ hipError_t gn_fwd_launch(const GnArgs& a, const void* x, const float* gamma, con
     }
     trace_end(KC_GN_STATS);
     trace_begin(KC_GN_FWD);
-    NUMBAT_LAUNCH((gn_fwd_kernel<TX, TY, AL>), blocks_of(a, ga), dim3(kThreads), 0, s, a, ga, g, xp, gamma, beta, part,
+    NUMBAT_LAUNCH((gn_fwd_kernel<TX, TY, HOW>), blocks_of(a, ga), dim3(kThreads), 0, s, a, ga, g, xp, gamma, beta, part,
                   joined, yp, mean, rstd);
     trace_end(KC_GN_FWD);
   });
@@ -967,22 +983,22 @@ hipError_t gn_bwd_launch(const GnArgs& a, const void* dy, const void* x, const f
                          int accumulate, void* ws, hipStream_t s) {
   GnHeld h;
   const bool held = make_held(a, held_bwd_rows(a), &h);
-  const bool aligned = a.ldx % V == 0 && a.ldy % V == 0 && (dx == nullptr || a.lddx % V == 0) &&
-                       (res == nullptr || a.ldr % V == 0) && (!held || h.width % V == 0 || h.slabs == 1);
+  const bool whole = a.c % V == 0 && a.ldx % V == 0 && a.ldy % V == 0 && (dx == nullptr || a.lddx % V == 0) &&
+                     (res == nullptr || a.ldr % V == 0) && (!held || h.width % V == 0);
   const bool vectors = dgamma != nullptr || dbeta != nullptr;
   float* sums = static_cast<float*>(ws);
   int ranges = a.n;  // rows of sums
-  with_types(a, aligned, [&](auto tx, auto ty, auto al) {
+  with_types(a, whole, [&](auto tx, auto ty, auto how) {
     using TX = decltype(tx);
     using TY = decltype(ty);
-    constexpr bool AL = decltype(al)::value;
+    constexpr int HOW = decltype(how)::value;
     const TX *xp = static_cast<const TX*>(x), *rp = static_cast<const TX*>(res);
     const TY* dp = static_cast<const TY*>(dy);
     TX* op = static_cast<TX*>(dx);
     if (held) {
       trace_begin(KC_GN_BWD);
       auto go = [&](auto nv) {
-        NUMBAT_LAUNCH((gn_bwd_held_kernel<TX, TY, AL, decltype(nv)::value, kHeldThreads>), dim3((unsigned)(a.n * h.slabs)),
+        NUMBAT_LAUNCH((gn_bwd_held_kernel<TX, TY, HOW, decltype(nv)::value, kHeldThreads>), dim3((unsigned)(a.n * h.slabs)),
                       dim3(kHeldThreads), held_lds(h, 2), s, a, h, dp, xp, mean, rstd, gamma, beta, rp, op,
                       vectors ? sums : nullptr);
       };
@@ -996,7 +1012,7 @@ hipError_t gn_bwd_launch(const GnArgs& a, const void* dy, const void* x, const f
     float2* joined = reinterpret_cast<float2*>(sums + (size_t)ranges * 2 * a.c);
     float2* part = joined + (size_t)a.n * a.groups;
     trace_begin(KC_GN_BWD_SUMS);
-    NUMBAT_LAUNCH((gn_bwd_sums_kernel<TX, TY, AL>), blocks_of(a, g), dim3(kThreads), 0, s, a, g, dp, xp, mean, rstd, gamma,
+    NUMBAT_LAUNCH((gn_bwd_sums_kernel<TX, TY, HOW>), blocks_of(a, g), dim3(kThreads), 0, s, a, g, dp, xp, mean, rstd, gamma,
                   beta, sums, part);
     if (joins_in_block(a, g)) {
       joined = nullptr;
@@ -1007,7 +1023,7 @@ hipError_t gn_bwd_launch(const GnArgs& a, const void* dy, const void* x, const f
     trace_end(KC_GN_BWD_SUMS);
     if (dx != nullptr) {
       trace_begin(KC_GN_BWD);
-      NUMBAT_LAUNCH((gn_bwd_kernel<TX, TY, AL>), blocks_of(a, ga), dim3(kThreads), 0, s, a, ga, g, dp, xp, mean, rstd, gamma,
+      NUMBAT_LAUNCH((gn_bwd_kernel<TX, TY, HOW>), blocks_of(a, ga), dim3(kThreads), 0, s, a, ga, g, dp, xp, mean, rstd, gamma,
                     beta, rp, part, joined, op);
       trace_end(KC_GN_BWD);
     }
