@@ -94,12 +94,14 @@ class AttentionBlock:
         self.lse = new(rows * heads, torch.float32)
         self.norm = new(1, torch.float32)
         self.kept = None  # (rows, extents, whether with lengths) of the forward whose activations, statistics and weights are at hand
-        # all calls of the block are on one stream, one after another: they share a workspace
-        self.ws, self.ws_bytes = None, 0
+        # all calls of the block are on one stream, one after another: they share a workspace (one that was too
+        # small for a later batch is kept, as a captured graph may use it)
+        self.ws, self.ws_bytes, self.outgrown = None, 0, []
         self._workspace(nb.numbat_workspace_size(nb.OP_ADAMW, None))
 
     def _workspace(self, need):
         if need > self.ws_bytes:
+            self.outgrown.append(self.ws)
             self.ws, self.ws_bytes = workspace(need, self.device), need
         return self.ws
 

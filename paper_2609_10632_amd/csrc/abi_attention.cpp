@@ -125,7 +125,8 @@ numbat_status check_attention(const numbat_attention_problem* p, AttnArgs* a) {
   if (p->q_heads % p->kv_heads != 0)
     return fail(NUMBAT_ERR_BAD_DESC, "kv_heads = %d does not divide q_heads = %d", p->kv_heads, p->q_heads);
   if (p->causal != 0 && p->causal != 1) return fail(NUMBAT_ERR_BAD_DESC, "causal is 0 or 1");
-  if (!(p->scale > 0.0f && p->scale < 3.0e38f)) return fail(NUMBAT_ERR_BAD_DESC, "scale must be finite and above 0");
+  // (the kernels multiply it by log2(e))
+  if (!(p->scale > 0.0f && p->scale <= 1.0e38f)) return fail(NUMBAT_ERR_BAD_DESC, "scale must be above 0 and at most 1e38");
   if (p->reserved != 0) return fail(NUMBAT_ERR_BAD_DESC, "reserved must be 0");
   const int64_t qw = (int64_t)p->q_heads * p->d, kw = (int64_t)p->kv_heads * p->d;
   const int32_t group = p->q_heads / p->kv_heads;

@@ -31,7 +31,7 @@ __global__ __launch_bounds__(NW * 64, DP <= 64 || NW == 4 ? 2 : 1) void attn_fwd
   __shared__ __attribute__((aligned(1024))) unsigned char st1[2 * H::TILE];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int half = lane >> 5;
-  AttnPlace p(a, g);
+  AttnPlace p(a, g, NW > 1);
   if (a.causal) p.tile = g.tiles - 1 - p.tile;  // the longest first
   const Lengths n(a, p.b);
   const int cols = a.q_len * a.group, c0 = p.tile * NW * 32;

@@ -150,7 +150,7 @@ def test_attention_refusals(call, op):
     bad.struct_size += 8
     assert status_of(call, bad) == nb.ERR_VERSION
     for kw in ({"batch": -1}, {"q_len": -1}, {"kv_len": -1}, {"q_heads": 0}, {"kv_heads": 0}, {"kv_heads": 3}, {"d": 0},
-               {"scale": 0.0}, {"scale": -1.0}, {"scale": float("nan")}, {"scale": float("inf")}, {"q_row_stride": 248},
+               {"scale": 0.0}, {"scale": -1.0}, {"scale": float("nan")}, {"scale": float("inf")}, {"scale": 2e38}, {"q_row_stride": 248},
                {"y_row_stride": -256}, {"k_row_stride": 64}, {"v_row_stride": (1 << 21) + 8}):
         assert status_of(call, make(**kw)) == nb.ERR_BAD_DESC, kw
         assert status_of(nb.numbat_workspace_size, op, make(**kw)) == nb.ERR_BAD_DESC, kw
