@@ -211,11 +211,11 @@ __global__ __launch_bounds__(64) void attn_join_kernel(AttnArgs a, int splits, c
   }
 }
 
-int fwd_waves(const AttnArgs& a) { return attn_waves(a, (int64_t)a.q_len * a.group, true); }
+int fwd_waves(const AttnArgs& a) { return attn_waves(a, (int64_t)a.q_len * a.group, a.kv_len, true); }
 
 AttnGrid fwd_grid(const AttnArgs& a) {
   const int64_t columns = fwd_waves(a) * 32, tiles = ((int64_t)a.q_len * a.group + columns - 1) / columns;
-  return make_attn_grid(a, tiles, a.kv_len, fwd_waves(a) == 1 ? 1024 : 512, 256);
+  return make_attn_grid(a, tiles, a.kv_len, fwd_waves(a));
 }
 
 size_t columns_of(const AttnArgs& a) { return (size_t)a.batch * a.kv_heads * a.q_len * a.group; }

@@ -345,19 +345,19 @@ __global__ __launch_bounds__(64) void attn_bwd_join_kernel(AttnArgs a, int split
   }
 }
 
-int dq_waves(const AttnArgs& a) { return attn_waves(a, (int64_t)a.q_len * a.group, false); }
-int dkv_waves(const AttnArgs& a) { return attn_waves(a, a.kv_len, false); }
+int dq_waves(const AttnArgs& a) { return attn_waves(a, (int64_t)a.q_len * a.group, a.kv_len, false); }
+int dkv_waves(const AttnArgs& a) { return attn_waves(a, a.kv_len, (int64_t)a.q_len * a.group, false); }
 
 size_t columns_of(const AttnArgs& a) { return (size_t)a.batch * a.kv_heads * a.q_len * a.group; }
 size_t keys_of(const AttnArgs& a) { return (size_t)a.batch * a.kv_heads * a.kv_len; }
 
 AttnGrid dq_grid(const AttnArgs& a) {
   const int64_t side = dq_waves(a) * 32;
-  return make_attn_grid(a, ((int64_t)a.q_len * a.group + side - 1) / side, a.kv_len, 512, 256);
+  return make_attn_grid(a, ((int64_t)a.q_len * a.group + side - 1) / side, a.kv_len, dq_waves(a));
 }
 AttnGrid dkv_grid(const AttnArgs& a) {
   const int64_t side = dkv_waves(a) * 32;
-  return make_attn_grid(a, ((int64_t)a.kv_len + side - 1) / side, (int64_t)a.q_len * a.group, 512, 256);
+  return make_attn_grid(a, ((int64_t)a.kv_len + side - 1) / side, (int64_t)a.q_len * a.group, dkv_waves(a));
 }
 // dq and dkv run one after the other: their partials share their space
 size_t part_floats(const AttnArgs& a) {

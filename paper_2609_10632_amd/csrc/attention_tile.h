@@ -290,11 +290,15 @@ struct AttnPlace {
   }
 };
 
-// tiles * splits * sequences * heads; ranges where there would be fewer blocks than `want`, of `least` rows at least
-inline AttnGrid make_attn_grid(const AttnArgs& a, int64_t tiles, int64_t rows, int64_t want, int64_t least) {
+// Ranges of `rows` rows where there would be fewer than 512 blocks (1024 of one wave), of 256 rows at least
+inline int64_t attn_splits(int64_t blocks, int64_t rows, int waves) {
+  return std::clamp<int64_t>((waves == 1 ? 1024 : 512) / std::max<int64_t>(1, blocks), 1, std::max<int64_t>(1, rows / 256));
+}
+
+// tiles * splits * sequences * heads
+inline AttnGrid make_attn_grid(const AttnArgs& a, int64_t tiles, int64_t rows, int waves) {
   AttnGrid g;
-  const int64_t base = std::max<int64_t>(1, (int64_t)a.batch * a.kv_heads * tiles);
-  const int64_t splits = std::clamp<int64_t>(want / base, 1, std::max<int64_t>(1, rows / least));
+  const int64_t splits = attn_splits((int64_t)a.batch * a.kv_heads * tiles, rows, waves);
   int64_t per = (rows + splits - 1) / splits;
   per = std::max<int64_t>(kTile, (per + kTile - 1) / kTile * kTile);
   g.per_split = (int32_t)std::min<int64_t>(per, 1 << 30);
@@ -309,16 +313,17 @@ inline AttnGrid make_attn_grid(const AttnArgs& a, int64_t tiles, int64_t rows, i
 }
 
 // Waves of a block: four share a tile's loads, but a grid of few blocks, or blocks of few columns, leave less of the
-// card idle with two or one.  What counts is the waves' work on the fullest CU, times what a wave's work costs
+// card idle with two or one.  What counts is the waves' work on the fullest CU, ranges counted, times what it costs
 // with fewer to share the loads (4 x 8 heads, 4096 x 4096, d = 64, dq: 1.2 to 1.4 times in twos; forward of 16 x 6
 // heads of 1600 columns: 149 us in ones, 80 in fours; of 16 x 9 heads of 400: 19 us in fours, 16 in twos).
-inline int attn_waves(const AttnArgs& a, int64_t columns, bool one) {
+inline int attn_waves(const AttnArgs& a, int64_t columns, int64_t rows, bool one) {
   const int64_t heads = (int64_t)a.batch * a.kv_heads;
   int best = 4;
   double least = 1e300;
   for (int nw = 4; nw >= (one ? 1 : 2); nw /= 2) {
-    const int64_t blocks = heads * ((columns + nw * 32 - 1) / (nw * 32));
-    const double work = (double)((blocks + kCus - 1) / kCus * nw) * (nw == 4 ? 1.0 : nw == 2 ? 1.3 : 1.9);
+    const int64_t blocks = heads * ((columns + nw * 32 - 1) / (nw * 32)), splits = attn_splits(blocks, rows, nw);
+    const double work = (double)((blocks * splits + kCus - 1) / kCus * nw) / (double)splits *
+                        (nw == 4 ? 1.0 : nw == 2 ? 1.3 : 1.9);
     if (work < least) {
       least = work;
       best = nw;
