@@ -227,6 +227,8 @@ __device__ __forceinline__ void each_group(int c0, int width, int per_group, F&&
     f(grp, lo, hi, (int)threadIdx.x % lanes, lanes);
   }
 }
+// (what is no number stays that)
+__device__ __forceinline__ float not_below_zero(float t) { return t < 0.f ? 0.f : t; }
 __device__ __forceinline__ float lane_sum(float t, int lanes) {
   for (int o = lanes / 2; o > 0; o /= 2) t += __shfl_xor(t, o);
   return t;
@@ -336,7 +338,7 @@ __global__ __launch_bounds__(T) void gn_fwd_held_kernel(GnArgs a, GnHeld g, cons
   const float rows = (float)m;
   for (int c = threadIdx.x; c < g.width; c += T) {  // each channel's mean and centred squares
     const float d = s_a[c] / rows;
-    s_b[c] = fmaxf(__builtin_fmaf(-s_a[c], d, s_b[c]), 0.f);
+    s_b[c] = not_below_zero(__builtin_fmaf(-s_a[c], d, s_b[c]));
     s_a[c] = s_shift[c] + d;
   }
   __syncthreads();
@@ -596,7 +598,7 @@ __global__ __launch_bounds__(kThreads) void gn_stats_kernel(GnArgs a, GnGrid g, 
   const float rows = (float)(p.end - first);
   for (int c = threadIdx.x; c < p.width; c += kThreads) {
     const float d = s_a[c] / rows;
-    s_b[c] = fmaxf(__builtin_fmaf(-s_a[c], d, s_b[c]), 0.f);
+    s_b[c] = not_below_zero(__builtin_fmaf(-s_a[c], d, s_b[c]));
     s_a[c] = s_shift[c] + d;
   }
   __syncthreads();
@@ -639,7 +641,7 @@ __device__ __forceinline__ float2 join_stats(const GnArgs& a, const GnGrid& g, c
   t1 = lane_sum(t1, lanes);
   t2 = lane_sum(t2, lanes);
   const float inv = 1.0f / ((float)a.m * (float)g.per_group), d = t1 * inv;
-  return make_float2(shift + d, 1.0f / sqrtf(fmaxf(__builtin_fmaf(-t1, d, t2), 0.f) * inv + a.eps));
+  return make_float2(shift + d, 1.0f / sqrtf(not_below_zero(__builtin_fmaf(-t1, d, t2)) * inv + a.eps));
 }
 // the entries' sums, times what makes them means
 __device__ __forceinline__ float2 join_sums(const GnArgs& a, const GnGrid& g, const float2* part, int img, int grp,

@@ -132,6 +132,25 @@ def test_causal(size):
     both(*size, causal=True)  # (more queries than keys: the first see nothing)
 
 
+@pytest.mark.parametrize("feat", (32, 64, 96, 128))
+@pytest.mark.parametrize("batch,length,heads,kv_heads,causal", [
+    (4, 500, 16, 16, False),  # 256 blocks of four waves, one to a CU: as many waves as 512 of two, which cost more
+    (4, 500, 32, 16, True),
+    (3, 100, 24, 24, False),  # 72 blocks of four waves leave more of the card idle than 144 of two
+    (3, 100, 24, 24, True)])
+def test_waves_of_a_block(batch, length, heads, kv_heads, causal, feat):
+    both(batch, length, length, heads, kv_heads, feat, causal=causal)
+
+
+@pytest.mark.parametrize("causal", (False, True))
+def test_a_batch_in_the_order_of_its_work(causal):
+    """64 sequences of all lengths are taken longest first; 65 are not ordered."""
+    g = torch.Generator().manual_seed(8)
+    for batch in (64, 65):
+        lengths = torch.randint(0, 41, (batch,), generator=g).tolist()
+        both(batch, 40, 40, 2, 2, 32, causal=causal, q_lengths=lengths, kv_lengths=lengths[::-1])
+
+
 @pytest.mark.parametrize("causal", (False, True))
 @pytest.mark.parametrize("feat", (32, 64, 128))
 def test_padded_batches(feat, causal):

@@ -127,19 +127,23 @@ def test_forward_without_spread():
     close(rs, torch.full((1, 2), 1e-5 ** -0.5, dtype=D), 2 * U * 317, "rstd")
 
 
-def test_numbers_that_are_none_stay_in_their_group():
-    n, m, c, groups = 2, 40, 32, 4
+@pytest.mark.parametrize("m", (40, 20000))  # held, in passes
+def test_numbers_that_are_none_stay_in_their_group(m):
+    n, c, groups = 2, 32, 4
     x = matrix(n * m, c, 3, torch.bfloat16)
     p = problem(n, m, c, groups, "silu", "bf16", "bf16", 0, 1e-5)
-    clean, y = torch.empty((n * m, c), dtype=torch.bfloat16, device="cuda"), torch.empty((n * m, c), dtype=torch.bfloat16, device="cuda")
+    clean, y = (torch.empty((n * m, c), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    mu, rs = torch.zeros((n, groups), device="cuda"), torch.zeros((n, groups), device="cuda")
     ws = space(nb.OP_GROUP_NORM_FWD, p)
     nb.numbat_group_norm_fwd(p, x, None, None, clean, None, None, ws)
     x[5, 9] = float("nan")  # image 0, group 1
     x[m + 7, 30] = float("inf")  # image 1, group 3
-    nb.numbat_group_norm_fwd(p, x, None, None, y, None, None, ws)
+    nb.numbat_group_norm_fwd(p, x, None, None, y, mu, rs, ws)
     bad = torch.zeros((n * m, c), dtype=torch.bool, device="cuda")
     bad[:m, 8:16] = bad[m:, 24:] = True
     assert torch.equal(y[~bad], clean[~bad]) and bool(y[bad].isnan().all())
+    which = torch.tensor([[False, True, False, False], [False, False, False, True]], device="cuda")
+    assert torch.equal(rs.isnan(), which) and bool((~mu[which].isfinite()).all()) and bool(mu[~which].isfinite().all())
 
 
 def backward(n, m, c, groups, name="silu", xt="bf16", yt="bf16", pitch=0, affine=True, seed=0, wanted="xgb"):
