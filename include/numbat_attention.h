@@ -77,7 +77,7 @@ typedef struct {
   int32_t kv_heads;        /* heads of k and v; divides q_heads: head h of q reads head h / (q_heads / kv_heads) */
   int32_t d;               /* features of a head: a multiple of 8, at most 128 */
   int32_t causal;          /* 1: query i sees keys j <= i + (keys - queries), each sequence's own numbers */
-  float scale;             /* of the scores, above 0 and at most 1e38 */
+  float scale;             /* of the scores, above 0 and at most 1e38; what q_i k_j is has to be finite in fp32 */
   int32_t reserved;        /* 0 */
   int64_t q_row_stride;    /* q and dq; a multiple of 8, like the others */
   int64_t k_row_stride;    /* k and dk */

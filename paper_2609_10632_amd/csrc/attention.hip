@@ -7,7 +7,10 @@
 // second product's operand as they lie (attention_tile.h): y^T += v^T p^T.  k and v come by direct-to-LDS
 // loads into one of two stages while the other is worked on; q stays in registers.
 // The maximum is only raised where a score has passed it by 2^8: until then weights up to 2^8 do as well,
-// and the accumulators need no scaling.  Few columns over many keys (one new token) are split into ranges
+// and the accumulators need no scaling.  Weights are exp2(s scale log2(e) - unit) with the maximum's product
+// rounded once into unit, which all of a column's weights share; where that rounding could be more than a
+// small factor (scores past 10^4) the maximum is taken off the scores first, so that the largest key's weight
+// is one at any score.  Few columns over many keys (one new token) are split into ranges
 // of keys, whose results a second kernel joins.
 //
 // A tile's 64 x 32 scores cost a wave 128 d multiply-adds on the matrix unit, 32 cycles for each 32 x 32 x 16 of them,
@@ -25,10 +28,11 @@ namespace numbat {
 
 namespace {
 
-constexpr float kRaise = 8.f;  // (log2)
+constexpr float kRaise = 8.f;            // (log2)
+constexpr float kFar = 16384.f;  // a unit's rounding, and a range's logarithm's, is at most 2^-11 up to here
 
 template <int DP, int NW>
-__global__ __launch_bounds__(NW * 64, DP <= 64 || NW == 4 ? 2 : 1) void attn_fwd_kernel(AttnArgs a, AttnGrid g, float* part, float* part_lse) {
+__global__ __launch_bounds__(NW * 64, DP <= 64 || NW == 4 ? 2 : 1) void attn_fwd_kernel(AttnArgs a, AttnGrid g, float* part, float2* part_lse) {
   using H = Head<DP>;
   // a wave on its own reads operands ahead; waves that share a SIMD cover each other's reads (in either order within
   // 1%, but for d = 64: 4 x 8 heads, 4096 x 4096 155 us in the compiler's order, 164 pinned)
@@ -81,7 +85,11 @@ __global__ __launch_bounds__(NW * 64, DP <= 64 || NW == 4 ? 2 : 1) void attn_fwd
   f32x16 o[FB];
 #pragma unroll
   for (int f = 0; f < FB; ++f) o[f] = zeros16();
-  float most = -INFINITY, sum = 0.f;  // log2 of the weights' unit; this half's sum of weights
+  // A score's weight is exp2((s - base) scale_log2 - unit), base = 0 up to kFar; this half's sum of weights
+  float base = 0.f, unit = -INFINITY, sum = 0.f;
+  float limit = -INFINITY;  // the score from which on the maximum is raised
+  bool far = false;         // whether a column of the wave has a base
+  const float per_log2 = 1.0f / a.scale_log2;
 
   auto tile = [&](const unsigned char* st, int key) __attribute__((always_inline)) {
     f32x16 s[2];
@@ -103,22 +111,35 @@ __global__ __launch_bounds__(NW * 64, DP <= 64 || NW == 4 ? 2 : 1) void attn_fwd
     for (int i = 0; i < 2; ++i)
 #pragma unroll
       for (int r = 0; r < 16; ++r) top = fmaxf(top, s[i][r]);
-    top = half_max(top) * a.scale_log2;
-    if (__any(top > most + kRaise)) {
-      const float up = fmaxf(most, top), by = __builtin_amdgcn_exp2f(most - (up == -INFINITY ? 0.f : up));
-      most = up;
+    top = half_max(top);
+    if (far || __any(top > limit)) {
+      const float was = base, had = unit, at = top * a.scale_log2;
+      if (__builtin_fmaf(top - base, a.scale_log2, -unit) > 0.f) {  // (its weight would be above one)
+        const bool past = !(fabsf(at) <= kFar);
+        base = past ? top : 0.f;
+        unit = past ? 0.f : at;
+        limit = __builtin_fmaf(unit + kRaise, per_log2, base);
+      }
+      // (a column that has seen no key yet has nothing to scale)
+      const float by = had == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(__builtin_fmaf(was - base, a.scale_log2, had - unit));
       sum *= by;
 #pragma unroll
       for (int f = 0; f < FB; ++f)
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[f][r] *= by;
+      far = __any(base != 0.f);
+      if (far)
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[i][r] -= base;
     }
-    const float unit = most == -INFINITY ? 0.f : most;  // (a column that has seen no key yet)
+    const float less = unit == -INFINITY ? 0.f : unit;  // (a column that has seen no key yet)
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
-        s[i][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i][r], a.scale_log2, -unit));
+        s[i][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i][r], a.scale_log2, -less));
         sum += s[i][r];
       }
 #pragma unroll
@@ -146,23 +167,24 @@ __global__ __launch_bounds__(NW * 64, DP <= 64 || NW == 4 ? 2 : 1) void attn_fwd
   sum = half_sum(sum);
   const bool any = valid && !(sum == 0.f);  // (a sum that is no number stays one)
   const float inv = any ? 1.0f / sum : 0.f;
-  const float lse = any ? most + __builtin_amdgcn_logf(sum) : -INFINITY;  // (log2)
+  const float lse = any ? unit + __builtin_amdgcn_logf(sum) : -INFINITY;  // (log2, beside base)
+  if (!any) base = 0.f;
   if (!any)  // (what columns that count for nothing have added up)
 #pragma unroll
     for (int f = 0; f < FB; ++f) o[f] = zeros16();
   if (g.splits == 1) {
     store_row<FB>(a.out + ((int64_t)p.b * a.q_len + row) * a.ldy + head * a.d, inside, a.d, o, inv, half);
     if (a.lse != nullptr && inside && half == 0)
-      a.lse[((int64_t)p.b * a.kv_heads * a.group + head) * a.q_len + row] = lse * kLn2;
+      a.lse[((int64_t)p.b * a.kv_heads * a.group + head) * a.q_len + row] = __builtin_fmaf(base, a.scale, lse * kLn2);
   } else {
     const int64_t at = (((int64_t)p.split * a.batch + p.b) * a.kv_heads + p.h) * cols + col;
     store_part<FB>(part + at * a.d, inside, a.d, o, inv, half);
-    if (inside && half == 0) part_lse[at] = lse;
+    if (inside && half == 0) part_lse[at] = make_float2(base, lse);
   }
 }
 
 // the ranges' results weighted by their sums: a thread for 4 features of a column
-__global__ __launch_bounds__(64) void attn_join_kernel(AttnArgs a, int splits, const float* part, const float* part_lse) {
+__global__ __launch_bounds__(64) void attn_join_kernel(AttnArgs a, int splits, const float* part, const float2* part_lse) {
   const int per = a.d / 4, cols = a.q_len * a.group;
   const int64_t total = (int64_t)a.batch * a.kv_heads * cols;
   for (int64_t i = blockIdx.x * 64ll + threadIdx.x; i < total * per; i += gridDim.x * 64ll) {
@@ -170,18 +192,22 @@ __global__ __launch_bounds__(64) void attn_join_kernel(AttnArgs a, int splits, c
     const int f = (int)(i - c * per) * 4;
     // (eight ranges' loads in flight)
     constexpr int N = 8;
-    float top = -INFINITY, sum = 0.f;
+    float base = 0.f, unit = -INFINITY, sum = 0.f;  // the largest range's
     f32x4 y = {0.f, 0.f, 0.f, 0.f};
     for (int s = 0; s < splits; s += N) {
-      float lse[N];
+      float2 lse[N];
 #pragma unroll
       for (int e = 0; e < N; ++e) lse[e] = part_lse[min(s + e, splits - 1) * total + c];
 #pragma unroll
-      for (int e = 0; e < N; ++e) top = fmaxf(top, lse[e]);
+      for (int e = 0; e < N; ++e)
+        if (__builtin_fmaf(lse[e].x - base, a.scale_log2, lse[e].y - unit) > 0.f) {
+          base = lse[e].x;
+          unit = lse[e].y;
+        }
     }
-    const float unit = top == -INFINITY ? 0.f : top;
+    if (unit == -INFINITY) unit = 0.f;
     for (int s = 0; s < splits; s += N) {
-      float lse[N];
+      float2 lse[N];
       f32x4 v[N];
 #pragma unroll
       for (int e = 0; e < N; ++e) {
@@ -191,7 +217,9 @@ __global__ __launch_bounds__(64) void attn_join_kernel(AttnArgs a, int splits, c
       }
 #pragma unroll
       for (int e = 0; e < N; ++e) {
-        const float w = s + e < splits ? __builtin_amdgcn_exp2f(lse[e] - unit) : 0.f;
+        const float w = s + e < splits
+                            ? __builtin_amdgcn_exp2f(__builtin_fmaf(lse[e].x - base, a.scale_log2, lse[e].y - unit))
+                            : 0.f;
         sum += w;
 #pragma unroll
         for (int i = 0; i < 4; ++i) y[i] = __builtin_fmaf(w, v[e][i], y[i]);
@@ -207,7 +235,7 @@ __global__ __launch_bounds__(64) void attn_join_kernel(AttnArgs a, int splits, c
     *reinterpret_cast<uint2*>(a.out + ((int64_t)b * a.q_len + row) * a.ldy + head * a.d + f) = out;
     if (a.lse != nullptr && f == 0)
       a.lse[((int64_t)b * a.kv_heads * a.group + head) * a.q_len + row] =
-          sum == 0.f ? -INFINITY : (unit + __builtin_amdgcn_logf(sum)) * kLn2;
+          sum == 0.f ? -INFINITY : __builtin_fmaf(base, a.scale, (unit + __builtin_amdgcn_logf(sum)) * kLn2);
   }
 }
 
@@ -230,13 +258,13 @@ bool attn_fits(const AttnArgs& a) {
 
 size_t attn_fwd_ws(const AttnArgs& a) {
   const AttnGrid g = fwd_grid(a);
-  return g.splits > 1 ? g.splits * columns_of(a) * (a.d + 1) * sizeof(float) : 0;
+  return g.splits > 1 ? g.splits * columns_of(a) * (a.d + 2) * sizeof(float) : 0;
 }
 
 hipError_t attn_fwd_launch(const AttnArgs& a, void* ws, hipStream_t s) {
   const AttnGrid g = fwd_grid(a);
   float* part = static_cast<float*>(ws);
-  float* part_lse = part + (g.splits > 1 ? g.splits * columns_of(a) * a.d : 0);
+  float2* part_lse = reinterpret_cast<float2*>(part + (g.splits > 1 ? g.splits * columns_of(a) * a.d : 0));
   trace_begin(KC_ATTN_FWD);
   with_head(a.d, [&](auto dc) {
     constexpr int DP = decltype(dc)::value;
