@@ -137,7 +137,9 @@ numbat_status numbat_attention_fwd(const numbat_attention_problem* p, const void
  *   dv_j = sum_i P_ij dy_i,  ds_ij = P_ij (dy_i v_j - delta_i),  dq_i = scale sum_j ds_ij k_j,
  *   dk_j = scale sum_i ds_ij q_i          (sums over the heads of q that share a head of k and v)
  * dq, dk, dv: bf16, with the strides of q, k and v; zero behind the sequences' lengths, where q, k, v, y, dy and
- * lse are not read.  P and ds are rounded to bf16 for their products, sums are fp32.
+ * lse are not read.  P and ds are rounded to bf16 for their products, sums are fp32.  P comes from lse as fp32 holds
+ * it: its exponent is off by up to 2^-21 |lse|, so that P is off by as much as bf16's rounding where lse is 8192 and
+ * by a factor of 1.6 where it is 10^6.  The forward has no such bound.
  * ws: numbat_workspace_size(NUMBAT_OP_ATTENTION_BWD). */
 numbat_status numbat_attention_bwd(const numbat_attention_problem* p, const void* dy, const void* q, const void* k,
                                    const void* v, const void* y, const float* lse, const int32_t* q_lengths,

@@ -5,7 +5,9 @@ not.
 The scores here are exact in fp32 (a power of two times a small number, plus eighths where they are small enough for
 them), so that only what follows them rounds.  With g = s - max s, a weight's argument is off by 4 2^-24 |g| and
 its exponential by 2^-20 (twice where ranges are joined, whose logarithms are off by 2^-10 at most up to 2^14 and
-by 2^-24 of a sum's logarithm past it); a sum of n terms by (n + 8) 2^-24; weights and y are rounded to bf16."""
+by 2^-24 of a sum's logarithm past it); a sum of n terms by (n + 8) 2^-24; weights and y are rounded to bf16.
+Of the gradients' weights: lse and its product with log2(e) are rounded five times between the forward's
+logarithm and the backward's exponent, 5 2^-24 |lse| < 2^-21 |lse|."""
 import math
 
 import pytest
@@ -120,3 +122,27 @@ def test_scales(scale):
 def test_causal():
     levels = torch.tensor([(-1.0) ** j * ODD * 2.0 ** -(j % 7) for j in range(150)])
     forward(*inputs(levels, torch.zeros(150), 150, 2.0 ** 33), 1.0, causal=True)
+
+
+@pytest.mark.parametrize("rows,n", [(40, 200), (1, 3000), (300, 77)])
+@pytest.mark.parametrize("power", (10, 13, 16))
+def test_gradients_as_far_as_lse_allows(rows, n, power):
+    """A weight's exponent is off by 2^-21 |lse| where it is formed from an lse in fp32."""
+    g = torch.Generator().manual_seed(power)
+    small = torch.randint(-16, 17, (n,), generator=g).float() / 8
+    q, k, v, s = inputs(torch.full((n,), ODD), small, rows, 2.0 ** power)
+    p, y, lse, t = forward(q, k, v, s, 1.0)
+    dy = torch.randn((rows, FEAT), generator=g).bfloat16().cuda()
+    dq, dk, dv = (torch.full_like(a, 7.0) for a in (q, k, v))
+    nb.numbat_attention_bwd(p, dy, q, k, v, y, lse, None, None, dq, dk, dv,
+                            blocks.workspace(nb.numbat_workspace_size(nb.OP_ATTENTION_BWD, p)))
+    q, k, v, y, dy = (d(a) for a in (q, k, v, y, dy))
+    w = torch.softmax(t, 1)
+    off = torch.expm1(2 ** -21 * torch.logsumexp(t, 1).abs())[:, None] + 2 ** -20
+    ds = w * (dy @ v.t() - (dy * y).sum(1, keepdim=True))
+    ds_off = ds.abs() * (off + B + 4 * U) + w * (1 + off) * (FEAT + 16) * U * (dy.abs() @ v.abs().t() + (dy * y).abs().sum(1, keepdim=True))
+    for name, got, ref, bound in (
+            ("dq", dq, ds @ k, (ds_off + (n + 8) * 2 * U * ds.abs()) @ k.abs()),
+            ("dk", dk, ds.t() @ q, (ds_off + (rows + 8) * 2 * U * ds.abs()).t() @ q.abs()),
+            ("dv", dv, w.t() @ dy, (w * (B + off + (rows + 8) * 2 * U)).t() @ dy.abs())):
+        close(got, ref, bound * (1 + B) + B * ref.abs(), name)
