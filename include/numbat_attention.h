@@ -127,7 +127,8 @@ numbat_status numbat_rotary(const numbat_rotary_problem* p, const void* x, const
  * queries that see no key.  lse: fp32 [batch][q_heads][q_len] or NULL (the backward reads it).
  * Scores, their exponentials' sums and the sums of products are fp32; the weights exp(s - max) are rounded to bf16
  * for their product with v.  The value of a key that only some queries of a tile see (causal) has to be
- * finite for those that do not.
+ * finite for those that do not: what is no number there is multiplied by a weight of zero and reaches queries up to
+ * 127 rows before the key.
  * ws: numbat_workspace_size(NUMBAT_OP_ATTENTION_FWD), which may be 0. */
 numbat_status numbat_attention_fwd(const numbat_attention_problem* p, const void* q, const void* k, const void* v,
                                    const int32_t* q_lengths, const int32_t* kv_lengths, void* y, float* lse, void* ws,
@@ -140,6 +141,9 @@ numbat_status numbat_attention_fwd(const numbat_attention_problem* p, const void
  * lse are not read.  P and ds are rounded to bf16 for their products, sums are fp32.  P comes from lse as fp32 holds
  * it: its exponent is off by up to 2^-21 |lse|, so that P is off by as much as bf16's rounding where lse is 8192 and
  * by a factor of 1.6 where it is 10^6.  The forward has no such bound.
+ * Queries that see no key (causal, more queries than keys) are not taken in, whatever they hold.  Of the others q, k, v
+ * and dy have to be finite as in the forward: between a query and a key of the same tile that it does not see (causal;
+ * up to 128 rows apart) what is no number is multiplied by zero and reaches the gradients of both.
  * ws: numbat_workspace_size(NUMBAT_OP_ATTENTION_BWD). */
 numbat_status numbat_attention_bwd(const numbat_attention_problem* p, const void* dy, const void* q, const void* k,
                                    const void* v, const void* y, const float* lse, const int32_t* q_lengths,

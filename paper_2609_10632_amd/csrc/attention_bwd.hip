@@ -61,7 +61,7 @@ __global__ __launch_bounds__(NW * 64, DP <= 64 || NW == 4 ? 2 : 1) void attn_dq_
     df[k] = row_chunk(drow, valid, a.d, k, half);
   }
   // lse in base 2 and delta of the lane's column, which the other kernel reads too; a column that counts for
-  // nothing gets an lse of plus infinity, hence weights of zero
+  // nothing, or sees no key, gets an lse of plus infinity, hence weights of zero, and no delta, whatever it holds
   float2 stat = make_float2(INFINITY, 0.f);
   {
     const bf16_t* yrow = a.y + ((int64_t)p.b * a.q_len + row) * a.ldy + head * a.d;
@@ -75,10 +75,10 @@ __global__ __launch_bounds__(NW * 64, DP <= 64 || NW == 4 ? 2 : 1) void attn_dq_
 #pragma unroll
       for (int e = 0; e < 8; ++e) t = __builtin_fmaf(y[e], g8[e], t);
     }
-    stat.y = half_sum(t);
-    if (valid) {
+    t = half_sum(t);
+    if (keys > 0) {
       const float lse = a.lse[((int64_t)p.b * a.kv_heads * a.group + head) * a.q_len + row];
-      if (lse != -INFINITY) stat.x = lse * kLog2e;
+      if (lse != -INFINITY) stat = make_float2(lse * kLog2e, t);
     }
     if (inside && half == 0 && p.split == 0) rows[((int64_t)p.b * a.kv_heads + p.h) * cols + col] = stat;
   }
@@ -139,7 +139,7 @@ __global__ __launch_bounds__(NW * 64, DP <= 64 || NW == 4 ? 2 : 1) void attn_dq_
     step(st0, st1, key);
     if (key + kTile < block_end) step(st1, st0, key + kTile);
   }
-  if (!valid)
+  if (keys == 0)
 #pragma unroll
     for (int f = 0; f < FB; ++f) dq[f] = zeros16();
   if (g.splits == 1) {
@@ -176,11 +176,12 @@ __global__ __launch_bounds__(NW * 64, DP <= 64 || (NW == 4 && DP <= 96) ? 2 : 1)
     vf[k] = row_chunk(a.v + krow * a.ldv + p.h * a.d, valid, a.d, k, half);
   }
 
-  // columns that see a key of the block: all that count, or those from the first row that sees key k0 on
-  const int first_row = a.causal ? max(k0 - (n.kv - n.q), 0) : 0;
-  const int64_t want = max((int64_t)first_row * a.group / kTile * kTile, (int64_t)p.split * g.per_split);
+  // columns that see a key of the block: all that count, or those from the first row that sees key k0 on.  (The
+  // others of its tile are zeros, like those behind the end.)
   const int end = k0 < n.kv ? (int)min((int64_t)n.q * a.group, (int64_t)(p.split + 1) * g.per_split) : 0;
-  const int begin = (int)min(want, (int64_t)end);
+  const int first = (int)min(a.causal ? (int64_t)max(k0 - (n.kv - n.q), 0) * a.group : 0, (int64_t)end);
+  const int begin = (int)min(max((int64_t)(first / kTile * kTile), (int64_t)p.split * g.per_split), (int64_t)end);
+  auto sees = [&](int c) __attribute__((always_inline)) { return (uint32_t)(c - first) < (uint32_t)(end - first); };
 
   // Rows of q and dy of a tile of columns: bytes from the tile's first row
   using L = TileLoad<DP, NW>;
@@ -193,7 +194,7 @@ __global__ __launch_bounds__(NW * 64, DP <= 64 || (NW == 4 && DP <= 96) ? 2 : 1)
     for (int q = 0; q < L::N; ++q) {
       const int col = c + L::row(q, wave, lane), chunk = L::chunk(q, wave, lane);
       const int r = (int)fdiv((uint32_t)col, a.div_group), at = (col - r * a.group) * a.d + chunk * 8;
-      const bool counts = col < end && chunk * 8 < a.d;
+      const bool counts = sees(col) && chunk * 8 < a.d;
       const uint32_t vq = counts ? (uint32_t)((r - r0) * a.ldq + at) * 2 : kOob;
       const uint32_t vd = counts ? (uint32_t)((r - r0) * a.ldy + at) * 2 : kOob;
       lds_void_t* to = (lds_void_t*)(st + (q * NW + wave) * 1024);
@@ -203,7 +204,7 @@ __global__ __launch_bounds__(NW * 64, DP <= 64 || (NW == 4 && DP <= 96) ? 2 : 1)
   };
   const float2* stats = rows + ((int64_t)p.b * a.kv_heads + p.h) * cols;
   auto stat_of = [&](int c) __attribute__((always_inline)) {
-    return tid < kTile && c + tid < end ? stats[c + tid] : make_float2(INFINITY, 0.f);
+    return tid < kTile && sees(c + tid) ? stats[c + tid] : make_float2(INFINITY, 0.f);
   };
   auto put_stats = [&](int u, int c, float2 v) __attribute__((always_inline)) {
     if (tid < kTile) {
