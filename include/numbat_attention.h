@@ -129,6 +129,7 @@ numbat_status numbat_rotary(const numbat_rotary_problem* p, const void* x, const
  * for their product with v.  The value of a key that only some queries of a tile see (causal) has to be
  * finite for those that do not: what is no number there is multiplied by a weight of zero and reaches queries up to
  * 127 rows before the key.
+ * y or lse at the address of an operand or of each other: NUMBAT_ERR_BAD_DESC.
  * ws: numbat_workspace_size(NUMBAT_OP_ATTENTION_FWD), which may be 0. */
 numbat_status numbat_attention_fwd(const numbat_attention_problem* p, const void* q, const void* k, const void* v,
                                    const int32_t* q_lengths, const int32_t* kv_lengths, void* y, float* lse, void* ws,
@@ -144,6 +145,8 @@ numbat_status numbat_attention_fwd(const numbat_attention_problem* p, const void
  * Queries that see no key (causal, more queries than keys) are not taken in, whatever they hold.  Of the others q, k, v
  * and dy have to be finite as in the forward: between a query and a key of the same tile that it does not see (causal;
  * up to 128 rows apart) what is no number is multiplied by zero and reaches the gradients of both.
+ * dq, dk or dv at the address of an operand or of each other: NUMBAT_ERR_BAD_DESC (dk and dv are formed from q and dy
+ * after dq is written).
  * ws: numbat_workspace_size(NUMBAT_OP_ATTENTION_BWD). */
 numbat_status numbat_attention_bwd(const numbat_attention_problem* p, const void* dy, const void* q, const void* k,
                                    const void* v, const void* y, const float* lse, const int32_t* q_lengths,

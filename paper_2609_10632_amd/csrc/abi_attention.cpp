@@ -3,6 +3,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstring>
+#include <initializer_list>
 
 #include "../../include/numbat_attention.h"
 #include "abi_util.h"
@@ -110,6 +111,18 @@ numbat_status check_rotary(const numbat_rotary_problem* p, bool grid, RotaryArgs
     if (grid) a->extent[i] = make_fastdiv((uint32_t)p->extents[i]);
     for (int k = 0; k < p->pairs[i]; ++k, ++j)
       a->turns[j] = way * std::pow(p->base, p->shared ? -(double)j / (double)total : -(double)k / (double)p->pairs[i]);
+  }
+  return NUMBAT_OK;
+}
+
+// A result at the address of an operand, or of another result, that is there
+numbat_status check_apart(std::initializer_list<const void*> results, std::initializer_list<const void*> operands) {
+  for (auto r = results.begin(); r != results.end(); ++r) {
+    if (*r == nullptr) continue;
+    for (const void* o : operands)
+      if (*r == o) return fail(NUMBAT_ERR_BAD_DESC, "a result lies in an operand's buffer, which others still read");
+    for (auto q = results.begin(); q != r; ++q)
+      if (*r == *q) return fail(NUMBAT_ERR_BAD_DESC, "two results lie in one buffer");
   }
   return NUMBAT_OK;
 }
@@ -286,6 +299,8 @@ numbat_status numbat_attention_fwd(const numbat_attention_problem* p, const void
     return fail(NUMBAT_ERR_ALIGN, "q_lengths, kv_lengths and lse must be 4-byte aligned");
   st = check_ws(ws, ws_bytes, with_header(attn_fwd_ws(a)));
   if (st != NUMBAT_OK) return st;
+  st = check_apart({y, lse}, {q, k, v, q_lengths, kv_lengths});
+  if (st != NUMBAT_OK) return st;
   a.q = static_cast<const bf16_t*>(q);
   a.k = static_cast<const bf16_t*>(k);
   a.v = static_cast<const bf16_t*>(v);
@@ -314,6 +329,8 @@ numbat_status numbat_attention_bwd(const numbat_attention_problem* p, const void
   if (!aligned4(q_lengths) || !aligned4(kv_lengths) || !aligned4(lse))
     return fail(NUMBAT_ERR_ALIGN, "q_lengths, kv_lengths and lse must be 4-byte aligned");
   st = check_ws(ws, ws_bytes, with_header(attn_bwd_ws(a)));
+  if (st != NUMBAT_OK) return st;
+  st = check_apart({dq, dk, dv}, {dy, q, k, v, y, lse, q_lengths, kv_lengths});
   if (st != NUMBAT_OK) return st;
   a.q = static_cast<const bf16_t*>(q);
   a.k = static_cast<const bf16_t*>(k);
