@@ -19,6 +19,9 @@ constexpr int64_t kMaxStride = 1 << 21;  // a tile's rows stay within 31-bit byt
 bool stride_ok(int64_t stride, int64_t width) { return stride == 0 || (stride >= width && stride <= kMaxStride); }
 int64_t dense(int64_t stride, int64_t width) { return stride != 0 ? stride : width; }
 bool known_type(int32_t t) { return t == NUMBAT_TYPE_BF16 || t == NUMBAT_TYPE_F32; }
+// Launches report by hipGetLastError: an error that another caller's call has left there is not one of theirs, and would
+// keep the later kernels of an operator from being launched
+void drop_old_error() { (void)hipGetLastError(); }
 bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 
 template <typename P>
@@ -225,6 +228,7 @@ numbat_status numbat_group_norm_fwd(const numbat_group_norm_problem* p, const vo
                 (long long)a.ldx);
   st = check_ws(ws, ws_bytes, with_header(gn_fwd_ws(a)));
   if (st != NUMBAT_OK) return st;
+  drop_old_error();
   const hipError_t e = gn_fwd_launch(a, x, gamma, beta, y, mean, rstd, ws_body(ws), static_cast<hipStream_t>(stream));
   return e == hipSuccess ? ok() : hip_fail(e, "group norm forward launch");
 }
@@ -241,6 +245,7 @@ numbat_status numbat_group_norm_bwd(const numbat_group_norm_problem* p, const vo
   for (const float* f : {mean, rstd, gamma, beta, (const float*)dgamma, (const float*)dbeta})
     if (!aligned4(f)) return fail(NUMBAT_ERR_ALIGN, "mean, rstd, gamma, beta, dgamma and dbeta must be 4-byte aligned");
   if (gn_empty(a)) {  // empty sums
+    drop_old_error();
     if (!accumulate && dgamma != nullptr) e = fill_zero_launch(dgamma, a.c, s);
     if (!accumulate && dbeta != nullptr && e == hipSuccess) e = fill_zero_launch(dbeta, a.c, s);
     return e == hipSuccess ? ok() : hip_fail(e, "group norm backward launch");
@@ -263,6 +268,7 @@ numbat_status numbat_group_norm_bwd(const numbat_group_norm_problem* p, const vo
                 (long long)a.lddx, (long long)a.ldy);
   st = check_ws(ws, ws_bytes, with_header(gn_bwd_ws(a)));
   if (st != NUMBAT_OK) return st;
+  drop_old_error();
   e = gn_bwd_launch(a, dy, x, mean, rstd, gamma, beta, residual_grad, dx, dgamma, dbeta, accumulate != 0, ws_body(ws), s);
   return e == hipSuccess ? ok() : hip_fail(e, "group norm backward launch");
 }
@@ -280,6 +286,7 @@ numbat_status numbat_rotary(const numbat_rotary_problem* p, const void* x, const
     return fail(NUMBAT_ERR_BAD_DESC, "y in x's buffer needs its row stride (y %lld, x %lld)", (long long)a.ldy,
                 (long long)a.ldx);
   a.pos = positions;
+  drop_old_error();
   const hipError_t e = rotary_launch(a, x, y, static_cast<hipStream_t>(stream));
   return e == hipSuccess ? ok() : hip_fail(e, "rotary launch");
 }
@@ -308,6 +315,7 @@ numbat_status numbat_attention_fwd(const numbat_attention_problem* p, const void
   a.kv_lengths = kv_lengths;
   a.out = static_cast<bf16_t*>(y);
   a.lse = lse;
+  drop_old_error();
   const hipError_t e = attn_fwd_launch(a, ws_body(ws), static_cast<hipStream_t>(stream));
   return e == hipSuccess ? ok() : hip_fail(e, "attention forward launch");
 }
@@ -343,6 +351,7 @@ numbat_status numbat_attention_bwd(const numbat_attention_problem* p, const void
   a.dq = static_cast<bf16_t*>(dq);
   a.dk = static_cast<bf16_t*>(dk);
   a.dv = static_cast<bf16_t*>(dv);
+  drop_old_error();
   const hipError_t e = attn_bwd_launch(a, ws_body(ws), static_cast<hipStream_t>(stream));
   return e == hipSuccess ? ok() : hip_fail(e, "attention backward launch");
 }

@@ -385,7 +385,7 @@ hipError_t attn_bwd_launch(const AttnArgs& a, void* ws, hipStream_t s) {
                   dim3(64), 0, s, a, g.splits, part);
     trace_end(KC_ATTN_JOIN);
   };
-  hipError_t e = hipGetLastError();
+  hipError_t e = hipSuccess;
   with_head(a.d, [&](auto dc) {
     constexpr int DP = decltype(dc)::value;
     if (e == hipSuccess && a.q_len > 0) {
