@@ -666,14 +666,22 @@ bool joins_in_block(const GnArgs& a, const GnGrid& g) {
   return groups * g.chunks <= kJoinInBlock && groups <= kThreads;
 }
 
-// both joins of a group that its lanes have at hand: f(entry's result) for every channel
+// Joins every group, a wave for each.  (Groups of all images may be more than the waves of a launch, which end at 2^32
+// threads.)
 template <bool STATS>
 __global__ __launch_bounds__(kThreads) void gn_join_kernel(GnArgs a, GnGrid g, const float2* part, float2* joined) {
-  const int64_t i = (int64_t)blockIdx.x * (kThreads / 64) + threadIdx.x / 64;
-  if (i >= (int64_t)a.n * a.groups) return;
-  const int img = (int)(i / a.groups), grp = (int)(i - (int64_t)img * a.groups), lane = threadIdx.x % 64;
-  const float2 t = STATS ? join_stats(a, g, part, img, grp, lane, 64) : join_sums(a, g, part, img, grp, lane, 64);
-  if (lane == 0) joined[i] = t;
+  constexpr int kWaves = kThreads / 64;
+  for (int64_t i = (int64_t)blockIdx.x * kWaves + threadIdx.x / 64; i < (int64_t)a.n * a.groups; i += (int64_t)gridDim.x * kWaves) {
+    const int img = (int)(i / a.groups), grp = (int)(i - (int64_t)img * a.groups), lane = threadIdx.x % 64;
+    const float2 t = STATS ? join_stats(a, g, part, img, grp, lane, 64) : join_sums(a, g, part, img, grp, lane, 64);
+    if (lane == 0) joined[i] = t;
+  }
+}
+template <bool STATS>
+void join_launch(const GnArgs& a, const GnGrid& g, const float2* part, float2* joined, hipStream_t s) {
+  const int64_t joins = ((int64_t)a.n * a.groups + kThreads / 64 - 1) / (kThreads / 64);
+  NUMBAT_LAUNCH((gn_join_kernel<STATS>), dim3((unsigned)std::min<int64_t>(joins, 1 << 20)), dim3(kThreads), 0, s, a, g, part,
+                joined);
 }
 
 // s_join[group of the slab]: from the entries (joined == nullptr), or from what was joined before
@@ -965,8 +973,7 @@ hipError_t gn_fwd_launch(const GnArgs& a, const void* x, const float* gamma, con
     if (joins_in_block(a, g)) {
       joined = nullptr;
     } else {
-      const unsigned joins = (unsigned)(((int64_t)a.n * a.groups + kThreads / 64 - 1) / (kThreads / 64));
-      NUMBAT_LAUNCH((gn_join_kernel<true>), dim3(joins), dim3(kThreads), 0, s, a, g, part, joined);
+      join_launch<true>(a, g, part, joined, s);
     }
     trace_end(KC_GN_STATS);
     trace_begin(KC_GN_FWD);
@@ -1024,8 +1031,7 @@ hipError_t gn_bwd_launch(const GnArgs& a, const void* dy, const void* x, const f
     if (joins_in_block(a, g)) {
       joined = nullptr;
     } else if (dx != nullptr) {
-      const unsigned joins = (unsigned)(((int64_t)a.n * a.groups + kThreads / 64 - 1) / (kThreads / 64));
-      NUMBAT_LAUNCH((gn_join_kernel<false>), dim3(joins), dim3(kThreads), 0, s, a, g, part, joined);
+      join_launch<false>(a, g, part, joined, s);
     }
     trace_end(KC_GN_BWD_SUMS);
     if (dx != nullptr) {
