@@ -179,6 +179,19 @@ __device__ __forceinline__ void lds_get(const float* p, float (&f)[V]) {
   f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
 }
 
+// A thread's sums go into LDS, there added to those of before, and begin anew
+__device__ __forceinline__ void lds_close(float* p, float (&f)[V], bool first) {
+  if (!first) {
+    float t[V];
+    lds_get(p, t);
+#pragma unroll
+    for (int e = 0; e < V; ++e) f[e] += t[e];
+  }
+  lds_put(p, f);
+#pragma unroll
+  for (int e = 0; e < V; ++e) f[e] = 0.f;
+}
+
 // Sums two values of every channel over the `side` threads down a slab of `width` channels (rounded up to whole
 // vectors): in a[c] and b[c] of a[side][width], b[side][width] afterwards.  Called by all T threads, after a
 // barrier.
@@ -488,6 +501,7 @@ struct GnGrid {
   int32_t cols, side;         // threads across a slab and down
   int32_t chunks;             // ranges of rows
   int64_t rows;               // of a range (the last may have fewer)
+  int32_t run;                // rows whose sums a thread adds one after another, before it adds what they come to
   int32_t per_group;          // channels of a group
 };
 
@@ -504,6 +518,9 @@ GnGrid make_grid(const GnArgs& a, int64_t blocks, int64_t most) {
   const int64_t chunks = std::clamp<int64_t>(blocks / ((int64_t)a.n * g.slabs), 1, most);
   g.rows = std::max(least, (a.m + g.side * chunks - 1) / (g.side * chunks) * g.side);
   g.chunks = (int32_t)((a.m + g.rows - 1) / g.rows);
+  // 64 rows, or the root of a thread's where that is more: sums of few additions in a row, however long a range is
+  g.run = 64;
+  while ((int64_t)g.run * g.run < g.rows / g.side) g.run += 64;
   g.per_group = a.c / a.groups;
   return g;
 }
@@ -574,6 +591,9 @@ __global__ __launch_bounds__(kThreads) void gn_stats_kernel(GnArgs a, GnGrid g, 
   __syncthreads();
   if (p.count > 0) {
     lds_get(s_shift + p.at, shift);
+    float *at_a = s_a + p.lane_row * g.slab + p.at, *at_b = s_b + p.lane_row * g.slab + p.at;
+    int run = 0;
+    bool first_run = true;
     for (int64_t r = p.row; r < p.end; r += (int64_t)kAhead * g.side) {
 #pragma unroll
       for (int i = 0; i < kAhead; ++i)
@@ -589,9 +609,16 @@ __global__ __launch_bounds__(kThreads) void gn_stats_kernel(GnArgs a, GnGrid g, 
           row_done();
         }
       get_rows<HOW>(xp, a.ldx, r + (int64_t)kAhead * g.side, p, g.side, v);
+      run += kAhead;
+      if (run == g.run) {
+        lds_close(at_a, s1, first_run);
+        lds_close(at_b, s2, first_run);
+        run = 0;
+        first_run = false;
+      }
     }
-    lds_put(s_a + p.lane_row * g.slab + p.at, s1);
-    lds_put(s_b + p.lane_row * g.slab + p.at, s2);
+    lds_close(at_a, s1, first_run);
+    lds_close(at_b, s2, first_run);
   }
   __syncthreads();
   slab_sums<kThreads>(s_a, s_b, g.slab, g.side);
@@ -772,6 +799,9 @@ __global__ __launch_bounds__(kThreads) void gn_bwd_sums_kernel(GnArgs a, GnGrid 
       mu[e] = mean[(int64_t)p.img * a.groups + grp];
       rs[e] = rstd[(int64_t)p.img * a.groups + grp];
     });
+    float *at_a = s_a + p.lane_row * g.slab + p.at, *at_b = s_b + p.lane_row * g.slab + p.at;
+    int run = 0;
+    bool first_run = true;
     for (int64_t r = p.row; r < p.end; r += (int64_t)N * g.side) {
 #pragma unroll
       for (int i = 0; i < N; ++i)
@@ -789,9 +819,16 @@ __global__ __launch_bounds__(kThreads) void gn_bwd_sums_kernel(GnArgs a, GnGrid 
         }
       get_rows<HOW>(xp, a.ldx, r + (int64_t)N * g.side, p, g.side, v);
       get_rows<HOW>(dp, a.ldy, r + (int64_t)N * g.side, p, g.side, d);
+      run += N;
+      if (run == g.run) {
+        lds_close(at_a, s1, first_run);
+        lds_close(at_b, s2, first_run);
+        run = 0;
+        first_run = false;
+      }
     }
-    lds_put(s_a + p.lane_row * g.slab + p.at, s1);
-    lds_put(s_b + p.lane_row * g.slab + p.at, s2);
+    lds_close(at_a, s1, first_run);
+    lds_close(at_b, s2, first_run);
   }
   __syncthreads();
   slab_sums<kThreads>(s_a, s_b, g.slab, g.side);

@@ -67,3 +67,56 @@ def test_groups_past_the_waves_of_a_launch():
         db_size += h.abs().sum(0).view(-1) * (DEEP + n * U)
     within(dg, dg_ref, dg_size, "dgamma")
     within(db, db_ref, db_size, "dbeta")
+
+
+def long_rows(pattern, c, dtype):
+    """Rows of a constant each, `pattern` over and over in ranges."""
+    return pattern.to(dtype).cuda().repeat(256)[:, None].expand(-1, c).contiguous()
+
+
+# one image of 1032 channels: 256 ranges at most, a thread down a slab, so 4000 rows of each thread.  Numbers just
+# above one by half of what a sum in the thousands can hold: added one after another every addition is off to the
+# same side (a thousand times 2^-24 of the sum)
+C, RANGE, ODD = 1032, 4000, 0.49 * 2.0 ** -12
+
+
+def test_long_sums_of_squares():
+    v = (1 + ODD) ** 0.5
+    pattern = torch.tensor([0.0] * 8 + [v, -v] * (RANGE // 2 - 4))
+    x = long_rows(pattern, C, torch.float32)
+    m = x.shape[0]
+    p = nb.group_norm_problem(1, m, C, 3, x_type=nb.F32)
+    y = torch.empty((m, C), dtype=torch.bfloat16, device="cuda")
+    mean, rstd = torch.empty((1, 3), device="cuda"), torch.empty((1, 3), device="cuda")
+    print("group norm", 1, m, C, 3, flush=True)
+    nb.numbat_group_norm_fwd(p, x, None, None, y, mean, rstd, space(nb.OP_GROUP_NORM_FWD, p))
+    exact = pattern.double()
+    ref = 1 / torch.sqrt((exact ** 2).mean() + 1e-5)
+    close(mean, torch.zeros((1, 3), dtype=D), DEEP * v, "mean")
+    close(rstd, ref.expand(1, 3), ref * (DEEP + (DEEP * v * ref) ** 2 + 4 * U * v * ref), "rstd")
+    ref = (exact * ref)[:, None].expand(RANGE, C)
+    close(y[-RANGE:], ref, (2 * DEEP + 8 * U) * (1 + ref.abs()) + B * ref.abs(), "y")
+
+
+def test_long_sums():
+    pattern = torch.tensor([0.0] * 8 + [1 + ODD] * (RANGE - 8))
+    x = long_rows(pattern, C, torch.float32)
+    m = x.shape[0]
+    p = nb.group_norm_problem(1, m, C, 3, x_type=nb.F32, y_type=nb.F32)
+    mean, rstd, one = torch.empty((1, 3), device="cuda"), torch.empty((1, 3), device="cuda"), float(pattern[-1])
+    out = torch.empty_like(x)
+    print("group norm", 1, m, C, 3, flush=True)
+    nb.numbat_group_norm_fwd(p, x, None, None, out, mean, rstd, space(nb.OP_GROUP_NORM_FWD, p))
+    close(mean, pattern.double().mean().expand(1, 3), DEEP * one, "mean")
+    # x as a gradient: dbeta is its sum, dgamma that of its products with a norm of one
+    mean.zero_()
+    rstd.fill_(1.0)
+    xh = torch.ones_like(x)
+    dg, db = torch.empty(C, device="cuda"), torch.empty(C, device="cuda")
+    nb.numbat_group_norm_bwd(p, x, xh, mean, rstd, None, None, out, dg, db, False, space(nb.OP_GROUP_NORM_BWD, p))
+    total = 256 * pattern.double().sum()
+    for name, got in (("dgamma", dg), ("dbeta", db)):
+        close(got, total.expand(C), (DEEP + U) * total, name)
+    # dx = dy - mean(dy) - xh mean(dy xh), with xh = 1
+    ref = (pattern.double() - 2 * pattern.double().mean())[:, None].expand(RANGE, C)
+    close(out[-RANGE:], ref, 2 * (DEEP + 4 * U) * one + U * ref.abs(), "dx")
