@@ -43,9 +43,14 @@ class AttentionBlock:
     def __init__(self, images, extents, width, heads, kv_heads=None, groups=32, pairs=None, act="none", causal=False,
                  base=10000.0, eps=1e-5, state_bits=32, seed=0, device=DEV):
         kv_heads = heads if kv_heads is None else kv_heads
-        if width % heads or heads % kv_heads or width % groups or (width // heads) % 8:
+        extents = tuple(extents)
+        if min(width, heads, kv_heads, groups) < 1 or width % heads or heads % kv_heads or width % groups or (width // heads) % 8:
             raise ValueError("width: whole heads of a multiple of 8 features and whole groups; kv_heads divides heads")
-        self.images, self.extents, self.width, self.heads, self.kv_heads = images, tuple(extents), width, heads, kv_heads
+        if width // heads > 128:
+            raise ValueError(f"width: heads of {width // heads} features, at most 128")
+        if min(extents, default=0) < 1:
+            raise ValueError(f"extents: {extents}, at least one axis of at least one row")
+        self.images, self.extents, self.width, self.heads, self.kv_heads = images, extents, width, heads, kv_heads
         self.d, self.groups, self.causal, self.base, self.eps = width // heads, groups, causal, base, eps
         if pairs is None:
             each = self.d // 2 // len(self.extents)
@@ -53,6 +58,8 @@ class AttentionBlock:
         self.pairs = tuple(pairs)
         if self.pairs and len(self.pairs) != len(self.extents):
             raise ValueError("pairs: a number for each axis, or none at all")
+        if self.pairs and (len(self.pairs) > 4 or min(self.pairs) < 1 or 2 * sum(self.pairs) > self.d):
+            raise ValueError(f"pairs: {self.pairs}, at least 1 for each of at most 4 axes and {self.d // 2} in all")
         self.act, self.state_bits, self.steps, self.device = ACTS[act], state_bits, 0, device
         self.qkv_width = (heads + 2 * kv_heads) * self.d
         shapes = {"wqkv": (self.qkv_width, width), "bqkv": (self.qkv_width,), "wo": (width, heads * self.d), "bo": (width,),
@@ -145,7 +152,7 @@ class AttentionBlock:
         output buffer, in which x may not lie."""
         extents = self.extents if extents is None else tuple(extents)
         n = math.prod(extents)
-        if len(extents) != len(self.extents) or n < 1 or x.dim() != 2 or x.shape[0] % n or x.shape[0] > self.y.shape[0] \
+        if len(extents) != len(self.extents) or min(extents) < 1 or x.dim() != 2 or x.shape[0] % n or x.shape[0] > self.y.shape[0] \
                 or x.shape[0] // n > self.images:
             raise ValueError(f"x: whole maps of {extents}, at most {self.images} and {self.y.shape[0]} rows")
         rows, images = x.shape[0], x.shape[0] // n
