@@ -99,6 +99,7 @@ class AttentionBlock:
         self.dnormed, self.dqkv, self.dmixed, self.dx = bf(width), bf(self.qkv_width), bf(heads * self.d), bf(width)
         self.mean, self.rstd = new((images, groups), torch.float32), new((images, groups), torch.float32)
         self.lse = new(rows * heads, torch.float32)
+        self.lengths = new(images, torch.int32)  # of the forward that is kept, as its backward takes them
         self.norm = new(1, torch.float32)
         self.kept = None  # (rows, extents, whether with lengths) of the forward whose activations, statistics and weights are at hand
         # all calls of the block are on one stream, one after another: they share a workspace (one that was too
@@ -172,6 +173,8 @@ class AttentionBlock:
         if turn:
             nb.numbat_rotary(turn[0], self.qkv, None, self.qkv)
         q, k, v = self._cut(self.qkv, rows)
+        if keep and lengths is not None:
+            lengths = self.lengths[:images].copy_(lengths)
         nb.numbat_attention_fwd(att, q, k, v, lengths, lengths, self.mixed, self.lse if keep else None, ws)
         nb.numbat_linear_fwd(out, self.mixed, c["wo"], self.params["bo"], x, None, self.y, ws)
         self.kept = (rows, extents, lengths is not None) if keep else None
@@ -179,7 +182,8 @@ class AttentionBlock:
 
     def backward(self, x, g, extents=None, lengths=None, accumulate=False):
         """The gradients of sum(g y): parameters' into ``grads`` (accumulate: added), x's into the returned
-        buffer.  The last forward has to be of the same x, extents and lengths with keep, with no step() since."""
+        buffer.  The last forward has to be of the same x and extents with keep, with no step() since, and with
+        lengths if they are given here; what they were then is what counts."""
         extents = self.extents if extents is None else tuple(extents)
         if self.kept != (x.shape[0], extents, lengths is not None):
             raise RuntimeError(f"backward of {x.shape[0]} rows in {extents}{' with' if lengths is not None else ' without'} "
@@ -187,6 +191,8 @@ class AttentionBlock:
         rows, images = x.shape[0], x.shape[0] // math.prod(extents)
         stride, g_stride = self._check(x, "x", rows), self._check(g, "g", rows)
         self._check_lengths(lengths, images)
+        if lengths is not None:
+            lengths = self.lengths[:images]
         norm, qkv, out, out_grad, turn, att = self._problems(images, extents, stride, g_stride)
         size = nb.numbat_workspace_size
         ws = self._workspace(max(size(nb.OP_LINEAR_BWD_DATA, out_grad), size(nb.OP_LINEAR_BWD_WEIGHT, out_grad),
