@@ -101,6 +101,9 @@ class AttentionBlock:
         self.lse = new(rows * heads, torch.float32)
         self.lengths = new(images, torch.int32)  # of the forward that is kept, as its backward takes them
         self.norm = new(1, torch.float32)
+        # where results go that later calls of a forward, or of a backward, still read over their operands
+        self.written = {t.untyped_storage().data_ptr() for t in (self.y, self.normed, self.qkv, self.mixed)}
+        self.written_back = {t.untyped_storage().data_ptr() for t in (self.dnormed, self.dqkv, self.dmixed)}
         self.kept = None  # (rows, extents, whether with lengths) of the forward whose activations, statistics and weights are at hand
         # all calls of the block are on one stream, one after another: they share a workspace (one that was too
         # small for a later batch is kept, as a captured graph may use it)
@@ -133,10 +136,13 @@ class AttentionBlock:
         a, b = self.heads * self.d, (self.heads + self.kv_heads) * self.d
         return qkv[:rows, :a], qkv[:rows, a:b], qkv[:rows, b:]
 
-    def _check(self, t, what, rows):
+    def _check(self, t, what, rows, written):
+        """`written`: buffers that it may not lie in."""
         if t.dim() != 2 or t.shape != (rows, self.width) or t.dtype != torch.bfloat16 or t.stride(1) != 1 \
                 or (rows > 1 and t.stride(0) < self.width):
             raise ValueError(f"{what}: expected bf16 rows of {self.width}, {rows} of them")
+        if rows and t.untyped_storage().data_ptr() in written:
+            raise ValueError(f"{what}: lies in a buffer of the block that is written before it is read for the last time")
         return t.stride(0) if rows > 1 else self.width
 
     def _check_lengths(self, lengths, images):
@@ -150,17 +156,15 @@ class AttentionBlock:
         map that take part in attention (a padded batch of sequences), or None for all; a row behind them attends to
         nothing.  The norm's statistics are over all rows.  keep: for backward(); without, as in serving, the statistics
         are not written, and backward() refuses what an earlier forward has kept.  Returns a view of the block's
-        output buffer, in which x may not lie."""
+        output buffer, in which x may not lie; nor in one of its activations', or with keep of their gradients'."""
         extents = self.extents if extents is None else tuple(extents)
         n = math.prod(extents)
         if len(extents) != len(self.extents) or min(extents) < 1 or x.dim() != 2 or x.shape[0] % n or x.shape[0] > self.y.shape[0] \
                 or x.shape[0] // n > self.images:
             raise ValueError(f"x: whole maps of {extents}, at most {self.images} and {self.y.shape[0]} rows")
         rows, images = x.shape[0], x.shape[0] // n
-        stride = self._check(x, "x", rows)
+        stride = self._check(x, "x", rows, self.written | self.written_back if keep else self.written)
         self._check_lengths(lengths, images)
-        if rows and x.untyped_storage().data_ptr() == self.y.untyped_storage().data_ptr():
-            raise ValueError("x: lies in the block's own output, which this forward overwrites")
         self.kept = None
         norm, qkv, out, _, turn, att = self._problems(images, extents, stride, self.width)
         size = nb.numbat_workspace_size
@@ -183,13 +187,15 @@ class AttentionBlock:
     def backward(self, x, g, extents=None, lengths=None, accumulate=False):
         """The gradients of sum(g y): parameters' into ``grads`` (accumulate: added), x's into the returned
         buffer.  The last forward has to be of the same x and extents with keep, with no step() since, and with
-        lengths if they are given here; what they were then is what counts."""
+        lengths if they are given here; what they were then is what counts.  x or g may lie in the returned buffer (a
+        backward of x there is the last of its forward), not in the gradients of the block's activations."""
         extents = self.extents if extents is None else tuple(extents)
         if self.kept != (x.shape[0], extents, lengths is not None):
             raise RuntimeError(f"backward of {x.shape[0]} rows in {extents}{' with' if lengths is not None else ' without'} "
                                f"lengths: the last forward kept {self.kept or 'nothing'}, or a step followed it")
         rows, images = x.shape[0], x.shape[0] // math.prod(extents)
-        stride, g_stride = self._check(x, "x", rows), self._check(g, "g", rows)
+        stride = self._check(x, "x", rows, self.written | self.written_back)
+        g_stride = self._check(g, "g", rows, self.written_back)
         self._check_lengths(lengths, images)
         if lengths is not None:
             lengths = self.lengths[:images]
@@ -210,6 +216,8 @@ class AttentionBlock:
         nb.numbat_linear_bwd_weight(qkv, self.normed, self.dqkv, d["wqkv"], d["bqkv"], accumulate, ws)
         nb.numbat_group_norm_bwd(norm, self.dnormed, x, self.mean, self.rstd, self.params["gamma"], self.params["beta"],
                                  self.dx, d["gamma"], d["beta"], accumulate, ws, residual_grad=g)
+        if x.untyped_storage().data_ptr() == self.dx.untyped_storage().data_ptr():
+            self.kept = None  # (x has become its gradient)
         return self.dx[:rows]
 
     def step(self, lr, weight_decay=0.1, betas=(0.9, 0.95), eps=1e-8, max_norm=1.0):
