@@ -20,6 +20,7 @@ follow another of the same shape on synthetic maps:
 from __future__ import annotations
 
 import argparse
+import functools
 import math
 
 import torch
@@ -27,6 +28,17 @@ import torch
 from . import numbat as nb
 from .blocks import DEV, workspace
 from .mlp import ACTS, STATE_BLOCK
+
+
+def _on_its_device(call):
+    """A call of a block whose device is not the current one: the library launches on the current device."""
+    @functools.wraps(call)
+    def run(self, *a, **k):
+        if self.place.type != "cuda" or self.place.index == torch.cuda.current_device():
+            return call(self, *a, **k)
+        with torch.cuda.device(self.place):
+            return call(self, *a, **k)
+    return run
 
 
 class AttentionBlock:
@@ -97,6 +109,7 @@ class AttentionBlock:
         bf = lambda n: torch.empty((rows, n), dtype=torch.bfloat16, device=device)  # noqa: E731
         self.normed, self.qkv, self.mixed, self.y = bf(width), bf(self.qkv_width), bf(heads * self.d), bf(width)
         self.dnormed, self.dqkv, self.dmixed, self.dx = bf(width), bf(self.qkv_width), bf(heads * self.d), bf(width)
+        self.place = self.y.device
         self.mean, self.rstd = new((images, groups), torch.float32), new((images, groups), torch.float32)
         self.lse = new(rows * heads, torch.float32)
         self.lengths = new(images, torch.int32)  # of the forward that is kept, as its backward takes them
@@ -113,7 +126,7 @@ class AttentionBlock:
     def _workspace(self, need):
         if need > self.ws_bytes:
             self.outgrown.append(self.ws)
-            self.ws, self.ws_bytes = workspace(need, self.device), need
+            self.ws, self.ws_bytes = workspace(need, self.place), need
         return self.ws
 
     def _problems(self, images, extents, x_stride, g_stride):
@@ -139,17 +152,18 @@ class AttentionBlock:
     def _check(self, t, what, rows, written):
         """`written`: buffers that it may not lie in."""
         if t.dim() != 2 or t.shape != (rows, self.width) or t.dtype != torch.bfloat16 or t.stride(1) != 1 \
-                or (rows > 1 and t.stride(0) < self.width):
-            raise ValueError(f"{what}: expected bf16 rows of {self.width}, {rows} of them")
+                or (rows > 1 and t.stride(0) < self.width) or t.device != self.place:
+            raise ValueError(f"{what}: expected bf16 rows of {self.width}, {rows} of them, on the block's device")
         if rows and t.untyped_storage().data_ptr() in written:
             raise ValueError(f"{what}: lies in a buffer of the block that is written before it is read for the last time")
         return t.stride(0) if rows > 1 else self.width
 
     def _check_lengths(self, lengths, images):
         if lengths is not None and (lengths.dtype != torch.int32 or lengths.shape != (images,) or not lengths.is_contiguous()
-                                    or lengths.device.type != torch.device(self.device).type):
+                                    or lengths.device != self.place):
             raise ValueError(f"lengths: expected int32 [{images}] on the block's device")
 
+    @_on_its_device
     def forward(self, x, extents=None, lengths=None, keep=True):
         """x: bf16 [images prod(extents)][width], rows as far apart as its stride says.  extents: of this batch's
         maps (the block's unless given; at most as many rows).  lengths: int32 [images] on the device, the rows of each
@@ -184,6 +198,7 @@ class AttentionBlock:
         self.kept = (rows, extents, lengths is not None) if keep else None
         return self.y[:rows]
 
+    @_on_its_device
     def backward(self, x, g, extents=None, lengths=None, accumulate=False):
         """The gradients of sum(g y): parameters' into ``grads`` (accumulate: added), x's into the returned
         buffer.  The last forward has to be of the same x and extents with keep, with no step() since, and with
@@ -220,6 +235,7 @@ class AttentionBlock:
             self.kept = None  # (x has become its gradient)
         return self.dx[:rows]
 
+    @_on_its_device
     def step(self, lr, weight_decay=0.1, betas=(0.9, 0.95), eps=1e-8, max_norm=1.0):
         """One AdamW step from ``grads``; returns the device float that receives the gradients'
         norm, or None with max_norm = 0, which forms none."""
