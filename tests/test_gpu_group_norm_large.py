@@ -120,3 +120,60 @@ def test_long_sums():
     # dx = dy - mean(dy) - xh mean(dy xh), with xh = 1
     ref = (pattern.double() - 2 * pattern.double().mean())[:, None].expand(RANGE, C)
     close(out[-RANGE:], ref, 2 * (DEEP + 4 * U) * one + U * ref.abs(), "dx")
+
+
+@pytest.mark.parametrize("n,m,c,groups", [(2, 1100, 24, 3),     # held
+                                          (1, 2200, 40, 1),     # in passes
+                                          (3, 740, 45, 3)])     # rows that are no whole vectors
+def test_offsets_past_32_bits(n, m, c, groups):
+    """Rows 2^21 elements apart: elements and bytes pass 2^32.  The same bits as from dense rows."""
+    stride = 1 << 21
+    wide = torch.empty((n * m, stride), dtype=torch.bfloat16, device="cuda")
+    g = torch.Generator(device="cuda").manual_seed(1)
+    outs = []
+    gamma, beta = (torch.rand(c, generator=g, device="cuda") for _ in range(2))
+    x, dy, res = (torch.randn((n * m, c), generator=g, device="cuda").bfloat16() for _ in range(3))
+    print("group norm far rows", n, m, c, groups, flush=True)
+    for far in (False, True):
+        # (all of them beside each other in one matrix)
+        at = (lambda i: wide[:, 64 * i:64 * i + c]) if far else (lambda i: torch.empty((n * m, c), dtype=torch.bfloat16, device="cuda"))  # noqa: E731
+        y, dx, mine = at(0), at(1), [at(i + 2).copy_(t) for i, t in enumerate((x, dy, res))]
+        s = stride if far else 0
+        p = nb.group_norm_problem(n, m, c, groups, act=nb.ACT_SILU, x_row_stride=s, y_row_stride=s, r_row_stride=s, dx_row_stride=s)
+        mean, rstd = torch.empty((n, groups), device="cuda"), torch.empty((n, groups), device="cuda")
+        dg, db = torch.empty(c, device="cuda"), torch.empty(c, device="cuda")
+        nb.numbat_group_norm_fwd(p, mine[0], gamma, beta, y, mean, rstd, space(nb.OP_GROUP_NORM_FWD, p))
+        nb.numbat_group_norm_bwd(p, mine[1], mine[0], mean, rstd, gamma, beta, dx, dg, db, False, space(nb.OP_GROUP_NORM_BWD, p),
+                                 residual_grad=mine[2])
+        outs.append([t.contiguous() for t in (y, mean, rstd, dx, dg, db)])
+    for a, b, name in zip(*outs, ("y", "mean", "rstd", "dx", "dgamma", "dbeta")):
+        assert torch.equal(a, b), name
+
+
+@pytest.mark.parametrize("m", (40, 20000))  # held, in passes
+@pytest.mark.parametrize("bad", (float("nan"), float("inf")))
+def test_gradients_that_are_no_numbers_stay_in_their_group(m, bad):
+    n, c, groups = 2, 32, 4
+    g = torch.Generator().manual_seed(5)
+    x, dy = (torch.randn((n * m, c), generator=g).bfloat16().cuda() for _ in range(2))
+    p = nb.group_norm_problem(n, m, c, groups, act=nb.ACT_SILU)
+    mean, rstd = torch.zeros((n, groups), device="cuda"), torch.ones((n, groups), device="cuda")
+    ws = space(nb.OP_GROUP_NORM_BWD, p)
+
+    def call():
+        dx, dg, db = torch.empty_like(x), torch.empty(c, device="cuda"), torch.empty(c, device="cuda")
+        nb.numbat_group_norm_bwd(p, dy, x, mean, rstd, None, None, dx, dg, db, False, ws)
+        return dx, dg, db
+
+    clean = call()
+    for t, row, channel, image in ((dy, 5, 9, 0), (x, m + 7, 30, 1)):
+        was = t[row, channel].clone()
+        t[row, channel] = bad
+        got = call()
+        t[row, channel] = was
+        hit = torch.zeros((n * m, c), dtype=torch.bool, device="cuda")
+        hit[image * m:(image + 1) * m, channel // 8 * 8:channel // 8 * 8 + 8] = True
+        assert torch.equal(got[0][~hit], clean[0][~hit]) and not bool(got[0][hit].isfinite().any())
+        for now, then in zip(got[1:], clean[1:]):
+            own = torch.arange(c, device="cuda") == channel
+            assert torch.equal(now[~own], then[~own]) and not bool(now[own].isfinite().any())
