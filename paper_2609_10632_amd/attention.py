@@ -47,7 +47,9 @@ class AttentionBlock:
 
     extents: the axes of a map, the last the fastest: (height, width), (frames, height, width), or (tokens,).
     pairs: the pairs of features of each head that turn with each axis' position (an even share of half a head
-    unless given; () for none).  Parameters (fp32, views of one flat buffer): ``wqkv`` [(heads + 2 kv_heads) d][width],
+    unless given; () for none).  causal: a row attends to itself and the rows before it; the norm's mean and deviation
+    are over all rows all the same, so that through them a row's output depends on the rows behind it (a model that
+    generates rows one by one needs a norm of each row, as layer_norm_fwd is).  Parameters (fp32, views of one flat buffer): ``wqkv`` [(heads + 2 kv_heads) d][width],
     ``bqkv``, ``wo`` [width][heads d], ``bo``, ``gamma``, ``beta``; gradients of the same names in ``grads``.  The
     products read the bf16 ``copies`` of ``wqkv`` and ``wo``, which step() writes: who writes parameters by hand (a
     checkpoint's) writes those too."""
@@ -168,7 +170,9 @@ class AttentionBlock:
         """x: bf16 [images prod(extents)][width], rows as far apart as its stride says.  extents: of this batch's
         maps (the block's unless given; at most as many rows).  lengths: int32 [images] on the device, the rows of each
         map that take part in attention (a padded batch of sequences), or None for all; a row behind them attends to
-        nothing.  The norm's statistics are over all rows.  keep: for backward(); without, as in serving, the statistics
+        nothing.  They are the first rows of the map as it is laid out here, and their positions those of these extents:
+        maps padded at the bottom, not at the side.  The norm's statistics are over all rows, the padding's too, whose
+        values have to be finite and belong to the result.  keep: for backward(); without, as in serving, the statistics
         are not written, and backward() refuses what an earlier forward has kept.  Returns a view of the block's
         output buffer, in which x may not lie; nor in one of its activations', or with keep of their gradients'."""
         extents = self.extents if extents is None else tuple(extents)
