@@ -16,9 +16,9 @@
 // A tile's 64 x 32 scores cost a wave 128 d multiply-adds on the matrix unit, 32 cycles for each 32 x 32 x 16 of them,
 // and 160 vector instructions, 32 of them exponentials at a quarter of the rate: at d = 64 twice the matrix
 // unit's time, at d = 128 as much.  Two to four waves a SIMD cover one with the other.  2 x 32 heads on 2 x 8 of 8192
-// x 8192 causal, d = 128: 1.02 to 1.11 ms, 1083 TFLOP/s at best, of the 1218 that the largest library product reached
-// on that card (both are held by the card's power rather than by the matrix unit, which is busy 60% of the time at
-// 1.65 GHz).  16 x 9 heads of 400 x 400, d = 64: 15 us, of which the first loads, the last stores and the launch are
+// x 8192 causal, d = 128: 1.00 to 1.13 ms, 1098 TFLOP/s at best, of the 1218 that the largest library product reached
+// on that card (both are held by the card's power rather than by the matrix unit, which is busy 56 to 60% of the time
+// at 1.65 to 1.7 GHz).  16 x 9 heads of 400 x 400, d = 64: 15 us, of which the first loads, the last stores and the launch are
 // half.  One query of each of 8 x 32 heads over up to 8192 keys of 8 x 8: 48 us, 3.9 TB/s, with 4 us of the join.
 #include <algorithm>
 
@@ -35,7 +35,7 @@ template <int DP, int NW>
 __global__ __launch_bounds__(NW * 64, DP <= 64 || NW == 4 ? 2 : 1) void attn_fwd_kernel(AttnArgs a, AttnGrid g, float* part, float2* part_lse) {
   using H = Head<DP>;
   // a wave on its own reads operands ahead; waves that share a SIMD cover each other's reads (in either order within
-  // 1%, but for d = 64: 4 x 8 heads, 4096 x 4096 155 us in the compiler's order, 164 pinned)
+  // 1%, but for d = 64: 4 x 8 heads, 4096 x 4096 168 us in the compiler's order, 177 pinned)
   constexpr int KS = H::KS, FB = H::FB, AHEAD = NW == 1 ? 2 : 0;
   // one object per stage: the compiler then knows that a stage's reads do not wait for the loads in
   // flight into the other

@@ -245,9 +245,10 @@ struct Lengths {
 };
 
 // The sequence with the b-th most work of a batch of up to 64: the blocks of long sequences come first, so that the
-// last ones to run are short (gradients of 16 padded maps of 610 to 1600 pixels, 6 heads, d = 64: 178 us in the
-// sequences' own order, 166 in this).  Each wave ranks them for itself, which takes 3 us: blocks of one wave, whose
-// work is a few columns over a range of keys, take the sequences as they come.
+// last ones to run are short (gradients of 16 padded maps of 610 to 1600 pixels, 6 heads, d = 64: 176 us in the
+// sequences' own order, 163 in this; forward 57 and 53).  Each wave ranks them for itself, which takes 1 to 3 us and is
+// lost where a grid is one round of blocks (16 maps of up to 400 pixels, 9 heads: 13.5 us without, 14.5 with): blocks
+// of one wave, whose work is a few columns over a range of keys, take the sequences as they come.
 __device__ __forceinline__ int by_work(const AttnArgs& a, int b) {
   const int lane = threadIdx.x & 63;
   const Lengths n(a, min(lane, a.batch - 1));
