@@ -28,25 +28,30 @@ def d(t):
     return t.detach().cpu().to(D)
 
 
-def inputs(levels, small, rows, size, seed=0):
+def inputs(levels, small, rows, size, seed=0, feat=FEAT):
     """q, k, v of one head with q_i k_j = size levels[j] + small[j]."""
     n = len(levels)
-    q, k = torch.zeros((rows, FEAT)), torch.zeros((n, FEAT))
+    q, k = torch.zeros((rows, feat)), torch.zeros((n, feat))
     q[:, 0], q[:, 1] = size, 1.0
     k[:, 0], k[:, 1] = torch.as_tensor(levels), torch.as_tensor(small)
-    v = torch.randn((n, FEAT), generator=torch.Generator().manual_seed(seed))
+    v = torch.randn((n, feat), generator=torch.Generator().manual_seed(seed))
     q, k, v = (t.bfloat16().cuda() for t in (q, k, v))
     s = d(q) @ d(k).t()
     assert torch.equal(s, s.float().to(D))
     return q, k, v, s
 
 
-def forward(q, k, v, s, scale, causal=False):
+def forward(q, k, v, s, scale, causal=False, batch=1, heads=1):
+    """batch, heads: as many copies, which give the same results."""
     rows, n = s.shape
-    p = nb.attention_problem(1, rows, n, 1, 1, FEAT, causal=causal, scale=scale)
-    y, lse = torch.empty((rows, FEAT), dtype=torch.bfloat16, device="cuda"), torch.empty((1, 1, rows), device="cuda")
-    print("attention of far scores", rows, n, scale, float(s.min()), float(s.max()), flush=True)
-    nb.numbat_attention_fwd(p, q, k, v, None, None, y, lse, blocks.workspace(nb.numbat_workspace_size(nb.OP_ATTENTION_FWD, p)))
+    feat = q.shape[1]
+    p = nb.attention_problem(batch, rows, n, heads, heads, feat, causal=causal, scale=scale)
+    y, lse = torch.empty((batch * rows, heads * feat), dtype=torch.bfloat16, device="cuda"), torch.empty((batch, heads, rows), device="cuda")
+    print("attention of far scores", batch, heads, feat, rows, n, scale, float(s.min()), float(s.max()), flush=True)
+    nb.numbat_attention_fwd(p, *(t.repeat(batch, heads) for t in (q, k, v)), None, None, y, lse,
+                            blocks.workspace(nb.numbat_workspace_size(nb.OP_ATTENTION_FWD, p)))
+    assert torch.equal(y, y[:rows, :feat].repeat(batch, heads)) and torch.equal(lse, lse[:1, :1].expand(batch, heads, rows))
+    y, lse = y[:rows, :feat], lse[:1, :1]
     scale = float(torch.tensor(scale, dtype=torch.float32))
     t = s * scale
     if causal:
@@ -146,3 +151,19 @@ def test_gradients_as_far_as_lse_allows(rows, n, power):
             ("dk", dk, ds.t() @ q, (ds_off + (rows + 8) * 2 * U * ds.abs()).t() @ q.abs()),
             ("dv", dv, w.t() @ dy, (w * (B + off + (rows + 8) * 2 * U)).t() @ dy.abs())):
         close(got, ref, bound * (1 + B) + B * ref.abs(), name)
+
+
+@pytest.mark.parametrize("feat", (32, 40, 64, 96, 128))
+@pytest.mark.parametrize("batch,heads,rows,n", [(1, 1, 1, 4000), (1, 1, 70, 90), (3, 24, 100, 100), (4, 16, 500, 500)])
+@pytest.mark.parametrize("causal", (False, True))
+def test_widths_of_heads_and_blocks(feat, batch, heads, rows, n, causal):
+    """Every width of a head, in blocks of one, two and four waves; scores on both sides of where the maximum is taken off
+    first, with ties and contenders."""
+    g = torch.Generator().manual_seed(feat)
+    steps = torch.tensor([-1.0, -2.0 ** -6, 0.0, 2.0 ** -20, 2.0 ** -6, 0.5, 1.0])
+    levels = ODD * steps[torch.randint(0, 7, (n,), generator=g)]
+    small = torch.where(levels.abs() < 2.0 ** -10, torch.randint(-32, 33, (n,), generator=g).float() / 8, torch.zeros(n))
+    small = torch.where(levels == 0, small, torch.zeros(n))
+    for size in (2.0 ** 35, 2.0 ** 21):
+        for order in (slice(None), torch.arange(n - 1, -1, -1)):
+            forward(*inputs(levels[order], small[order], rows, size, feat=feat), 1.0, causal=causal, batch=batch, heads=heads)
