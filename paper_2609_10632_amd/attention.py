@@ -49,10 +49,12 @@ class AttentionBlock:
     pairs: the pairs of features of each head that turn with each axis' position (an even share of half a head
     unless given; () for none).  causal: a row attends to itself and the rows before it; the norm's mean and deviation
     are over all rows all the same, so that through them a row's output depends on the rows behind it (a model that
-    generates rows one by one needs a norm of each row, as layer_norm_fwd is).  Parameters (fp32, views of one flat buffer): ``wqkv`` [(heads + 2 kv_heads) d][width],
-    ``bqkv``, ``wo`` [width][heads d], ``bo``, ``gamma``, ``beta``; gradients of the same names in ``grads``.  The
-    products read the bf16 ``copies`` of ``wqkv`` and ``wo``, which step() writes: who writes parameters by hand (a
-    checkpoint's) writes those too."""
+    generates rows one by one needs a norm of each row, as layer_norm_fwd is).
+
+    Parameters (fp32, views of one flat buffer): ``wqkv`` [(heads + 2 kv_heads) d][width], ``bqkv``, ``wo``
+    [width][heads d], ``bo``, ``gamma``, ``beta``; gradients of the same names in ``grads``.  The products read the bf16
+    ``copies`` of ``wqkv`` and ``wo``, which step() writes: who writes parameters by hand (a checkpoint's) writes those
+    too."""
 
     def __init__(self, images, extents, width, heads, kv_heads=None, groups=32, pairs=None, act="none", causal=False,
                  base=10000.0, eps=1e-5, state_bits=32, seed=0, device=DEV):

@@ -14,11 +14,11 @@
 // of keys, whose results a second kernel joins.
 //
 // A tile's 64 x 32 scores cost a wave 128 d multiply-adds on the matrix unit, 32 cycles for each 32 x 32 x 16 of them,
-// and 160 vector instructions, 32 of them exponentials at a quarter of the rate: at d = 64 twice the matrix
-// unit's time, at d = 128 as much.  Two to four waves a SIMD cover one with the other.  2 x 32 heads on 2 x 8 of 8192
-// x 8192 causal, d = 128: 1.00 to 1.13 ms, 1098 TFLOP/s at best, of the 1218 that the largest library product reached
-// on that card (both are held by the card's power rather than by the matrix unit, which is busy 56 to 60% of the time
-// at 1.65 to 1.7 GHz).  16 x 9 heads of 400 x 400, d = 64: 15 us, of which the first loads, the last stores and the launch are
+// and 160 vector instructions, 32 of them exponentials at a quarter of the rate: at d = 64 twice the matrix unit's
+// time, at d = 128 as much.  Two to four waves a SIMD cover one with the other.  2 x 32 heads on 2 x 8 of 8192 x 8192
+// causal, d = 128: 1.00 to 1.13 ms, 1098 TFLOP/s at best, of the 1218 that the largest library product reached on that
+// card (both are held by the card's power rather than by the matrix unit, which is busy 56 to 60% of the time at 1.65
+// to 1.7 GHz).  16 x 9 heads of 400 x 400, d = 64: 15 us, of which the first loads, the last stores and the launch are
 // half.  One query of each of 8 x 32 heads over up to 8192 keys of 8 x 8: 48 us, 3.9 TB/s, with 4 us of the join.
 #include <algorithm>
 
@@ -28,7 +28,7 @@ namespace numbat {
 
 namespace {
 
-constexpr float kRaise = 8.f;            // (log2)
+constexpr float kRaise = 8.f;    // (log2)
 constexpr float kFar = 16384.f;  // a unit's rounding, and a range's logarithm's, is at most 2^-11 up to here
 
 template <int DP, int NW>

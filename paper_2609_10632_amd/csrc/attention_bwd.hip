@@ -3,19 +3,20 @@
 // as two kernels that each form P and ds anew, since a single one would have to add dq over blocks of
 // keys in an order that changes from run to run (or keep a copy of dq for each): seven products
 // where five would do.
-//   dq    first delta = sum dy y of each column, which it leaves for the other; a wave owns 32 columns and walks the keys, as in the forward: s^T = k q^T, dp^T = v dy^T,
-//         dq^T += k^T ds^T; k and v in LDS, q and dy in registers
+//   dq    first delta = sum dy y of each column, which it leaves for the other; a wave owns 32 columns and walks the
+//         keys, as in the forward: s^T = k q^T, dp^T = v dy^T, dq^T += k^T ds^T; k and v in LDS, q and dy in registers
 //   dkv   a wave owns 32 keys and walks the columns: s = q k^T, dp = dy v^T, dv^T += dy^T P, dk^T += q^T ds;
 //         q and dy in LDS, k and v in registers.  The heads that share a head of k and v are columns of one
 //         product, so their gradients are added in its sums.
 // Few columns, or few keys, are split into ranges of the other, whose sums a third kernel adds in order.
 //
-// Seven products of 2 d operations a pair and two exponentials.  2 x 16 heads on 2 x 8 of 8192 x 8192 causal, d = 128: dq
-// 0.72 ms (1140 TFLOP/s of its six d operations a pair), dkv 1.18 to 1.22 ms (900 to 930 of its eight), 1.83 to 1.96
-// together, against 1218 TFLOP/s of the largest library product.  dkv's accumulators, k and v take 192 registers of a lane at d = 128, so
-// that it runs one wave to a SIMD, its operands read two slices ahead; up to d = 96 two fit, which takes 4 x 8 heads of
-// 4096 x 4096 x 96 from 516 to 395 us.  16 padded maps of up to 1600 pixels, 6 heads, d = 64: 66 to 70 and 85 to 94 us; there the
-// vector work is more than the products, and the last blocks of long maps run alone.
+// Seven products of 2 d operations a pair and two exponentials.  2 x 16 heads on 2 x 8 of 8192 x 8192 causal, d = 128:
+// dq 0.72 ms (1140 TFLOP/s of its six d operations a pair), dkv 1.18 to 1.22 ms (900 to 930 of its eight), 1.83 to
+// 1.96 together, against 1218 TFLOP/s of the largest library product.  dkv's accumulators, k and v take 192 registers
+// of a lane at d = 128, so that it runs one wave to a SIMD, its operands read two slices ahead; up to d = 96 two fit,
+// which takes 4 x 8 heads of 4096 x 4096 x 96 from 516 to 395 us.  16 padded maps of up to 1600 pixels, 6 heads, d =
+// 64: 66 to 70 and 85 to 94 us; there the vector work is more than the products, and the last blocks of long maps run
+// alone.
 #include <algorithm>
 #include <type_traits>
 
